@@ -80,7 +80,9 @@ enum {
   IG_K_COPY = 7,     /* ig_copy_bytes */
   IG_K_READ = 8,     /* ig_read_bytes */
   IG_K_LAYER = 9,    /* ig_layer_step: next layer's scan + this layer's prefetch and attention, one launch */
-  IG_K_COUNT = 10
+  IG_K_CACHE = 10,   /* ig_cache_attention, ig_tree_attention: every launch of a call */
+  IG_K_EVICT = 11,   /* ig_pool_evict */
+  IG_K_COUNT = 12
 };
 
 typedef struct ig_ctx ig_ctx;
@@ -381,6 +383,73 @@ int ig_gather_attention(ig_ctx *ctx, const ig_desc *desc, const void *q, const v
                         const void *Vpool, const int32_t *sel_idx, int32_t sel_stride,
                         const int32_t *sel_cnt, void *K_sel, void *V_sel, const void *k_new,
                         const void *v_new, void *out, void *stream);
+
+/* ---- attention over a whole pool, eviction by its weights, drafted tokens -------------------- */
+
+/* Baseline to the lists: attention that sees every valid slot of a pool, the eviction by accumulated
+ * attention weight that Section 2.3 and Section 5.1 compare with, and the verification of drafted
+ * tokens over the same pool.  Common to the calls below:
+ *  - Pools in device memory, [B, H, N_cap, d] of desc->dtype; d = 32, 64, 128 or 256 (IG_ESHAPE
+ *    otherwise) in the attention calls, any multiple of 16 bytes in the other two.
+ *  - group >= 1 query heads share a pool: query head h * group + g reads pool head h (group = 1: as
+ *    many query heads as pools).  B, H of the descriptor count pools; r is only used with a slab, alpha
+ *    and rope are not used.
+ *  - kv_len: device int32 [B], valid slots of each sequence, or NULL: N for all.  Clamped to [0, N]; N
+ *    is the largest length the call may meet and sizes its grid.  N = 0 is allowed.
+ *  - Rows of the valid slots are expected to be finite.  What lies in other slots is never used,
+ *    whatever it holds.
+ *  - mass: device float32 [B*H, N_cap], one sum per slot, zero-initialised by the caller.  born: device
+ *    int32 [B*H, N_cap], the position of the token a slot holds (the stamps of IG_POLICY_FIFO). */
+
+/* Attention of n_q tokens per sequence that are in the cache already (a prompt, a chunk of one; n_q = 1:
+ * the single-token form of a decode step), with the weight every slot receives:
+ *   query i of sequence b is slot s = kv_len[b] - q_len[b] + i and sees the slots t <= s
+ *   p = softmax_t(scale * q . K),  out = sum_t p V,  mass[b*H+h, t] += sum over queries and their heads of p
+ * q, out: device [B, n_q, H*group, d], 16-byte aligned.  q_len: device int32 [B], clamped to [0, n_q], or
+ * NULL: n_q; rows from q_len[b] on are left as they were.  A query that sees no slot (s < 0) gets zeros.
+ * mass may be NULL; with it, sums run in a fixed order (repeatable bit for bit). */
+int ig_cache_attention(ig_ctx *ctx, const ig_desc *desc, int32_t group, int32_t n_q, const void *q,
+                       const int32_t *q_len, const void *Kpool, const void *Vpool, const int32_t *kv_len,
+                       float *mass, void *out, void *stream);
+
+/* Attention of a tree of n_tree <= 64 drafted tokens (nodes) per sequence over its cache: node i sees every
+ * valid slot of the pool and the nodes j whose bit j of visible[b, i] is set (itself only if bit i is).
+ * q, out: device [B, n_tree, H*group, d]; k_tree, v_tree: device [B, n_tree, H, d], the nodes' keys
+ * (skewed, like the pool's) and values; all 16-byte aligned.  visible: device uint64 [B, n_tree].
+ * tree_len: device int32 [B], nodes of each sequence, clamped to [0, n_tree], or NULL: n_tree; rows from
+ * there on are left as they were, bits from there on are not used.  A node that sees nothing gets zeros. */
+int ig_tree_attention(ig_ctx *ctx, const ig_desc *desc, int32_t group, int32_t n_tree, const void *q,
+                      const void *k_tree, const void *v_tree, const uint64_t *visible,
+                      const int32_t *tree_len, const void *Kpool, const void *Vpool, const int32_t *kv_len,
+                      void *out, void *stream);
+
+/* Size the workspace of ig_cache_attention, ig_tree_attention and ig_pool_evict for up to n_q query tokens of
+ * `group` heads a pool and desc->N_cap slots (allocates; synchronous), as ig_reserve does for the calls above. */
+int ig_reserve_cache(ig_ctx *ctx, const ig_desc *desc, int32_t group, int32_t n_q);
+
+/* ig_append_token for several rows and ragged sequences: the accepted path of a tree, or a prompt's rows.
+ * For j < n_append[b], slot kv_len[b] + j of every pool of sequence b receives row path[b, j] of k_rows, v_rows
+ * (device [B, n_rows, H, d], 16-byte aligned); slots >= N_cap are skipped.  path: device int32 [B, n_rows],
+ * entries clamped to [0, n_rows), or NULL: row j.  n_append: device int32 [B], clamped to [0, n_rows], or
+ * NULL: n_rows.  Here kv_len is the length before the append (NULL: N).  mass, if given, restarts at 0 in
+ * these slots, born, if given, becomes pos[b] + j (pos: device int32 [B], or NULL: the slot).  slab with
+ * idx_dev, if given, receives the kept key channels as in ig_append_token.  The caller then adds n_append
+ * to kv_len. */
+int ig_append_rows(ig_ctx *ctx, const ig_desc *desc, int32_t n_rows, const void *k_rows, const void *v_rows,
+                   const int32_t *path, const int32_t *n_append, const int32_t *kv_len, const int32_t *pos,
+                   const int32_t *idx_dev, void *slab, void *Kpool, void *Vpool, float *mass, int32_t *born,
+                   void *stream);
+
+/* Eviction down to `keep` >= 1 slots of every pool, in place.  Of the kv_len[b] valid slots those stay that come
+ * first by: born >= protect_from[b] (protect_from: device int32 [B], or NULL: none; needs born), then the
+ * larger mass (NaN smallest), then the lower slot.  Slots >= keep that stay move, in ascending order, into the
+ * evicted slots < keep: K and V rows, mass, born (may be NULL) and, if slab is given (with idx_dev), the kept
+ * key channels.  Pools with at most `keep` valid slots are left as they are; the caller takes kv_len[b] =
+ * min(kv_len[b], keep) from there.  Every pool of a sequence keeps its own slots.  With kv_len = keep + 1
+ * this is the eviction of a decode step: one slot a pool. */
+int ig_pool_evict(ig_ctx *ctx, const ig_desc *desc, int32_t keep, const int32_t *kv_len, float *mass,
+                  int32_t *born, const int32_t *protect_from, const int32_t *idx_dev, void *slab, void *Kpool,
+                  void *Vpool, void *stream);
 
 /* ---- measurement --------------------------------------------------------------------------- */
 

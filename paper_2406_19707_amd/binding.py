@@ -18,7 +18,7 @@ __all__ = [
     "IG_OK", "IG_EINVAL", "IG_ESHAPE", "IG_EDTYPE", "IG_ECAPACITY", "IG_EHIP", "IG_ENOCONV",
     "IG_ENOMEM", "IG_F32", "IG_F16", "IG_MEM_DEVICE", "IG_MEM_HOST_PINNED", "IG_POLICY_COUNTER", "IG_POLICY_FIFO", "IG_POLICY_LRU", "IG_K_PROJECT",
     "IG_K_FINALIZE", "IG_K_SCAN", "IG_K_SELECT", "IG_K_GATHER", "IG_K_ATTENTION", "IG_K_BUILD",
-    "IG_K_COPY", "IG_K_READ", "IG_K_LAYER", "IgDesc", "IgLayerIO", "IgBufferSet", "IgError", "Context", "lib", "lib_path", "ig_skew_offline",
+    "IG_K_COPY", "IG_K_READ", "IG_K_LAYER", "IG_K_CACHE", "IG_K_EVICT", "IgDesc", "IgLayerIO", "IgBufferSet", "IgError", "Context", "lib", "lib_path", "ig_skew_offline",
     "ig_partial_index", "ig_apply_skew", "ig_rope_rows", "ig_speculate_host", "ig_wq_bytes", "ig_slab_bytes", "EXPORTS",
 ]
 
@@ -27,7 +27,7 @@ IG_F32, IG_F16 = 0, 1
 IG_MEM_DEVICE, IG_MEM_HOST_PINNED = 0, 1
 IG_POLICY_COUNTER, IG_POLICY_FIFO, IG_POLICY_LRU = 0, 1, 2
 (IG_K_PROJECT, IG_K_FINALIZE, IG_K_SCAN, IG_K_SELECT, IG_K_GATHER, IG_K_ATTENTION, IG_K_BUILD,
- IG_K_COPY, IG_K_READ, IG_K_LAYER) = range(10)
+ IG_K_COPY, IG_K_READ, IG_K_LAYER, IG_K_CACHE, IG_K_EVICT) = range(12)
 
 # every symbol include/infinigen.h declares
 EXPORTS = [
@@ -39,6 +39,7 @@ EXPORTS = [
     "ig_speculate", "ig_project", "ig_scan_select", "ig_project_indexed", "ig_speculate_indexed",
     "ig_speculate_host", "ig_speculate_equalized", "ig_equalize_heads", "ig_gather_kv", "ig_sparse_attention", "ig_sparse_attention_static",
     "ig_sparse_attention_indexed", "ig_gather_attention", "ig_layer_step", "ig_decode_step_overlapped", "ig_set_wait_limit", "ig_profile_begin", "ig_profile_end", "ig_profile_read",
+    "ig_cache_attention", "ig_tree_attention", "ig_reserve_cache", "ig_append_rows", "ig_pool_evict",
     "ig_copy_bytes", "ig_read_bytes",
 ]
 
@@ -136,6 +137,11 @@ def lib():
             "ig_gather_attention": (ctypes.c_int, [_vp, _dp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
             "ig_decode_step_overlapped": (ctypes.c_int, [_vp, _dp, ctypes.c_int, _vp, _vp, _vp, _vp, _vp, ctypes.c_int,
                                                          ctypes.c_int, _vp, _i32, _vp, _vp]),
+            "ig_cache_attention": (ctypes.c_int, [_vp, _dp, _i32, _i32] + [_vp] * 8),
+            "ig_tree_attention": (ctypes.c_int, [_vp, _dp, _i32, _i32] + [_vp] * 10),
+            "ig_reserve_cache": (ctypes.c_int, [_vp, _dp, _i32, _i32]),
+            "ig_append_rows": (ctypes.c_int, [_vp, _dp, _i32] + [_vp] * 13),
+            "ig_pool_evict": (ctypes.c_int, [_vp, _dp, _i32] + [_vp] * 9),
             "ig_set_wait_limit": (ctypes.c_int, [_vp, ctypes.c_int64]),
             "ig_profile_begin": (ctypes.c_int, [_vp]),
             "ig_profile_end": (ctypes.c_int, [_vp]),
@@ -463,6 +469,27 @@ class Context:
         self._ck(_entries.ig_decode_step_overlapped(self._address, desc, len(layers), ctypes.addressof(layers), wq,
                                                     bias, A_p, pos, pool_space, len(sets), ctypes.addressof(sets),
                                                     sel_stride, _stream(main_stream), _stream(side_stream)))
+
+    def ig_cache_attention(self, desc, group, n_q, q, q_len, Kpool, Vpool, kv_len, mass, out, stream=None):
+        self._ck(_entries.ig_cache_attention(self._address, desc, group, n_q, q, q_len, Kpool, Vpool, kv_len, mass,
+                                             out, _stream(stream)))
+
+    def ig_tree_attention(self, desc, group, n_tree, q, k_tree, v_tree, visible, tree_len, Kpool, Vpool, kv_len, out,
+                          stream=None):
+        self._ck(_entries.ig_tree_attention(self._address, desc, group, n_tree, q, k_tree, v_tree, visible, tree_len,
+                                            Kpool, Vpool, kv_len, out, _stream(stream)))
+
+    def ig_reserve_cache(self, desc, group, n_q):
+        self._ck(lib().ig_reserve_cache(self._h, ctypes.byref(desc), group, n_q))
+
+    def ig_append_rows(self, desc, n_rows, k_rows, v_rows, path, n_append, kv_len, pos, idx_dev, slab, Kpool, Vpool,
+                       mass=None, born=None, stream=None):
+        self._ck(_entries.ig_append_rows(self._address, desc, n_rows, k_rows, v_rows, path, n_append, kv_len, pos,
+                                         idx_dev, slab, Kpool, Vpool, mass, born, _stream(stream)))
+
+    def ig_pool_evict(self, desc, keep, kv_len, mass, born, protect_from, idx_dev, slab, Kpool, Vpool, stream=None):
+        self._ck(_entries.ig_pool_evict(self._address, desc, keep, kv_len, mass, born, protect_from, idx_dev, slab,
+                                        Kpool, Vpool, _stream(stream)))
 
     def ig_set_wait_limit(self, ticks: int):
         self._ck(lib().ig_set_wait_limit(self._h, int(ticks)))

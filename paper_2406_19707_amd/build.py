@@ -13,7 +13,8 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libinfinigen_hip.so")
 CALL = os.path.join(HERE, "_ig_call" + sysconfig.get_config_var("EXT_SUFFIX"))    # for this Python alone
-SOURCES = ["ig_api.hip", "k_scan.hip", "k_project.hip", "k_kv.hip", "k_layer.hip", "k_equalize.hip", "k_index.hip", "k_skew.hip", "ig_host.cpp"]
+SOURCES = ["ig_api.hip", "k_scan.hip", "k_project.hip", "k_kv.hip", "k_layer.hip", "k_equalize.hip", "k_index.hip", "k_skew.hip", "k_cache.hip", "k_evict.hip",
+           "ig_host.cpp"]
 HIPCC = "/opt/rocm/bin/hipcc"
 # packed-fp32 instruction selection is switched off for every device compile
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -1,0 +1,109 @@
+// What the kernels over a whole key / value pool share: their arguments, and small device functions.
+#pragma once
+#include <math.h>
+
+#include "ig_internal.h"
+
+struct StreamArgs {
+  const void *q, *K, *V, *k_tree, *v_tree;
+  void *out;
+  const uint64_t *visible;            // [B][n_q]
+  const int32_t *q_len, *kv_len;      // [B], or NULL: n_q, N
+  int n_q, R, Hq, N, N_cap;           // R = n_q * group query rows share a pool
+  int nrb, slices, total, per_xcd;    // row blocks and slices of a pool, workgroups in all and of one XCD
+  FastDiv by_pair, by_slices, by_H, by_group;
+  int flip;                           // 1: the scale is negative and q is taken with its sign changed; 2: it is zero, and q is taken as zero
+  float c;                            // |scale| / ln 2
+  float2 *stats;                      // [B*H][R] maximum and 1 / sum of finished rows, or NULL
+  float2 *part_ml;                    // [B*H][slices][R]
+  float *part;                        // [B*H][slices][R][d]
+  float *logits;                      // [B*H][R][logits_ld]
+  long logits_ld;
+};
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+
+// Workgroups go to the eight XCDs in turn; this gives every XCD one contiguous run of the work, so that what
+// shares keys and values shares an L2.
+__device__ __forceinline__ int xcd_order(int id, int per_xcd) { return (id & 7) * per_xcd + (id >> 3); }
+
+// a sequence's length from the caller's array, never outside [0, most]
+__device__ __forceinline__ int length_of(const int32_t *len, int b, int all, int most) {
+  return len ? min(max(len[b], 0), min(all, most)) : all;
+}
+__device__ __forceinline__ unsigned long long low_bits(int n) { return n >= 64 ? ~0ull : (1ull << n) - 1; }
+
+__device__ __forceinline__ int wave_min_int(int v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_max_int(int v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+
+// 2^x to the last bit but one; denormal results are zero (a weight of 2^-126 of the largest)
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <typename T> __device__ __forceinline__ uint4 flip_sign(uint4 v, int flip) {
+  const unsigned bits = flip == 1 ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u, keep = flip == 2 ? 0u : ~0u;
+  return make_uint4((v.x ^ bits) & keep, (v.y ^ bits) & keep, (v.z ^ bits) & keep, (v.w ^ bits) & keep);
+}
+
+// 16 bytes of 16 rows of A and 16 columns of B: s += A B over the channels they hold
+template <typename T> __device__ __forceinline__ floatx4 dot_step(uint4 a, uint4 b, floatx4 s) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), s, 0, 0, 0);
+  } else {
+    const floatx4 x = __builtin_bit_cast(floatx4, a), y = __builtin_bit_cast(floatx4, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], s, 0, 0, 0);
+    return s;
+  }
+}
+
+// W consecutive words, in loads of up to 16 bytes (the address is aligned to them)
+template <int W> __device__ __forceinline__ void load_words(const void *from, unsigned (&to)[W]) {
+  if constexpr (W == 1) {
+    to[0] = *static_cast<const unsigned *>(from);
+  } else if constexpr (W == 2) {
+    const uint2 x = *static_cast<const uint2 *>(from);
+    to[0] = x.x, to[1] = x.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i) {
+      const uint4 x = static_cast<const uint4 *>(from)[i];
+      to[4 * i] = x.x, to[4 * i + 1] = x.y, to[4 * i + 2] = x.z, to[4 * i + 3] = x.w;
+    }
+  }
+}
+template <int W, typename T, int N> __device__ __forceinline__ void store_words(void *to, const T (&from)[N]) {
+  static_assert(W * 4 == N * sizeof(T), "whole words");
+  if constexpr (W == 1) {
+    struct one { unsigned v; };
+    *static_cast<unsigned *>(to) = __builtin_bit_cast(unsigned, half2v{(half_t)from[0], (half_t)from[1]});
+  } else {
+    typedef T vecT __attribute__((ext_vector_type(W == 2 ? 8 / sizeof(T) : 16 / sizeof(T))));
+    constexpr int PER = sizeof(vecT) / sizeof(T);
+#pragma unroll
+    for (int i = 0; i < N / PER; ++i) {
+      vecT x;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) x[e] = from[i * PER + e];
+      static_cast<vecT *>(to)[i] = x;
+    }
+  }
+}
+
+// channel j of eight rows that a lane holds as pairs of channels
+template <int W> __device__ __forceinline__ half8 column_of(const unsigned (&v)[8][W], int j) {
+  uint4 r;
+  const unsigned pick = j & 1 ? 0x07060302u : 0x05040100u;
+  r.x = __builtin_amdgcn_perm(v[1][j / 2], v[0][j / 2], pick);
+  r.y = __builtin_amdgcn_perm(v[3][j / 2], v[2][j / 2], pick);
+  r.z = __builtin_amdgcn_perm(v[5][j / 2], v[4][j / 2], pick);
+  r.w = __builtin_amdgcn_perm(v[7][j / 2], v[6][j / 2], pick);
+  return __builtin_bit_cast(half8, r);
+}

@@ -251,6 +251,7 @@ int ig_destroy(ig_ctx *ctx) {
   if (ctx->eq_cnt) (void)hipFree(ctx->eq_cnt);
   if (ctx->words) (void)hipFree(ctx->words);
   if (ctx->cnt_copy) (void)hipFree(ctx->cnt_copy);
+  if (ctx->cache_ws) (void)hipFree(ctx->cache_ws);
   if (ctx->attn_part) (void)hipFree(ctx->attn_part);
   if (ctx->attn_cnt) (void)hipFree(ctx->attn_cnt);
   if (ctx->status) (void)hipFree(ctx->status);
@@ -272,7 +273,7 @@ size_t ig_workspace_bytes(const ig_ctx *ctx) {
   if (!ctx) return 0;
   return ctx->part_bytes + ctx->qp_bytes + ctx->scores_bytes + ctx->tmax_bytes + ctx->pcount_bytes +
          ctx->attn_part_bytes + ctx->attn_cnt_bytes + ctx->skew_ws_bytes + ctx->pair_sync_bytes + ctx->seq_sync_bytes +
-         ctx->words_bytes + ctx->cnt_copy_bytes + ctx->eq_cnt_bytes;
+         ctx->words_bytes + ctx->cnt_copy_bytes + ctx->eq_cnt_bytes + ctx->cache_ws_bytes;
 }
 
 int ig_check_status(ig_ctx *ctx) {
@@ -947,6 +948,99 @@ int ig_decode_step_overlapped(ig_ctx *ctx, const ig_desc *d, int n_layers, const
   }
   // the side stream's last work is joined to the main stream by the last wait above
   return IG_OK;
+}
+
+// ---- attention over a whole pool, eviction by its weights, drafted tokens ----
+
+// The descriptor of a call over whole pools: a cache without a token is allowed, group query heads share a pool.
+static int check_cache(ig_ctx *ctx, const ig_desc *d, const char *what, int group, int n_q, bool attends, void *stream) {
+  if (!ctx) return IG_EINVAL;
+  ctx->call_stream = (hipStream_t)stream;
+  if (!d) return ig_fail(ctx, IG_EINVAL, "descriptor is NULL");
+  ig_desc one = *d;
+  if (one.N == 0 && one.N_cap >= 1) one.N = 1;
+  if (int rc = check_desc(ctx, &one)) return rc;
+  if (group < 1 || n_q < 1) return ig_fail(ctx, IG_ESHAPE, "%s: group = %d, %d tokens", what, group, n_q);
+  // (row and workgroup numbers are 32-bit; a pool has at most n_q * group rows and 64 slices of each 16 of them)
+  if ((double)group * n_q * d->H * d->B > 1073741824.0 / 16)
+    return ig_fail(ctx, IG_ESHAPE, "%s: too many query rows", what);
+  if ((double)d->B * d->H * ((double)d->N_cap / 16 + 64) > 1073741824.0)
+    return ig_fail(ctx, IG_ESHAPE, "%s: B * H * N_cap too large", what);
+  if (attends && d->d != 32 && d->d != 64 && d->d != 128 && d->d != 256)
+    return ig_fail(ctx, IG_ESHAPE, "%s: d = %d is not 32, 64, 128 or 256", what, d->d);
+  return IG_OK;
+}
+
+int ig_reserve_cache(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_q) {
+  int rc = check_cache(ctx, d, "ig_reserve_cache", group, n_q, false, nullptr);
+  if (rc) return rc;
+  if ((rc = set_device(ctx))) return rc;
+  // the largest workspace of any call this covers: with weights or a tree, any length and number of tokens up
+  // to these, any number of slots to keep
+  return ig_ensure(ctx, (void **)&ctx->cache_ws, &ctx->cache_ws_bytes, ig_cache_reserve_bytes(d, group, n_q));
+}
+
+static int attend_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, void *stream) {
+  int rc = set_device(ctx);
+  if (rc) return rc;
+  const CachePlan p = ig_cache_plan(d, c);
+  if ((rc = ig_ensure(ctx, (void **)&ctx->cache_ws, &ctx->cache_ws_bytes, p.bytes))) return rc;
+  return ig_launch_cache(ctx, d, c, p, ctx->cache_ws, (hipStream_t)stream);
+}
+
+int ig_cache_attention(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_q, const void *q, const int32_t *q_len,
+                       const void *Kpool, const void *Vpool, const int32_t *kv_len, float *mass, void *out,
+                       void *stream) {
+  int rc = check_cache(ctx, d, "ig_cache_attention", group, n_q, true, stream);
+  if (rc) return rc;
+  if (!q || !Kpool || !Vpool || !out) return ig_fail(ctx, IG_EINVAL, "ig_cache_attention: NULL argument");
+  if ((rc = check_aligned(ctx, "ig_cache_attention", {q, Kpool, Vpool, out}))) return rc;
+  return attend_cache(ctx, d, CacheCall{group, n_q, q, Kpool, Vpool, nullptr, nullptr, nullptr, q_len, kv_len, mass, out}, stream);
+}
+
+int ig_tree_attention(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_tree, const void *q, const void *k_tree,
+                      const void *v_tree, const uint64_t *visible, const int32_t *tree_len, const void *Kpool,
+                      const void *Vpool, const int32_t *kv_len, void *out, void *stream) {
+  int rc = check_cache(ctx, d, "ig_tree_attention", group, n_tree, true, stream);
+  if (rc) return rc;
+  if (n_tree > 64) return ig_fail(ctx, IG_ESHAPE, "ig_tree_attention: %d nodes, at most 64", n_tree);
+  if (!q || !k_tree || !v_tree || !visible || !Kpool || !Vpool || !out)
+    return ig_fail(ctx, IG_EINVAL, "ig_tree_attention: NULL argument");
+  if ((uintptr_t)visible % 8) return ig_fail(ctx, IG_EINVAL, "ig_tree_attention: visible must be 8-byte aligned");
+  if ((rc = check_aligned(ctx, "ig_tree_attention", {q, k_tree, v_tree, Kpool, Vpool, out}))) return rc;
+  return attend_cache(ctx, d, CacheCall{group, n_tree, q, Kpool, Vpool, k_tree, v_tree, visible, tree_len, kv_len, nullptr, out},
+                      stream);
+}
+
+int ig_append_rows(ig_ctx *ctx, const ig_desc *d, int32_t n_rows, const void *k_rows, const void *v_rows,
+                   const int32_t *path, const int32_t *n_append, const int32_t *kv_len, const int32_t *pos,
+                   const int32_t *idx_dev, void *slab, void *Kpool, void *Vpool, float *mass, int32_t *born,
+                   void *stream) {
+  int rc = check_cache(ctx, d, "ig_append_rows", 1, n_rows, false, stream);
+  if (rc) return rc;
+  if (!k_rows || !v_rows || !Kpool || !Vpool) return ig_fail(ctx, IG_EINVAL, "ig_append_rows: NULL argument");
+  if (slab && !idx_dev) return ig_fail(ctx, IG_EINVAL, "ig_append_rows: a slab needs idx_dev");
+  if ((rc = check_aligned(ctx, "ig_append_rows", {k_rows, v_rows, Kpool, Vpool, slab}))) return rc;
+  if ((rc = set_device(ctx))) return rc;
+  return ig_launch_append_rows(ctx, d, n_rows, k_rows, v_rows, path, n_append, kv_len, pos, idx_dev, slab, Kpool, Vpool,
+                               mass, born, (hipStream_t)stream);
+}
+
+int ig_pool_evict(ig_ctx *ctx, const ig_desc *d, int32_t keep, const int32_t *kv_len, float *mass, int32_t *born,
+                  const int32_t *protect_from, const int32_t *idx_dev, void *slab, void *Kpool, void *Vpool,
+                  void *stream) {
+  int rc = check_cache(ctx, d, "ig_pool_evict", 1, 1, false, stream);
+  if (rc) return rc;
+  if (keep < 1) return ig_fail(ctx, IG_ESHAPE, "ig_pool_evict: keep = %d", keep);
+  if (!mass || !Kpool || !Vpool) return ig_fail(ctx, IG_EINVAL, "ig_pool_evict: NULL argument");
+  if (protect_from && !born) return ig_fail(ctx, IG_EINVAL, "ig_pool_evict: protect_from needs born");
+  if (slab && !idx_dev) return ig_fail(ctx, IG_EINVAL, "ig_pool_evict: a slab needs idx_dev");
+  if ((rc = check_aligned(ctx, "ig_pool_evict", {Kpool, Vpool, slab}))) return rc;
+  if (d->N <= keep) return IG_OK;                     // no pool holds more than keep
+  if ((rc = set_device(ctx))) return rc;
+  if ((rc = ig_ensure(ctx, (void **)&ctx->cache_ws, &ctx->cache_ws_bytes, ig_evict_workspace(d, keep)))) return rc;
+  return ig_launch_evict(ctx, d, keep, kv_len, mass, born, protect_from, idx_dev, slab, Kpool, Vpool, ctx->cache_ws,
+                         (hipStream_t)stream);
 }
 
 int ig_set_wait_limit(ig_ctx *ctx, int64_t ticks) {

@@ -67,6 +67,7 @@ template <typename T> Outcome take_const(PyObject *o, const T **out) {
 Outcome take(PyObject *o, const void **out) { return take_const<void>(o, out); }
 Outcome take(PyObject *o, const float **out) { return take_const<float>(o, out); }
 Outcome take(PyObject *o, const int32_t **out) { return take_const<int32_t>(o, out); }
+Outcome take(PyObject *o, const uint64_t **out) { return take_const<uint64_t>(o, out); }
 Outcome take(PyObject *o, const ig_layer_io **out) { return take_const<ig_layer_io>(o, out); }
 Outcome take(PyObject *o, const ig_buffer_set **out) { return take_const<ig_buffer_set>(o, out); }
 Outcome take(PyObject *o, int *out) {
@@ -128,7 +129,7 @@ template <typename... A> PyObject *run(const char *name, int (*f)(A...), PyObjec
   X(ig_project_indexed) X(ig_speculate_indexed) X(ig_speculate_equalized) X(ig_equalize_heads)              \
   X(ig_gather_kv) X(ig_sparse_attention) X(ig_sparse_attention_static) X(ig_sparse_attention_indexed)       \
   X(ig_gather_attention) X(ig_layer_step) X(ig_decode_step_overlapped) X(ig_skew_device)                    \
-  X(ig_partial_index_device)
+  X(ig_partial_index_device) X(ig_cache_attention) X(ig_tree_attention) X(ig_append_rows) X(ig_pool_evict)
 
 #define WRAPPER(NAME) \
   PyObject *call_##NAME(PyObject *, PyObject *const *args, Py_ssize_t n) { return run(#NAME, NAME, args, n); }

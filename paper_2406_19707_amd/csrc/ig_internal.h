@@ -125,6 +125,8 @@ struct ig_ctx {
   size_t eq_cnt_bytes = 0;
   hipStream_t call_stream = nullptr;   // stream of the entry point being served (capture check in ig_ensure)
   long spin_limit;                           // scan: bound of a split's wait for its partners, 100 MHz ticks
+  char *cache_ws = nullptr;            // attention over a whole pool: slice states, row statistics, logits; eviction: moves
+  size_t cache_ws_bytes = 0;
   double *skew_ws;  size_t skew_ws_bytes;   // ig_skew_device: Gram matrices and eigenvectors [2][H][d][d]
   int32_t *status;                        // device status word (sticky flags)
   void *static_scratch;                   // this device's address of the library's static scratch array
@@ -283,6 +285,32 @@ int ig_static_scratch_bind(ig_ctx *ctx);
 int ig_launch_attention_static(ig_ctx *ctx, const ig_desc *d, const void *q, const void *K, const void *V,
                                int32_t sel_stride, const int32_t *sel_cnt, const void *k_new,
                                const void *v_new, void *out, hipStream_t s);
+// attention over a whole pool (k_cache.hip)
+struct CacheCall {
+  int group, n_q;
+  const void *q, *K, *V, *k_tree, *v_tree;      // k_tree: a tree of n_q drafted tokens; NULL: n_q tokens of the cache
+  const uint64_t *visible;
+  const int32_t *q_len, *kv_len;
+  float *mass;                                  // or NULL
+  void *out;
+};
+struct CachePlan {
+  int rb, nrb, slices;
+  long logits_ld;
+  size_t stats_at, part_ml_at, part_at, logits_at, bytes;      // parts of the workspace
+};
+CachePlan ig_cache_plan(const ig_desc *d, const CacheCall &c);
+size_t ig_cache_reserve_bytes(const ig_desc *d, int group, int n_q);
+int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const CachePlan &p, char *ws, hipStream_t s);
+// eviction by weight and the append of rows (k_evict.hip)
+size_t ig_evict_workspace(const ig_desc *d, int keep);
+int ig_launch_evict(ig_ctx *ctx, const ig_desc *d, int keep, const int32_t *kv_len, float *mass, int32_t *born,
+                    const int32_t *protect_from, const int32_t *idx, void *slab, void *Kpool, void *Vpool, char *ws,
+                    hipStream_t s);
+int ig_launch_append_rows(ig_ctx *ctx, const ig_desc *d, int n_rows, const void *k_rows, const void *v_rows,
+                          const int32_t *path, const int32_t *n_append, const int32_t *kv_len, const int32_t *pos,
+                          const int32_t *idx, void *slab, void *Kpool, void *Vpool, float *mass, int32_t *born,
+                          hipStream_t s);
 int ig_launch_copy(ig_ctx *ctx, const void *src, void *dst, size_t bytes, hipStream_t s);
 int ig_launch_read(ig_ctx *ctx, const void *src, size_t bytes, hipStream_t s);
 
