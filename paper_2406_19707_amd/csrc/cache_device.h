@@ -14,13 +14,18 @@ struct StreamArgs {
   FastDiv by_pair, by_slices, by_H, by_group;
   int flip;                           // 1: the scale is negative and q is taken with its sign changed; 2: it is zero, and q is taken as zero
   float c;                            // |scale| / ln 2
-  float2 *stats;                      // [B*H][R] maximum and 1 / sum of finished rows, or NULL
-  float2 *part_ml;                    // [B*H][slices][R]
+  float2 *stats;                      // [B*H][R] reference and 1 / sum of finished rows, or NULL
+  float2 *part_ml;                    // [B*H][slices][R] reference and sum of a slice
   float *part;                        // [B*H][slices][R][d]
   float *logits;                      // [B*H][R][logits_ld]
   long logits_ld;
 };
 
+// A row's weights are exp2(c s - ref) / sum.  The reference is its largest c s so far, or somewhat less; a row
+// that has seen nothing has NOTHING_SEEN, against which every weight is zero, and a sum of zero.
+constexpr float NOTHING_SEEN = -1e30f;
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 
 // Workgroups go to the eight XCDs in turn; this gives every XCD one contiguous run of the work, so that what
@@ -46,6 +51,9 @@ __device__ __forceinline__ int wave_max_int(int v) {
 
 // 2^x to the last bit but one; denormal results are zero (a weight of 2^-126 of the largest)
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// 1 / sum, zero for a row without weights
+__device__ __forceinline__ float inverse_of(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 
 template <typename T> __device__ __forceinline__ uint4 flip_sign(uint4 v, int flip) {
   const unsigned bits = flip == 1 ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u, keep = flip == 2 ? 0u : ~0u;
@@ -106,4 +114,41 @@ template <int W> __device__ __forceinline__ half8 column_of(const unsigned (&v)[
   r.z = __builtin_amdgcn_perm(v[5][j / 2], v[4][j / 2], pick);
   r.w = __builtin_amdgcn_perm(v[7][j / 2], v[6][j / 2], pick);
   return __builtin_bit_cast(half8, r);
+}
+
+// ---- tiles in LDS -----------------------------------------------------------------------------------------
+// A tile is rows of D halves with the 16-byte pieces of a row in another order: piece c of row r lies where piece
+// c ^ piece_swap(r) would.  16 rows' pieces of one column (what a wave reads of K or Q) and 64 bytes of four
+// consecutive rows (of V) then fall on different banks.
+template <int D> __device__ __forceinline__ int piece_swap(int row) {
+  if constexpr (D == 32) return (row >> 2) & 3;
+  else if constexpr (D == 64) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
+  else return (row & 3) << 2 | ((row >> 2) & 3);
+}
+template <int D> __device__ __forceinline__ half8 tile_row_piece(const half_t *tile, int row, int c) {
+  return *reinterpret_cast<const half8 *>(tile + row * D + ((c ^ piece_swap<D>(row)) * 8));
+}
+// Four rows' values of one column a lane: lane i of 16 gets column c0 + i of rows row .. row + 3 (c0 a multiple
+// of 16).  The hardware's transposing read takes 8 bytes of a row from each of the 16 lanes: lane i supplies row
+// i / 4, columns 4 (i % 4) onwards.
+template <int D> __device__ __forceinline__ uint2 tile_columns(const half_t *tile, int row, int c0, int i) {
+  typedef __fp16 fp4 __attribute__((__vector_size__(8)));
+  const int r = row + (i >> 2), c = (c0 >> 3) + ((i >> 1) & 1);
+  const half_t *at = tile + r * D + ((c ^ piece_swap<D>(r)) * 8) + (i & 1) * 4;
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4f16((fp4 __attribute__((address_space(3))) *)at));
+}
+// 64 pieces from memory to LDS, `to` onwards (the same in all lanes), without passing through registers
+__device__ __forceinline__ void load_to_lds(const void *from, half_t *to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                   (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
+// the other half wave's value and this one's: both in both
+__device__ __forceinline__ float both_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float both_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }

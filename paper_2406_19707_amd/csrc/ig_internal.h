@@ -295,6 +295,7 @@ struct CacheCall {
   void *out;
 };
 struct CachePlan {
+  bool prompt;
   int rb, nrb, slices;
   long logits_ld;
   size_t stats_at, part_ml_at, part_at, logits_at, bytes;      // parts of the workspace

@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   float m_run[NT], l_run[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    m_run[n] = -INFINITY;
+    m_run[n] = NOTHING_SEEN;
     l_run[n] = 0.f;
 #pragma unroll
     for (int j = 0; j < CJ; ++j) acc[n][j] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -162,14 +162,13 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
         for (int r = 0; r < 4; ++r) top = fmaxf(top, s[n][m][r]);
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float m_new = fmaxf(m_run[n], top);
-      const float ref = m_new == -INFINITY ? 0.f : m_new * a.c;      // (nothing seen yet: every weight is exp2(-inf))
-      if (__any(m_new > m_run[n])) {
-        const float shrink = exp2_fast(m_run[n] * a.c - ref);
+      const float ref = fmaxf(m_run[n], top * a.c);
+      if (__any(ref > m_run[n])) {
+        const float shrink = exp2_fast(m_run[n] - ref);
         l_run[n] *= shrink;
 #pragma unroll
         for (int j = 0; j < CJ; ++j) acc[n][j] *= shrink;
-        m_run[n] = m_new;
+        m_run[n] = ref;
       }
       float sum = 0.f;
 #pragma unroll
@@ -221,12 +220,11 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   for (int n = 0; n < NT; ++n) {
     const int at = n * 16 + i;
     const float m = fmaxf(fmaxf(box_m[0][at], box_m[1][at]), fmaxf(box_m[2][at], box_m[3][at]));
-    const float ref = m == -INFINITY ? 0.f : m * a.c;
     m_all[n] = m;
     l_all[n] = 0.f;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) l_all[n] += box_l[x][at] * exp2_fast(box_m[x][at] * a.c - ref);
-    const float shrink = exp2_fast(m_run[n] * a.c - ref);
+    for (int x = 0; x < 4; ++x) l_all[n] += box_l[x][at] * exp2_fast(box_m[x][at] - m);
+    const float shrink = exp2_fast(m_run[n] - m);
 #pragma unroll
     for (int j = 0; j < CJ; ++j) acc[n][j] *= shrink;
   }
@@ -253,7 +251,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   for (int n = 0; n < NT; ++n) {
     const int row = rb * RB + n * 16 + i;
     if (!live[n]) continue;
-    const float inv = l_all[n] > 0.f || l_all[n] != l_all[n] ? 1.f / l_all[n] : 0.f;
+    const float inv = inverse_of(l_all[n]);
     if (a.slices == 1) {
       const int iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
       T *to = static_cast<T *>(a.out) + (((long)b * a.n_q + iq) * a.Hq + h * (int)a.by_group.d + gq) * D;
@@ -276,6 +274,164 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   }
 }
 
+// ---- many query rows, half precision -------------------------------------------------------------------
+// The same products on 32x32 matrix instructions: a wave takes 32 query rows, a workgroup 128 that share the
+// cached rows' tiles of 64, which come to LDS asynchronously, one ahead.  As above S^T = K Q^T and O^T = V^T P^T,
+// so that a query row is one lane of each half wave.  The accumulator of a 32-token block holds, in half h, the
+// tokens 8 x + 4 h + 0 .. 3; P^T takes them in that order, and V^T is read through LDS's transposing loads in the
+// same one, so the weights never leave their lane.
+// The reference of a row's weights only moves when its largest logit passes it by RISE (weights up to 2^RISE, far
+// inside half precision): the row's output, 16 registers for every 32 channels, is then scaled only now and then.
+constexpr float RISE = 6.f;
+constexpr int PROMPT_ROWS = 128, PROMPT_KEYS = 64;
+
+template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_prompt(StreamArgs a) {
+  constexpr int KS = D / 16, OB = D / 32, PC = D / 8, TK = PROMPT_KEYS;
+  __shared__ __attribute__((aligned(16))) half_t tiles[2][2][TK * D];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = lane & 31, hb = lane >> 5;
+  int work = xcd_order(blockIdx.x, a.per_xcd);
+  if (work >= a.total) return;
+  const int bh = a.by_pair.div(work);
+  work -= bh * (int)a.by_pair.d;
+  const int rb = a.nrb - 1 - a.by_slices.div(work);       // (a prompt's last rows see most: first)
+  const int slice = a.by_slices.mod(work);
+  const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, G = (int)a.by_group.d;
+  const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
+
+  const int row = rb * PROMPT_ROWS + w * 32 + i, iq = a.by_group.div(row), gq = row - iq * G;
+  const bool live = row < a.R && iq < nq;
+  const int lim = live ? (TREE ? kv : max(0, kv - nq + iq + 1)) : 0x7fffffff;
+  const unsigned long long sees = TREE && live ? a.visible[(long)b * a.n_q + iq] & low_bits(nq) : 0;
+  const long row_at = (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * G + gq) * D;
+  const int lim_min = wave_min_int(lim), lim_max = wave_max_int(live ? lim : 0);
+  // (what the workgroup's last live row sees)
+  const int last_row = min(min(a.R, nq * G), (rb + 1) * PROMPT_ROWS) - 1;
+  const int most = last_row < rb * PROMPT_ROWS ? 0 : (TREE ? kv : max(0, kv - nq + a.by_group.div(last_row) + 1));
+  const int cache_tiles = (most + TK - 1) / TK;
+  const int tiles_all = cache_tiles + (TREE && last_row >= rb * PROMPT_ROWS ? (nq + TK - 1) / TK : 0);
+  const int per = (tiles_all + a.slices - 1) / a.slices;
+  const int t_begin = min(tiles_all, slice * per), t_end = min(tiles_all, t_begin + per);
+
+  half8 qf[KS];
+  {
+    const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const half_t *>(a.q) + row_at);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(half8, flip_sign<half_t>(src[2 * s + hb], a.flip));
+  }
+  auto fetch = [&](int tile, int slot) {
+    const bool drafted = TREE && tile >= cache_tiles;
+    const long pool_at = drafted ? ((long)b * a.n_q * a.by_H.d + h) * D : (long)bh * a.N_cap * D;
+    const half_t *K = static_cast<const half_t *>(drafted ? a.k_tree : a.K) + pool_at;
+    const half_t *V = static_cast<const half_t *>(drafted ? a.v_tree : a.V) + pool_at;
+    const long stride = drafted ? (long)a.by_H.d * D : D;
+    const int t0 = (drafted ? tile - cache_tiles : tile) * TK, last = (drafted ? nq : kv) - 1;
+#pragma unroll
+    for (int x = 0; x < PC / 4; ++x) {
+      const int at = (w * (PC / 4) + x) * 64, r = (at + lane) / PC, c = ((at + lane) % PC) ^ piece_swap<D>(r);
+      const long from = min(t0 + r, last) * stride + c * 8;
+      load_to_lds(K + from, tiles[slot][0] + at * 8);
+      load_to_lds(V + from, tiles[slot][1] + at * 8);
+    }
+  };
+
+  floatx16 acc[OB];
+#pragma unroll
+  for (int o = 0; o < OB; ++o)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[o][e] = 0.f;
+  float ref = NOTHING_SEEN, sum = 0.f;
+
+  if (t_begin < t_end) fetch(t_begin, 0);
+  for (int tile = t_begin; tile < t_end; ++tile) {
+    const int slot = (tile - t_begin) & 1;
+    __builtin_amdgcn_s_waitcnt(0x0f70);                   // vmcnt(0): this tile is there ...
+    __syncthreads();                                      // ... in every wave's part, and the other slot is free
+    if (tile + 1 < t_end) fetch(tile + 1, slot ^ 1);
+    const bool drafted = TREE && tile >= cache_tiles;
+    const int t0 = (drafted ? tile - cache_tiles : tile) * TK;
+    if (!drafted && t0 >= lim_max) continue;              // (no row of this wave sees any of it)
+    const half_t *K = tiles[slot][0], *V = tiles[slot][1];
+    floatx16 s[2];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[m][e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        s[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(tile_row_piece<D>(K, m * 32 + i, 2 * k + hb), qf[k], s[m], 0, 0, 0);
+    }
+    if (drafted) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!(sees >> (m * 32 + (e / 4) * 8 + hb * 4 + e % 4) & 1)) s[m][e] = -INFINITY;
+    } else if (t0 + TK > lim_min) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (t0 + m * 32 + (e / 4) * 8 + hb * 4 + e % 4 >= lim) s[m][e] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[m][e]);
+    if (__any(top * a.c > ref + RISE)) {
+      const float to = fmaxf(ref, both_max(top) * a.c), shrink = exp2_fast(ref - to);
+      ref = to;
+      sum *= shrink;
+#pragma unroll
+      for (int o = 0; o < OB; ++o) acc[o] *= shrink;
+    }
+    half8 p[4];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = exp2_fast(fmaf(s[m][e], a.c, -ref));
+        sum += x;
+        p[m * 2 + e / 8][e % 8] = (half_t)x;
+      }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int o = 0; o < OB; ++o) {
+        const uint2 lo = tile_columns<D>(V, k * 16 + 4 * hb, o * 32 + (lane & 16), lane & 15);
+        const uint2 hi = tile_columns<D>(V, k * 16 + 8 + 4 * hb, o * 32 + (lane & 16), lane & 15);
+        acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, make_uint4(lo.x, lo.y, hi.x, hi.y)), p[k], acc[o], 0, 0, 0);
+      }
+  }
+
+  if (!live) return;
+  sum = both_sum(sum);
+  const float inv = inverse_of(sum);
+  if (a.slices == 1) {
+    half_t *to = static_cast<half_t *>(a.out) + row_at;
+#pragma unroll
+    for (int o = 0; o < OB; ++o)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        half_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = (half_t)(acc[o][x * 4 + e] * inv);
+        store_words<2>(to + o * 32 + x * 8 + hb * 4, v);
+      }
+    if (hb == 0 && a.stats) a.stats[(long)bh * a.R + row] = make_float2(ref, inv);
+  } else {
+    const long at = ((long)bh * a.slices + slice) * a.R + row;
+#pragma unroll
+    for (int o = 0; o < OB; ++o)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<floatx4 *>(a.part + at * D + o * 32 + x * 8 + hb * 4) =
+            floatx4{acc[o][x * 4], acc[o][x * 4 + 1], acc[o][x * 4 + 2], acc[o][x * 4 + 3]};
+    if (hb == 0) a.part_ml[at] = make_float2(ref, sum);
+  }
+}
+
 // ---- joining the slices, and the weights of single-token calls ------------------------------------------
 // A workgroup takes rows x, x + chunks, .. of a pool's R and, where logits were kept, the slots
 // 1024 x .. of that pool: mass[t] += sum over the rows of exp2(c s - c m) / l.
@@ -285,27 +441,24 @@ __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, in
   const int bh = by_chunks.div(blockIdx.x), x = by_chunks.mod(blockIdx.x), b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, tid = threadIdx.x;
   const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
   const int G = (int)a.by_group.d;
-  auto joined = [&](int row, float *shrink_of) {           // the row's maximum and sum over all slices
-    float m = -INFINITY, l = 0.f;
+  auto joined = [&](int row) {                             // the row's reference and 1 / sum over all slices
+    float m = NOTHING_SEEN, l = 0.f;
     for (int s = 0; s < a.slices; ++s) m = fmaxf(m, a.part_ml[((long)bh * a.slices + s) * a.R + row].x);
-    const float ref = m == -INFINITY ? 0.f : m * a.c;
     for (int s = 0; s < a.slices; ++s) {
       const float2 ml = a.part_ml[((long)bh * a.slices + s) * a.R + row];
-      l += ml.y * exp2_fast(ml.x * a.c - ref);
+      l += ml.y * exp2_fast(ml.x - m);
     }
-    *shrink_of = ref;
-    return make_float2(m, l > 0.f || l != l ? 1.f / l : 0.f);
+    return make_float2(m, inverse_of(l));
   };
   if (a.slices > 1) {
     const int per = 256 / D < 1 ? 1 : 256 / D;             // rows a workgroup takes at a time
     for (int row = x * per + tid / D; row < nq * G && tid < per * D; row += (int)by_chunks.d * per) {
-      float ref;
-      const float2 st = joined(row, &ref);
+      const float2 st = joined(row);
       const int e = tid % D;
       float o = 0.f;
       for (int s = 0; s < a.slices; ++s) {
         const long at = ((long)bh * a.slices + s) * a.R + row;
-        o += a.part[at * D + e] * exp2_fast(a.part_ml[at].x * a.c - ref);
+        o += a.part[at * D + e] * exp2_fast(a.part_ml[at].x - st.x);
       }
       const int iq = a.by_group.div(row), gq = row - iq * G;
       static_cast<T *>(a.out)[(((long)b * a.n_q + iq) * a.Hq + h * G + gq) * D + e] = (T)(o * st.y);
@@ -313,18 +466,13 @@ __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, in
     }
   }
   if (LOGITS) {
-    if (tid < a.R) {
-      float ref;
-      stat[tid] = a.slices > 1 ? joined(tid, &ref) : a.stats[(long)bh * a.R + tid];
-    }
+    if (tid < a.R) stat[tid] = a.slices > 1 ? joined(tid) : a.stats[(long)bh * a.R + tid];
     __syncthreads();
     if (nq < 1) return;
     for (int t = x * 1024 + tid; t < min(kv, x * 1024 + 1024); t += 256) {
       float sum = 0.f;
-      for (int row = 0; row < a.R; ++row) {
-        const float ref = stat[row].x == -INFINITY ? 0.f : stat[row].x * a.c;
-        sum = fmaf(exp2_fast(fmaf(a.logits[((long)bh * a.R + row) * a.logits_ld + t], a.c, -ref)), stat[row].y, sum);
-      }
+      for (int row = 0; row < a.R; ++row)
+        sum = fmaf(exp2_fast(fmaf(a.logits[((long)bh * a.R + row) * a.logits_ld + t], a.c, -stat[row].x)), stat[row].y, sum);
       mass[(long)bh * a.N_cap + t] += sum;
     }
   }
@@ -360,7 +508,7 @@ __global__ __launch_bounds__(256) void attend_mass(StreamArgs a, float *mass, Fa
     const bool live = r0 + i < rows;
     const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + (((long)b * a.n_q + iq) * a.Hq + h * G + gq) * D);
     const float2 st = a.stats[(long)bh * a.R + row];
-    const float ref = st.x == -INFINITY ? 0.f : st.x * a.c, inv = live ? st.y : 0.f;
+    const float ref = st.x, inv = live ? st.y : 0.f;
     const int lim = kv - nq + iq + 1;
     floatx4 s[MT];
 #pragma unroll
@@ -389,6 +537,97 @@ __global__ __launch_bounds__(256) void attend_mass(StreamArgs a, float *mass, Fa
     }
 }
 
+// The same in half precision for calls of many rows: a wave keeps 64 keys, a workgroup 256, and the query rows
+// come through LDS 64 at a time, one tile ahead.  What is left is the exponential and two fused multiply-adds a
+// pair beside the products.
+constexpr int MASS_KEYS = 256, MASS_ROWS = 64;
+template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_mass(StreamArgs a, float *mass, FastDiv by_chunks) {
+  constexpr int KS = D / 16, PC = D / 8;
+  __shared__ __attribute__((aligned(16))) half_t tiles[2][MASS_ROWS * D];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = lane & 31, hb = lane >> 5;
+  const int work = xcd_order(blockIdx.x, a.per_xcd);
+  if (work >= a.total) return;
+  const int bh = by_chunks.div(work), x0 = by_chunks.mod(work);
+  const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, G = (int)a.by_group.d;
+  const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
+  const int t0 = x0 * MASS_KEYS + w * 64;
+  if (x0 * MASS_KEYS >= kv) return;
+  // the first query that sees slot t is number t - (kv - nq)
+  const int rows = nq * G, first = max(0, x0 * MASS_KEYS - (kv - nq)) * G, tiles_n = (max(0, rows - first) + MASS_ROWS - 1) / MASS_ROWS;
+
+  half8 kf[2][KS];
+#pragma unroll
+  for (int m = 0; m < 2; ++m) {
+    const half_t *src = static_cast<const half_t *>(a.K) + ((long)bh * a.N_cap + min(t0 + m * 32 + i, kv - 1)) * D;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) kf[m][k] = __builtin_bit_cast(half8, flip_sign<half_t>(reinterpret_cast<const uint4 *>(src)[2 * k + hb], a.flip));
+  }
+  auto fetch = [&](int tile, int slot) {
+#pragma unroll
+    for (int x = 0; x < PC / 4; ++x) {
+      const int at = (w * (PC / 4) + x) * 64, r = (at + lane) / PC, c = ((at + lane) % PC) ^ piece_swap<D>(r);
+      const int row = min(first + tile * MASS_ROWS + r, rows - 1), iq = a.by_group.div(row);
+      load_to_lds(static_cast<const half_t *>(a.q) + (((long)b * a.n_q + iq) * a.Hq + h * G + row - iq * G) * D + c * 8,
+                  tiles[slot] + at * 8);
+    }
+  };
+  float sums[2][16] = {};
+  if (tiles_n > 0) fetch(0, 0);
+  for (int tile = 0; tile < tiles_n; ++tile) {
+    const int slot = tile & 1, r0 = first + tile * MASS_ROWS;
+    float2 st[2];
+    int seen[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const int row = min(r0 + n * 32 + i, rows - 1);
+      st[n] = a.stats[(long)bh * a.R + row];
+      seen[n] = kv - nq + a.by_group.div(row) + 1;
+      if (r0 + n * 32 + i >= rows) st[n] = make_float2(INFINITY, 0.f);      // (no such row: weights of zero)
+    }
+    const int seen_first = kv - nq + a.by_group.div(r0) + 1, seen_last = kv - nq + a.by_group.div(min(r0 + MASS_ROWS, rows) - 1) + 1;
+    __builtin_amdgcn_s_waitcnt(0x0f70);                   // vmcnt(0)
+    __syncthreads();
+    if (tile + 1 < tiles_n) fetch(tile + 1, slot ^ 1);
+    if (seen_last <= t0) continue;                        // (before the first query that sees this wave's keys)
+    const bool masked = seen_first < t0 + 64;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      floatx16 s[2];
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[m][e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const half8 q = tile_row_piece<D>(tiles[slot], n * 32 + i, 2 * k + hb);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) s[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[m][k], q, s[m], 0, 0, 0);
+      }
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float p = exp2_fast(fmaf(s[m][e], a.c, -st[n].x));
+          const float more = fmaf(p, st[n].y, sums[m][e]);
+          if (!masked || t0 + m * 32 + (e / 4) * 8 + hb * 4 + e % 4 < seen[n]) sums[m][e] = more;
+        }
+    }
+  }
+  // the 32 lanes of a half wave added up; lane i then keeps the sum of register i
+  float mine = 0.f;
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float v = row16_sum(sums[m][e]);
+      v += __shfl_xor(v, 16, 64);
+      if (i == m * 16 + e) mine = v;
+    }
+  const int t = t0 + (i / 16) * 32 + ((i % 16) / 4) * 8 + hb * 4 + i % 4;
+  if (t < kv) mass[(long)bh * a.N_cap + t] += mine;
+}
+
 int div_up(long n, long d) { return (int)((n + d - 1) / d); }
 
 // query rows a workgroup takes: 16, 32 or 64, what fits the registers beside the row's output
@@ -397,13 +636,13 @@ int row_block(const ig_desc *d, long R) {
   return R <= 16 ? 16 : (R <= 32 || most == 32 ? 32 : 64);
 }
 
-// Slices the cached rows of a pool are cut into: enough workgroups for about three a compute unit, while a
-// wave of each still has a tile.
-int slices_of(const ig_desc *d, long nrb, int n_keys) {
-  const int tile = d->dtype == IG_F16 ? 32 : 16;
-  const long want = (768 + d->B * (long)d->H * nrb - 1) / (d->B * (long)d->H * nrb);
-  const long most = div_up(n_keys, 4 * tile);
-  return (int)(want < 1 ? 1 : (want < most ? want : most) > 64 ? 64 : (want < most ? want : most));
+// Slices the cached rows of a pool are cut into: enough workgroups for two (prompt) or three a compute unit, while
+// a wave (prompt: a workgroup) of each still has a tile or two.
+int slices_of(const ig_desc *d, bool prompt, long nrb, int n_keys) {
+  const long groups = d->B * (long)d->H * nrb, aim = prompt ? 512 : 768;
+  const long want = (aim + groups - 1) / groups, most = div_up(n_keys, prompt ? 256 : (d->dtype == IG_F16 ? 128 : 64));
+  const long s = want < most ? want : most;
+  return (int)(s < 1 ? 1 : (s > 64 ? 64 : s));
 }
 
 }  // namespace
@@ -415,9 +654,10 @@ static bool keeps_logits(const CacheCall &c) { return c.mass && c.n_q == 1 && c.
 CachePlan ig_cache_plan(const ig_desc *d, const CacheCall &c) {
   CachePlan p;
   const long R = (long)c.n_q * c.group, BH = (long)d->B * d->H;
-  p.rb = row_block(d, R);
+  p.prompt = d->dtype == IG_F16 && R > 64;
+  p.rb = p.prompt ? PROMPT_ROWS : row_block(d, R);
   p.nrb = div_up(R, p.rb);
-  p.slices = slices_of(d, p.nrb, d->N + (c.k_tree ? c.n_q : 0));
+  p.slices = slices_of(d, p.prompt, p.nrb, d->N + (c.k_tree ? c.n_q : 0));
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -477,7 +717,19 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
     case 128: DO(T, 128) break;                                                                      \
     default: DO(T, 256) break;                                                                       \
   }
-  if (d->dtype == IG_F16) {
+#define PROMPT(T, D)                                                                                 \
+  {                                                                                                  \
+    if (tree) {                                                                                      \
+      auto k = attend_prompt<D, true>;                                                               \
+      IG_LAUNCH(ctx, IG_K_CACHE, k, grid, block, stream, a);                                         \
+    } else {                                                                                         \
+      auto k = attend_prompt<D, false>;                                                              \
+      IG_LAUNCH(ctx, IG_K_CACHE, k, grid, block, stream, a);                                         \
+    }                                                                                                \
+  }
+  if (p.prompt) {
+    BY_DIM(half_t, PROMPT)
+  } else if (d->dtype == IG_F16) {
     BY_DIM(half_t, STREAM_ROWS)
   } else {
     BY_DIM(float, STREAM_ROWS)
@@ -499,7 +751,17 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   }
     if (d->dtype == IG_F16) JOIN(half_t) else JOIN(float)
   }
-  if (c.mass && !logits) {
+  if (c.mass && !logits && p.prompt) {
+    const FastDiv by_chunks = ig_fast_div(div_up(d->N, MASS_KEYS));
+    a.total = (int)(by_chunks.d * BH), a.per_xcd = div_up(a.total, 8);
+    const dim3 mgrid(a.per_xcd * 8);
+#define PROMPT_MASS(T, D)                                                                            \
+  {                                                                                                  \
+    auto k = prompt_mass<D>;                                                                         \
+    IG_LAUNCH(ctx, IG_K_CACHE, k, mgrid, block, stream, a, c.mass, by_chunks);                       \
+  }
+    BY_DIM(half_t, PROMPT_MASS)
+  } else if (c.mass && !logits) {
     const int tile = d->dtype == IG_F16 ? 32 : 16;
     const FastDiv by_chunks = ig_fast_div(div_up(d->N, 4 * tile));
     const dim3 mgrid((unsigned)(by_chunks.d * BH));
