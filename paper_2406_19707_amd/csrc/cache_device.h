@@ -11,6 +11,7 @@ struct StreamArgs {
   const int32_t *q_len, *kv_len;      // [B], or NULL: n_q, N
   int n_q, R, Hq, N, N_cap;           // R = n_q * group query rows share a pool
   int nrb, slices, total, per_xcd;    // row blocks and slices of a pool, workgroups in all and of one XCD
+  int paired;                         // attend_prompt: a workgroup takes two row blocks
   FastDiv by_pair, by_slices, by_H, by_group;
   int flip;                           // 1: the scale is negative and q is taken with its sign changed; 2: it is zero, and q is taken as zero
   float c;                            // |scale| / ln 2
@@ -119,29 +120,53 @@ template <int W> __device__ __forceinline__ half8 column_of(const unsigned (&v)[
 // ---- tiles in LDS -----------------------------------------------------------------------------------------
 // A tile is rows of D halves with the 16-byte pieces of a row in another order: piece c of row r lies where piece
 // c ^ piece_swap(r) would.  16 rows' pieces of one column (what a wave reads of K or Q) and 64 bytes of four
-// consecutive rows (of V) then fall on different banks.
-template <int D> __device__ __forceinline__ int piece_swap(int row) {
+// consecutive rows (of V) then fall on different banks.  The swap of a sum of two rows without common bits is the
+// exclusive or of theirs, so a lane's addresses differ by exclusive ors and sums with constants, and one register
+// stands for all of them (`opaque` keeps the compiler from holding each in one of its own).
+template <int D> __host__ __device__ constexpr int piece_swap(int row) {
   if constexpr (D == 32) return (row >> 2) & 3;
   else if constexpr (D == 64) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
   else return (row & 3) << 2 | ((row >> 2) & 3);
 }
-template <int D> __device__ __forceinline__ half8 tile_row_piece(const half_t *tile, int row, int c) {
-  return *reinterpret_cast<const half8 *>(tile + row * D + ((c ^ piece_swap<D>(row)) * 8));
+__device__ __forceinline__ unsigned opaque(unsigned v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
-// Four rows' values of one column a lane: lane i of 16 gets column c0 + i of rows row .. row + 3 (c0 a multiple
-// of 16).  The hardware's transposing read takes 8 bytes of a row from each of the 16 lanes: lane i supplies row
-// i / 4, columns 4 (i % 4) onwards.
-template <int D> __device__ __forceinline__ uint2 tile_columns(const half_t *tile, int row, int c0, int i) {
+// the value is worked out before this point
+__device__ __forceinline__ void keep_here(float &v) { asm volatile("" : "+v"(v)); }
+typedef const char __attribute__((address_space(3))) *lds_bytes;
+__device__ __forceinline__ lds_bytes lds_at(const half_t *tile) {
+  return (lds_bytes)(const __attribute__((address_space(3))) half_t *)tile;
+}
+// Rows of a 32-row block as a product's operand: lane i of either half takes piece 2 k + half of row i.
+template <int D> __device__ __forceinline__ unsigned row_base(int lane) {
+  const int i = lane & 31, hb = lane >> 5;
+  return i * D * 2 + ((hb ^ piece_swap<D>(i)) * 16);
+}
+template <int D> __device__ __forceinline__ half8 row_piece(lds_bytes tile, unsigned base, int k) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) half8 *>(tile + (base ^ (k << 5)));
+}
+// Columns of 16 rows (0 .. 3, 8 .. 11 in the lower half wave, 4 .. 7, 12 .. 15 in the upper) as an operand: lane i
+// of a half takes column 32 o + i, four rows a call (x = 0: the first four).  The hardware's transposing read takes
+// 8 bytes of a row from each of 16 lanes, lane i's from row i / 4, and gives it column i of the four rows.
+template <int D> __device__ __forceinline__ unsigned column_base(int lane) {
+  const int i = lane & 15, hb = lane >> 5, r = 4 * hb + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
+  return r * D * 2 + ((c ^ piece_swap<D>(r)) * 16) + (i & 1) * 8;
+}
+template <int D> __device__ __forceinline__ uint2 column_rows(lds_bytes tile, unsigned base, int o, int x) {
   typedef __fp16 fp4 __attribute__((__vector_size__(8)));
-  const int r = row + (i >> 2), c = (c0 >> 3) + ((i >> 1) & 1);
-  const half_t *at = tile + r * D + ((c ^ piece_swap<D>(r)) * 8) + (i & 1) * 4;
-  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4f16((fp4 __attribute__((address_space(3))) *)at));
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4f16(
+                                       (fp4 __attribute__((address_space(3))) *)(tile + 8 * x * D * 2 + (base ^ (o << 6 | x << 5)))));
 }
-// 64 pieces from memory to LDS, `to` onwards (the same in all lanes), without passing through registers
-__device__ __forceinline__ void load_to_lds(const void *from, half_t *to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
-                                   (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+// 64 pieces from memory to LDS without passing through registers: lane i's, `offset` bytes from `from`, to piece i
+// of `to` (from and to the same in all lanes).  Not the compiler's builtin, because it waits for every such load
+// before any transposing read, also of other LDS; nothing is written but LDS, and who reads it waits
+// (wait_for_lds_loads, then a barrier where other waves loaded part of it).
+__device__ __forceinline__ void load_to_lds(const void *from, unsigned offset, half_t *to) {
+  const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)to;
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(at), "v"(offset), "s"(from) : "memory");
 }
+__device__ __forceinline__ void wait_for_lds_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // the other half wave's value and this one's: both in both
 __device__ __forceinline__ float both_max(float v) {

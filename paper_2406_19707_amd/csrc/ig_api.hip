@@ -964,6 +964,8 @@ static int check_cache(ig_ctx *ctx, const ig_desc *d, const char *what, int grou
   // (row and workgroup numbers are 32-bit; a pool has at most n_q * group rows and 64 slices of each 16 of them)
   if ((double)group * n_q * d->H * d->B > 1073741824.0 / 16)
     return ig_fail(ctx, IG_ESHAPE, "%s: too many query rows", what);
+  // (offsets among 64 tokens' rows are 32-bit)
+  if ((double)group * d->H * d->d > 16777216.0) return ig_fail(ctx, IG_ESHAPE, "%s: a token's heads are too many", what);
   if ((double)d->B * d->H * ((double)d->N_cap / 16 + 64) > 1073741824.0)
     return ig_fail(ctx, IG_ESHAPE, "%s: B * H * N_cap too large", what);
   if (attends && d->d != 32 && d->d != 64 && d->d != 128 && d->d != 256)

@@ -1,6 +1,8 @@
 // Attention over a whole key / value pool: a prompt, a chunk of one or a single token with the accumulated
 // attention weight of every slot, and a tree of drafted tokens over the pool (Section 2.1, softmax(q K^T) V;
 // Section 2.3: the weights of earlier steps are what the eviction-based baselines rank a cache by).
+#include <type_traits>
+
 #include "cache_device.h"
 
 namespace {
@@ -294,141 +296,212 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
   if (work >= a.total) return;
   const int bh = a.by_pair.div(work);
   work -= bh * (int)a.by_pair.d;
-  const int rb = a.nrb - 1 - a.by_slices.div(work);       // (a prompt's last rows see most: first)
-  const int slice = a.by_slices.mod(work);
+  const int unit = a.by_slices.div(work), slice = a.by_slices.mod(work);
   const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, G = (int)a.by_group.d;
   const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
 
-  const int row = rb * PROMPT_ROWS + w * 32 + i, iq = a.by_group.div(row), gq = row - iq * G;
-  const bool live = row < a.R && iq < nq;
-  const int lim = live ? (TREE ? kv : max(0, kv - nq + iq + 1)) : 0x7fffffff;
-  const unsigned long long sees = TREE && live ? a.visible[(long)b * a.n_q + iq] & low_bits(nq) : 0;
-  const long row_at = (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * G + gq) * D;
-  const int lim_min = wave_min_int(lim), lim_max = wave_max_int(live ? lim : 0);
-  // (what the workgroup's last live row sees)
-  const int last_row = min(min(a.R, nq * G), (rb + 1) * PROMPT_ROWS) - 1;
-  const int most = last_row < rb * PROMPT_ROWS ? 0 : (TREE ? kv : max(0, kv - nq + a.by_group.div(last_row) + 1));
-  const int cache_tiles = (most + TK - 1) / TK;
-  const int tiles_all = cache_tiles + (TREE && last_row >= rb * PROMPT_ROWS ? (nq + TK - 1) / TK : 0);
-  const int per = (tiles_all + a.slices - 1) / a.slices;
-  const int t_begin = min(tiles_all, slice * per), t_end = min(tiles_all, t_begin + per);
+  // what this lane fetches of every tile: this piece of this row first, then of 64 / PC rows further on, ..
+  const unsigned from_row = w * 16 + lane / PC, from_piece = (lane % PC) ^ piece_swap<D>(from_row);
+  const unsigned k_base = row_base<D>(lane), v_base = column_base<D>(lane);
 
-  half8 qf[KS];
-  {
-    const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const half_t *>(a.q) + row_at);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(half8, flip_sign<half_t>(src[2 * s + hb], a.flip));
-  }
-  auto fetch = [&](int tile, int slot) {
-    const bool drafted = TREE && tile >= cache_tiles;
-    const long pool_at = drafted ? ((long)b * a.n_q * a.by_H.d + h) * D : (long)bh * a.N_cap * D;
-    const half_t *K = static_cast<const half_t *>(drafted ? a.k_tree : a.K) + pool_at;
-    const half_t *V = static_cast<const half_t *>(drafted ? a.v_tree : a.V) + pool_at;
-    const long stride = drafted ? (long)a.by_H.d * D : D;
-    const int t0 = (drafted ? tile - cache_tiles : tile) * TK, last = (drafted ? nq : kv) - 1;
-#pragma unroll
-    for (int x = 0; x < PC / 4; ++x) {
-      const int at = (w * (PC / 4) + x) * 64, r = (at + lane) / PC, c = ((at + lane) % PC) ^ piece_swap<D>(r);
-      const long from = min(t0 + r, last) * stride + c * 8;
-      load_to_lds(K + from, tiles[slot][0] + at * 8);
-      load_to_lds(V + from, tiles[slot][1] + at * 8);
+  // one row block; in a paired call the last with the first, the last but one with the second, ..
+  for (int turn = 0; turn < (a.paired ? 2 : 1); ++turn) {
+    const int rb = turn ? unit : a.nrb - 1 - unit;        // (a prompt's last rows see most: first)
+    if (turn) {
+      if (2 * unit >= a.nrb - 1) break;
+      __syncthreads();                                    // the other waves are done with the tiles
     }
-  };
+    const int row = rb * PROMPT_ROWS + w * 32 + i, iq = a.by_group.div(row), gq = row - iq * G;
+    const bool live = row < a.R && iq < nq;
+    const int lim = live ? (TREE ? kv : max(0, kv - nq + iq + 1)) : 0x7fffffff;
+    const unsigned long long sees = TREE && live ? a.visible[(long)b * a.n_q + iq] & low_bits(nq) : 0;
+    const long row_at = (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * G + gq) * D;
+    const int lim_min = wave_min_int(lim);
+    // (what the row block's last live row sees)
+    const int last_row = min(min(a.R, nq * G), (rb + 1) * PROMPT_ROWS) - 1;
+    const int most = last_row < rb * PROMPT_ROWS ? 0 : (TREE ? kv : max(0, kv - nq + a.by_group.div(last_row) + 1));
+    const int cache_tiles = (most + TK - 1) / TK;
+    const int tiles_all = cache_tiles + (TREE && last_row >= rb * PROMPT_ROWS ? (nq + TK - 1) / TK : 0);
+    const int per = (tiles_all + a.slices - 1) / a.slices;
+    const int t_begin = min(tiles_all, slice * per), t_end = min(tiles_all, t_begin + per);
 
-  floatx16 acc[OB];
+    half8 qf[KS];
+    {
+      const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const half_t *>(a.q) + row_at);
 #pragma unroll
-  for (int o = 0; o < OB; ++o)
+      for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(half8, flip_sign<half_t>(src[2 * s + hb], a.flip));
+    }
+    // tile `tile` of K or V into a slot of it
+    auto fetch = [&](const void *pool, const void *nodes, int tile, half_t *to) {
+      if (tile >= t_end) return;
+      const bool drafted = TREE && tile >= cache_tiles;
+      const int stride = (drafted ? (int)a.by_H.d * D : D) * 2;
+      const int t0 = (drafted ? tile - cache_tiles : tile) * TK, last = (drafted ? nq : kv) - 1 - t0;
+      const char *base = drafted ? static_cast<const char *>(nodes) + ((long)b * a.n_q * a.by_H.d + h) * D * 2
+                                 : static_cast<const char *>(pool) + (long)bh * a.N_cap * D * 2;
+      const unsigned r0 = opaque(from_row);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[o][e] = 0.f;
-  float ref = NOTHING_SEEN, sum = 0.f;
+      for (int x = 0; x < PC / 4; ++x)       // (64 rows: offsets inside a tile fit 32 bits)
+        load_to_lds(base + (long)t0 * stride,
+                    (unsigned)(min((int)r0 + x * (64 / PC), last) * stride) + (from_piece ^ piece_swap<D>(x * (64 / PC))) * 16,
+                    to + (w * (PC / 4) + x) * 512);
+    };
 
-  if (t_begin < t_end) fetch(t_begin, 0);
-  for (int tile = t_begin; tile < t_end; ++tile) {
-    const int slot = (tile - t_begin) & 1;
-    __builtin_amdgcn_s_waitcnt(0x0f70);                   // vmcnt(0): this tile is there ...
-    __syncthreads();                                      // ... in every wave's part, and the other slot is free
-    if (tile + 1 < t_end) fetch(tile + 1, slot ^ 1);
-    const bool drafted = TREE && tile >= cache_tiles;
-    const int t0 = (drafted ? tile - cache_tiles : tile) * TK;
-    if (!drafted && t0 >= lim_max) continue;              // (no row of this wave sees any of it)
-    const half_t *K = tiles[slot][0], *V = tiles[slot][1];
-    floatx16 s[2];
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[m][e] = 0.f;
-#pragma unroll
-      for (int k = 0; k < KS; ++k)
-        s[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(tile_row_piece<D>(K, m * 32 + i, 2 * k + hb), qf[k], s[m], 0, 0, 0);
-    }
-    if (drafted) {
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (!(sees >> (m * 32 + (e / 4) * 8 + hb * 4 + e % 4) & 1)) s[m][e] = -INFINITY;
-    } else if (t0 + TK > lim_min) {
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (t0 + m * 32 + (e / 4) * 8 + hb * 4 + e % 4 >= lim) s[m][e] = -INFINITY;
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[m][e]);
-    if (__any(top * a.c > ref + RISE)) {
-      const float to = fmaxf(ref, both_max(top) * a.c), shrink = exp2_fast(ref - to);
-      ref = to;
-      sum *= shrink;
-#pragma unroll
-      for (int o = 0; o < OB; ++o) acc[o] *= shrink;
-    }
-    half8 p[4];
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float x = exp2_fast(fmaf(s[m][e], a.c, -ref));
-        sum += x;
-        p[m * 2 + e / 8][e % 8] = (half_t)x;
-      }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int o = 0; o < OB; ++o) {
-        const uint2 lo = tile_columns<D>(V, k * 16 + 4 * hb, o * 32 + (lane & 16), lane & 15);
-        const uint2 hi = tile_columns<D>(V, k * 16 + 8 + 4 * hb, o * 32 + (lane & 16), lane & 15);
-        acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, make_uint4(lo.x, lo.y, hi.x, hi.y)), p[k], acc[o], 0, 0, 0);
-      }
-  }
-
-  if (!live) return;
-  sum = both_sum(sum);
-  const float inv = inverse_of(sum);
-  if (a.slices == 1) {
-    half_t *to = static_cast<half_t *>(a.out) + row_at;
+    floatx16 acc[OB];
 #pragma unroll
     for (int o = 0; o < OB; ++o)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        half_t v[4];
+      for (int e = 0; e < 16; ++e) acc[o][e] = 0.f;
+    float ref = NOTHING_SEEN, sums[4] = {0.f, 0.f, 0.f, 0.f};       // (four sums: no chain of dependent additions)
+    floatx16 sA = {}, sB = {};
+    half8 pA[2], pB[2];
+
+    // The 32-token half blocks of the tiles are a pipeline: while the weights of one are worked out on the vector
+    // units, the matrix units take the logits of the next and the output of the one before.
+    //   now: logits in, weights out (half block `now_at` of the sequence of tiles); next: the logits of `next_row` ..
+    //   of tile K; out: acc += the weights `old` times rows `old_row` .. of tile V
+    auto half_step = [&](auto has_now, auto has_next, auto has_old, const floatx16 &now, int now_tile, int now_half,
+                         half8 (&weights)[2], floatx16 &next, const half_t *K, int next_row, const half8 (&old)[2],
+                         const half_t *V, int old_row) {
+      constexpr bool NOW = decltype(has_now)::value, NEXT = decltype(has_next)::value, OLD = decltype(has_old)::value;
+      half8 kf[KS];
+      uint2 vt[2][OB][2];
+      if constexpr (NEXT) {
+        const unsigned at = opaque(k_base);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (half_t)(acc[o][x * 4 + e] * inv);
-        store_words<2>(to + o * 32 + x * 8 + hb * 4, v);
+        for (int k = 0; k < KS; ++k) kf[k] = row_piece<D>(lds_at(K + next_row * D), at, k);
       }
-    if (hb == 0 && a.stats) a.stats[(long)bh * a.R + row] = make_float2(ref, inv);
-  } else {
-    const long at = ((long)bh * a.slices + slice) * a.R + row;
+      if constexpr (OLD) {
+        const unsigned at = opaque(v_base);
 #pragma unroll
-    for (int o = 0; o < OB; ++o)
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        *reinterpret_cast<floatx4 *>(a.part + at * D + o * 32 + x * 8 + hb * 4) =
-            floatx4{acc[o][x * 4], acc[o][x * 4 + 1], acc[o][x * 4 + 2], acc[o][x * 4 + 3]};
-    if (hb == 0) a.part_ml[at] = make_float2(ref, sum);
+          for (int o = 0; o < OB; ++o)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) vt[k][o][x] = column_rows<D>(lds_at(V + (old_row + k * 16) * D), at, o, x);
+      }
+      floatx16 s;
+      float shrink = 1.f;
+      bool rises = false;
+      if constexpr (NOW) {
+        s = now;
+        const bool drafted = TREE && now_tile >= cache_tiles;
+        const int t0 = (drafted ? now_tile - cache_tiles : now_tile) * TK + now_half * 32;
+        if (drafted) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!(sees >> (now_half * 32 + (e / 4) * 8 + hb * 4 + e % 4) & 1)) s[e] = -INFINITY;
+        } else if (t0 + 32 > lim_min) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (t0 + (e / 4) * 8 + hb * 4 + e % 4 >= lim) s[e] = -INFINITY;
+        }
+        float top = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+        top = both_max(top) * a.c;
+        const float to = top > ref + RISE ? top : ref;
+        rises = __any(to != ref);
+        shrink = exp2_fast(ref - to);
+        ref = to;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[e] *= shrink;
+      }
+      if constexpr (NEXT) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) next[e] = 0.f;
+      }
+      // (one product of each kind after the other, with the vector work between them)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        if constexpr (NEXT) {
+#pragma unroll
+          for (int k = x * KS / 8; k < (x + 1) * KS / 8; ++k)
+            next = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[k], qf[k], next, 0, 0, 0);
+        }
+        if constexpr (OLD) {
+#pragma unroll
+          for (int y = x * 2 * OB / 8; y < (x + 1) * 2 * OB / 8; ++y) {
+            const int k = y / OB, o = y % OB;
+            const uint4 v = make_uint4(vt[k][o][0].x, vt[k][o][0].y, vt[k][o][1].x, vt[k][o][1].y);
+            acc[o] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, v), old[k], acc[o], 0, 0, 0);
+          }
+        }
+        if constexpr (NOW) {
+#pragma unroll
+          for (int e = 2 * x; e < 2 * x + 2; ++e) {
+            const float p = exp2_fast(fmaf(s[e], a.c, -ref));
+            sums[e % 4] += p;
+            weights[e / 8][e % 8] = (half_t)p;
+          }
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) keep_here(sums[e]);      // (not put off: the weights' registers are needed)
+      if (NOW && rises) {
+#pragma unroll
+        for (int o = 0; o < OB; ++o) acc[o] *= shrink;
+      }
+    };
+    typedef std::true_type Y;
+    typedef std::false_type N;
+    if (t_begin < t_end) {
+      half_t *const k0 = tiles[0][0], *const k1 = tiles[1][0], *const v0 = tiles[0][1], *const v1 = tiles[1][1];
+      fetch(a.K, a.k_tree, t_begin, k0);
+      wait_for_lds_loads();
+      __syncthreads();
+      fetch(a.K, a.k_tree, t_begin + 1, k1);
+      fetch(a.V, a.v_tree, t_begin, v0);
+      half_step(N(), Y(), N(), sB, 0, 0, pB, sA, k0, 0, pA, v0, 0);
+      half_step(Y(), Y(), N(), sA, t_begin, 0, pA, sB, k0, 32, pB, v0, 0);
+      // a turn: the logits of tile `tile`, the weights of its first and the last tile's second half, the last tile's output
+      auto turn_of = [&](int tile, half_t *k, half_t *v, half_t *k_free, half_t *v_free) {
+        wait_for_lds_loads();                             // these tiles are there ...
+        __syncthreads();                                  // ... in every wave's part, and the other slots are free
+        fetch(a.K, a.k_tree, tile + 1, k_free);
+        fetch(a.V, a.v_tree, tile, v_free);
+        half_step(Y(), Y(), Y(), sB, tile - 1, 1, pB, sA, k, 0, pA, v, 0);
+        half_step(Y(), Y(), Y(), sA, tile, 0, pA, sB, k, 32, pB, v, 32);
+      };
+      int tile = t_begin + 1;
+      for (; tile + 1 < t_end; tile += 2) {
+        turn_of(tile, k1, v0, k0, v1);
+        turn_of(tile + 1, k0, v1, k1, v0);
+      }
+      const bool odd = tile < t_end;
+      if (odd) turn_of(tile, k1, v0, k0, v1);
+      wait_for_lds_loads();
+      __syncthreads();
+      const half_t *v = odd ? v1 : v0;
+      half_step(Y(), N(), Y(), sB, t_end - 1, 1, pB, sA, k0, 0, pA, v, 0);
+      half_step(N(), N(), Y(), sA, 0, 0, pA, sB, k0, 0, pB, v, 32);
+    }
+
+    if (!live) continue;
+    const float sum = both_sum((sums[0] + sums[1]) + (sums[2] + sums[3]));
+    const float inv = inverse_of(sum);
+    if (a.slices == 1) {
+      half_t *to = static_cast<half_t *>(a.out) + row_at;
+#pragma unroll
+      for (int o = 0; o < OB; ++o)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          half_t v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (half_t)(acc[o][x * 4 + e] * inv);
+          store_words<2>(to + o * 32 + x * 8 + hb * 4, v);
+        }
+      if (hb == 0 && a.stats) a.stats[(long)bh * a.R + row] = make_float2(ref, inv);
+    } else {
+      const long at = ((long)bh * a.slices + slice) * a.R + row;
+#pragma unroll
+      for (int o = 0; o < OB; ++o)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          *reinterpret_cast<floatx4 *>(a.part + at * D + o * 32 + x * 8 + hb * 4) =
+              floatx4{acc[o][x * 4], acc[o][x * 4 + 1], acc[o][x * 4 + 2], acc[o][x * 4 + 3]};
+      if (hb == 0) a.part_ml[at] = make_float2(ref, sum);
+    }
   }
 }
 
@@ -564,14 +637,16 @@ template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt
     for (int k = 0; k < KS; ++k) kf[m][k] = __builtin_bit_cast(half8, flip_sign<half_t>(reinterpret_cast<const uint4 *>(src)[2 * k + hb], a.flip));
   }
   auto fetch = [&](int tile, int slot) {
+    const int iq0 = a.by_group.div(first + tile * MASS_ROWS);
+    const half_t *q0 = static_cast<const half_t *>(a.q) + (((long)b * a.n_q + iq0) * a.Hq + h * G) * D;
 #pragma unroll
     for (int x = 0; x < PC / 4; ++x) {
       const int at = (w * (PC / 4) + x) * 64, r = (at + lane) / PC, c = ((at + lane) % PC) ^ piece_swap<D>(r);
       const int row = min(first + tile * MASS_ROWS + r, rows - 1), iq = a.by_group.div(row);
-      load_to_lds(static_cast<const half_t *>(a.q) + (((long)b * a.n_q + iq) * a.Hq + h * G + row - iq * G) * D + c * 8,
-                  tiles[slot] + at * 8);
+      load_to_lds(q0, (unsigned)(((iq - iq0) * a.Hq + row - iq * G) * D + c * 8) * 2, tiles[slot] + at * 8);
     }
   };
+  const unsigned q_base = row_base<D>(lane);
   float sums[2][16] = {};
   if (tiles_n > 0) fetch(0, 0);
   for (int tile = 0; tile < tiles_n; ++tile) {
@@ -600,7 +675,7 @@ template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt
         for (int e = 0; e < 16; ++e) s[m][e] = 0.f;
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        const half8 q = tile_row_piece<D>(tiles[slot], n * 32 + i, 2 * k + hb);
+        const half8 q = row_piece<D>(lds_at(tiles[slot] + n * 32 * D), q_base, k);
 #pragma unroll
         for (int m = 0; m < 2; ++m) s[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[m][k], q, s[m], 0, 0, 0);
       }
@@ -690,6 +765,12 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   a.part = reinterpret_cast<float *>(ws + p.part_at);
   a.logits = reinterpret_cast<float *>(ws + p.logits_at);
   a.logits_ld = p.logits_ld;
+  // a causal call with workgroups to spare: each takes a late and an early row block, so that all take equally long
+  a.paired = p.prompt && !tree && p.slices == 1 && BH * p.nrb >= 1024;
+  if (a.paired) {
+    const int units = (p.nrb + 1) / 2;
+    a.total = (int)(BH * units), a.per_xcd = div_up(a.total, 8), a.by_pair = ig_fast_div(units);
+  }
   const dim3 grid(a.per_xcd * 8), block(256);
 #define STREAM(T, D, NT)                                                                             \
   {                                                                                                  \
