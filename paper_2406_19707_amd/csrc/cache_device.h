@@ -133,7 +133,7 @@ __device__ __forceinline__ unsigned opaque(unsigned v) {
   return v;
 }
 // the value is worked out before this point
-__device__ __forceinline__ void keep_here(float &v) { asm volatile("" : "+v"(v)); }
+template <typename V> __device__ __forceinline__ void keep_here(V &v) { asm volatile("" : "+v"(v)); }
 typedef const char __attribute__((address_space(3))) *lds_bytes;
 __device__ __forceinline__ lds_bytes lds_at(const half_t *tile) {
   return (lds_bytes)(const __attribute__((address_space(3))) half_t *)tile;
@@ -164,7 +164,9 @@ template <int D> __device__ __forceinline__ uint2 column_rows(lds_bytes tile, un
 // (wait_for_lds_loads, then a barrier where other waves loaded part of it).
 __device__ __forceinline__ void load_to_lds(const void *from, unsigned offset, half_t *to) {
   const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)to;
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(at), "v"(offset), "s"(from) : "memory");
+  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)from), hi = __builtin_amdgcn_readfirstlane((unsigned)((uintptr_t)from >> 32));
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(__builtin_amdgcn_readfirstlane(at)), "v"(offset),
+               "s"((unsigned long long)hi << 32 | lo) : "memory");
 }
 __device__ __forceinline__ void wait_for_lds_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 

@@ -332,7 +332,7 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
       for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(half8, flip_sign<half_t>(src[2 * s + hb], a.flip));
     }
     // tile `tile` of K or V into a slot of it
-    auto fetch = [&](const void *pool, const void *nodes, int tile, half_t *to) {
+    auto fetch = [&](const void *pool, const void *nodes, int tile, half_t *to) __attribute__((always_inline)) {
       if (tile >= t_end) return;
       const bool drafted = TREE && tile >= cache_tiles;
       const int stride = (drafted ? (int)a.by_H.d * D : D) * 2;
@@ -362,7 +362,7 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
     //   of tile K; out: acc += the weights `old` times rows `old_row` .. of tile V
     auto half_step = [&](auto has_now, auto has_next, auto has_old, const floatx16 &now, int now_tile, int now_half,
                          half8 (&weights)[2], floatx16 &next, const half_t *K, int next_row, const half8 (&old)[2],
-                         const half_t *V, int old_row) {
+                         const half_t *V, int old_row) __attribute__((always_inline)) {
       constexpr bool NOW = decltype(has_now)::value, NEXT = decltype(has_next)::value, OLD = decltype(has_old)::value;
       half8 kf[KS];
       uint2 vt[2][OB][2];
@@ -388,13 +388,15 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
         const bool drafted = TREE && now_tile >= cache_tiles;
         const int t0 = (drafted ? now_tile - cache_tiles : now_tile) * TK + now_half * 32;
         if (drafted) {
+          const unsigned bits = (unsigned)(sees >> (now_half * 32)) >> opaque(hb * 4);
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (!(sees >> (now_half * 32 + (e / 4) * 8 + hb * 4 + e % 4) & 1)) s[e] = -INFINITY;
+            if (!(bits >> ((e / 4) * 8 + e % 4) & 1)) s[e] = -INFINITY;
         } else if (t0 + 32 > lim_min) {
+          const int mine = t0 + (int)opaque(hb * 4);
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (t0 + (e / 4) * 8 + hb * 4 + e % 4 >= lim) s[e] = -INFINITY;
+            if (mine + ((e / 4) * 8 + e % 4) >= lim) s[e] = -INFINITY;
         }
         float top = s[0];
 #pragma unroll
@@ -455,7 +457,7 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
       half_step(N(), Y(), N(), sB, 0, 0, pB, sA, k0, 0, pA, v0, 0);
       half_step(Y(), Y(), N(), sA, t_begin, 0, pA, sB, k0, 32, pB, v0, 0);
       // a turn: the logits of tile `tile`, the weights of its first and the last tile's second half, the last tile's output
-      auto turn_of = [&](int tile, half_t *k, half_t *v, half_t *k_free, half_t *v_free) {
+      auto turn_of = [&](int tile, half_t *k, half_t *v, half_t *k_free, half_t *v_free) __attribute__((always_inline)) {
         wait_for_lds_loads();                             // these tiles are there ...
         __syncthreads();                                  // ... in every wave's part, and the other slots are free
         fetch(a.K, a.k_tree, tile + 1, k_free);
@@ -611,96 +613,153 @@ __global__ __launch_bounds__(256) void attend_mass(StreamArgs a, float *mass, Fa
 }
 
 // The same in half precision for calls of many rows: a wave keeps 64 keys, a workgroup 256, and the query rows
-// come through LDS 64 at a time, one tile ahead.  What is left is the exponential and two fused multiply-adds a
-// pair beside the products.
+// come through LDS 64 at a time, one tile ahead.  As in attend_prompt it is a pipeline: while the weights of 32 rows
+// and 32 keys are worked out (an exponential and two fused multiply-adds a pair), the matrix units take the next
+// logits.
 constexpr int MASS_KEYS = 256, MASS_ROWS = 64;
-template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_mass(StreamArgs a, float *mass, FastDiv by_chunks) {
+template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_mass(StreamArgs a, float *mass) {
   constexpr int KS = D / 16, PC = D / 8;
   __shared__ __attribute__((aligned(16))) half_t tiles[2][MASS_ROWS * D];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = lane & 31, hb = lane >> 5;
   const int work = xcd_order(blockIdx.x, a.per_xcd);
   if (work >= a.total) return;
-  const int bh = by_chunks.div(work), x0 = by_chunks.mod(work);
+  const int bh = a.by_pair.div(work), unit = work - bh * (int)a.by_pair.d;
   const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, G = (int)a.by_group.d;
   const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
-  const int t0 = x0 * MASS_KEYS + w * 64;
-  if (x0 * MASS_KEYS >= kv) return;
-  // the first query that sees slot t is number t - (kv - nq)
-  const int rows = nq * G, first = max(0, x0 * MASS_KEYS - (kv - nq)) * G, tiles_n = (max(0, rows - first) + MASS_ROWS - 1) / MASS_ROWS;
-
-  half8 kf[2][KS];
-#pragma unroll
-  for (int m = 0; m < 2; ++m) {
-    const half_t *src = static_cast<const half_t *>(a.K) + ((long)bh * a.N_cap + min(t0 + m * 32 + i, kv - 1)) * D;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) kf[m][k] = __builtin_bit_cast(half8, flip_sign<half_t>(reinterpret_cast<const uint4 *>(src)[2 * k + hb], a.flip));
-  }
-  auto fetch = [&](int tile, int slot) {
-    const int iq0 = a.by_group.div(first + tile * MASS_ROWS);
-    const half_t *q0 = static_cast<const half_t *>(a.q) + (((long)b * a.n_q + iq0) * a.Hq + h * G) * D;
-#pragma unroll
-    for (int x = 0; x < PC / 4; ++x) {
-      const int at = (w * (PC / 4) + x) * 64, r = (at + lane) / PC, c = ((at + lane) % PC) ^ piece_swap<D>(r);
-      const int row = min(first + tile * MASS_ROWS + r, rows - 1), iq = a.by_group.div(row);
-      load_to_lds(q0, (unsigned)(((iq - iq0) * a.Hq + row - iq * G) * D + c * 8) * 2, tiles[slot] + at * 8);
-    }
-  };
+  const int rows = nq * G;
+  const unsigned from_row = w * 16 + lane / PC, from_piece = (lane % PC) ^ piece_swap<D>(from_row);
   const unsigned q_base = row_base<D>(lane);
-  float sums[2][16] = {};
-  if (tiles_n > 0) fetch(0, 0);
-  for (int tile = 0; tile < tiles_n; ++tile) {
-    const int slot = tile & 1, r0 = first + tile * MASS_ROWS;
-    float2 st[2];
-    int seen[2];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const int row = min(r0 + n * 32 + i, rows - 1);
-      st[n] = a.stats[(long)bh * a.R + row];
-      seen[n] = kv - nq + a.by_group.div(row) + 1;
-      if (r0 + n * 32 + i >= rows) st[n] = make_float2(INFINITY, 0.f);      // (no such row: weights of zero)
+
+  // one block of keys; in a paired call the first with the last, the second with the last but one, ..
+  for (int turn = 0; turn < (a.paired ? 2 : 1); ++turn) {
+    const int kb = turn ? a.nrb - 1 - unit : unit;        // (a prompt's first keys are seen by most rows: first)
+    if (turn) {
+      if (2 * unit >= a.nrb - 1) break;
+      __syncthreads();                                    // the other waves are done with the tiles
     }
-    const int seen_first = kv - nq + a.by_group.div(r0) + 1, seen_last = kv - nq + a.by_group.div(min(r0 + MASS_ROWS, rows) - 1) + 1;
-    __builtin_amdgcn_s_waitcnt(0x0f70);                   // vmcnt(0)
-    __syncthreads();
-    if (tile + 1 < tiles_n) fetch(tile + 1, slot ^ 1);
-    if (seen_last <= t0) continue;                        // (before the first query that sees this wave's keys)
-    const bool masked = seen_first < t0 + 64;
+    if (kb * MASS_KEYS >= kv) continue;
+    const int t0 = kb * MASS_KEYS + w * 64;
+    // the first query that sees slot t is number t - (kv - nq)
+    const int first = max(0, kb * MASS_KEYS - (kv - nq)) * G;
+    const int tiles_n = (max(0, rows - first) + MASS_ROWS - 1) / MASS_ROWS;
+    half8 kf[2][KS];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      floatx16 s[2];
+    for (int m = 0; m < 2; ++m) {
+      const half_t *src = static_cast<const half_t *>(a.K) + ((long)bh * a.N_cap + min(t0 + m * 32 + i, kv - 1)) * D;
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+      for (int k = 0; k < KS; ++k) kf[m][k] = __builtin_bit_cast(half8, flip_sign<half_t>(reinterpret_cast<const uint4 *>(src)[2 * k + hb], a.flip));
+    }
+    auto fetch = [&](int tile, half_t *to) __attribute__((always_inline)) {
+      if (tile >= tiles_n) return;
+      const int r0 = first + tile * MASS_ROWS, iq0 = a.by_group.div(r0);
+      const half_t *q0 = static_cast<const half_t *>(a.q) + (((long)b * a.n_q + iq0) * a.Hq + h * G) * D;
+      const int mine = r0 + (int)opaque(from_row);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[m][e] = 0.f;
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const half8 q = row_piece<D>(lds_at(tiles[slot] + n * 32 * D), q_base, k);
-#pragma unroll
-        for (int m = 0; m < 2; ++m) s[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[m][k], q, s[m], 0, 0, 0);
+      for (int x = 0; x < PC / 4; ++x) {
+        const int row = min(mine + x * (64 / PC), rows - 1), iq = a.by_group.div(row);
+        load_to_lds(q0, (unsigned)(((iq - iq0) * a.Hq + row - iq * G) * D) * 2 + (from_piece ^ piece_swap<D>(x * (64 / PC))) * 16,
+                    to + (w * (PC / 4) + x) * 512);
       }
+    };
+    // a half tile's row of this lane: what its weights are relative to, 1 / their sum, and the slots it sees
+    struct Row {
+      float ref, inv;
+      int seen;
+    };
+    auto row_of = [&](int tile, int half, float2 st) __attribute__((always_inline)) {
+      const int r = first + tile * MASS_ROWS + half * 32 + i;
+      const bool there = r < rows;                        // (else weights of zero)
+      return Row{there ? st.x : INFINITY, there ? st.y : 0.f, kv - nq + a.by_group.div(min(r, rows - 1)) + 1};
+    };
+    float2 st[2], st_now[2];                              // of the next tile, asked for with it, and of this one
+    auto ask = [&](int tile) __attribute__((always_inline)) {
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+      for (int half = 0; half < 2; ++half)
+        st[half] = a.stats[(long)bh * a.R + min(first + tile * MASS_ROWS + half * 32 + i, rows - 1)];
+    };
+    floatx16 sums[2] = {}, sA = {}, sB = {};
+    half8 qf[KS];
+    auto read_rows = [&](const half_t *Q) __attribute__((always_inline)) {
+      const unsigned at = opaque(q_base);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float p = exp2_fast(fmaf(s[m][e], a.c, -st[n].x));
-          const float more = fmaf(p, st[n].y, sums[m][e]);
-          if (!masked || t0 + m * 32 + (e / 4) * 8 + hb * 4 + e % 4 < seen[n]) sums[m][e] = more;
+      for (int k = 0; k < KS; ++k) qf[k] = row_piece<D>(lds_at(Q), at, k);
+    };
+    // weights of the logits `now` (row, keys m) added to the sums, while `next` becomes the logits of the rows in qf and keys n
+    auto step = [&](auto has_now, auto has_next, const floatx16 &now, const Row &row, int m, floatx16 &next, int n) __attribute__((always_inline)) {
+      constexpr bool NOW = decltype(has_now)::value, NEXT = decltype(has_next)::value;
+      floatx16 s = now;
+      if constexpr (NOW) {
+        if (__any(row.seen < t0 + m * 32 + 32)) {
+          const int mine = t0 + m * 32 + (int)opaque(hb * 4);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (mine + ((e / 4) * 8 + e % 4) >= row.seen) s[e] = -INFINITY;
         }
+      }
+      if constexpr (NEXT) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) next[e] = 0.f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) next = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[n][k], qf[k], next, 0, 0, 0);
+      }
+      if constexpr (NOW) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[m][e] = fmaf(exp2_fast(fmaf(s[e], a.c, -row.ref)), row.inv, sums[m][e]);
+        keep_here(sums[m]);
+      }
+    };
+    typedef std::true_type Y;
+    typedef std::false_type N;
+    if (tiles_n > 0) {
+      fetch(0, tiles[0]);
+      ask(0);
+      wait_for_lds_loads();
+      __syncthreads();
+      Row rA = row_of(0, 0, st[0]), rB = row_of(0, 1, st[1]);
+      auto turn_of = [&](auto has_last, int tile, half_t *q, half_t *q_free) __attribute__((always_inline)) {
+        fetch(tile + 1, q_free);
+        ask(tile + 1);
+        read_rows(q);
+        step(has_last, Y(), sB, rB, 1, sA, 0);
+        if (decltype(has_last)::value) rA = row_of(tile, 0, st_now[0]), rB = row_of(tile, 1, st_now[1]);
+        step(Y(), Y(), sA, rA, 0, sB, 1);
+        read_rows(q + 32 * D);
+        step(Y(), Y(), sB, rA, 1, sA, 0);
+        step(Y(), Y(), sA, rB, 0, sB, 1);
+      };
+      auto next_tile = [&]() __attribute__((always_inline)) {
+        wait_for_lds_loads();                             // the tile is there ...
+        __syncthreads();                                  // ... in every wave's part, and the other slot is free
+        st_now[0] = st[0], st_now[1] = st[1];
+      };
+      turn_of(N(), 0, tiles[0], tiles[1]);
+      int tile = 1;
+      for (; tile + 1 < tiles_n; tile += 2) {
+        next_tile();
+        turn_of(Y(), tile, tiles[1], tiles[0]);
+        next_tile();
+        turn_of(Y(), tile + 1, tiles[0], tiles[1]);
+      }
+      if (tile < tiles_n) {
+        next_tile();
+        turn_of(Y(), tile, tiles[1], tiles[0]);
+      }
+      step(Y(), N(), sB, rB, 1, sA, 0);
     }
+    // the 32 lanes of a half wave added up; lane i then keeps the sum of register i
+    float mine = 0.f;
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float v = row16_sum(sums[m][e]);
+        v += __shfl_xor(v, 16, 64);
+        if (i == m * 16 + e) mine = v;
+      }
+    const int t = t0 + (i / 16) * 32 + ((i % 16) / 4) * 8 + hb * 4 + i % 4;
+    if (t < kv) mass[(long)bh * a.N_cap + t] += mine;
   }
-  // the 32 lanes of a half wave added up; lane i then keeps the sum of register i
-  float mine = 0.f;
-#pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float v = row16_sum(sums[m][e]);
-      v += __shfl_xor(v, 16, 64);
-      if (i == m * 16 + e) mine = v;
-    }
-  const int t = t0 + (i / 16) * 32 + ((i % 16) / 4) * 8 + hb * 4 + i % 4;
-  if (t < kv) mass[(long)bh * a.N_cap + t] += mine;
 }
 
 int div_up(long n, long d) { return (int)((n + d - 1) / d); }
@@ -833,13 +892,17 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
     if (d->dtype == IG_F16) JOIN(half_t) else JOIN(float)
   }
   if (c.mass && !logits && p.prompt) {
-    const FastDiv by_chunks = ig_fast_div(div_up(d->N, MASS_KEYS));
-    a.total = (int)(by_chunks.d * BH), a.per_xcd = div_up(a.total, 8);
+    // keys in pairs of blocks as the rows above: a prompt's first keys are seen by all of its rows, its last by few
+    a.nrb = div_up(d->N, MASS_KEYS);
+    a.paired = BH * a.nrb >= 1024;
+    const int units = a.paired ? (a.nrb + 1) / 2 : a.nrb;
+    a.by_pair = ig_fast_div(units);
+    a.total = (int)(BH * units), a.per_xcd = div_up(a.total, 8);
     const dim3 mgrid(a.per_xcd * 8);
 #define PROMPT_MASS(T, D)                                                                            \
   {                                                                                                  \
     auto k = prompt_mass<D>;                                                                         \
-    IG_LAUNCH(ctx, IG_K_CACHE, k, mgrid, block, stream, a, c.mass, by_chunks);                       \
+    IG_LAUNCH(ctx, IG_K_CACHE, k, mgrid, block, stream, a, c.mass);                                  \
   }
     BY_DIM(half_t, PROMPT_MASS)
   } else if (c.mass && !logits) {
