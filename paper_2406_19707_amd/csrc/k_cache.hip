@@ -48,9 +48,14 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   const T *q = static_cast<const T *>(a.q);
   uint4 qf[NT][KCH];
   int lim_min = 0x7fffffff, lim_max = 0;
+  // Kept logits, up to 16 rows: the columns that are left hold the rows again, and each copy keeps another tile's
+  // logits, so that they are stored once every `copies` tiles and by all lanes.  (One row, 32768 slots, 160 pools:
+  // stored after every tile by a sixteenth of the lanes they cost 48 of 490 us.)
+  const int rows_p2 = LOGITS && NT == 1 ? a.rows_p2 : 16, copies = 16 / rows_p2, copy = LOGITS && NT == 1 ? i / rows_p2 : 0;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int row = rb * RB + n * 16 + i, iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
+    const int row = rb * RB + n * 16 + (LOGITS && NT == 1 ? i & (rows_p2 - 1) : i);
+    const int iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
     live[n] = row < a.R && iq < nq;
     lim[n] = live[n] ? (TREE ? kv : max(0, kv - nq + iq + 1)) : 0x7fffffff;
     sees[n] = TREE && live[n] ? a.visible[(long)b * a.n_q + iq] & low_bits(nq) : 0;
@@ -106,6 +111,8 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
     for (int j = 0; j < CJ; ++j) acc[n][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
+  floatx4 kept[MT];
+  int count = 0;
   int tile = t_begin + w;
   if (tile < t_end) {
     load_k(tile);
@@ -146,7 +153,20 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
           for (int r = 0; r < 4; ++r)
             if (t0 + 4 * m + r >= lim[n]) s[n][m][r] = -INFINITY;
     }
-    if (LOGITS) {
+    if constexpr (LOGITS && NT == 1) {
+      const int at = count++ & (copies - 1);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) kept[m][r] = copy == at ? s[0][m][r] : kept[m][r];
+      if (at == copies - 1 || !more) {
+        if (live[0] && copy <= at) {
+          float *to = a.logits + ((long)bh * a.R + (i & (rows_p2 - 1))) * a.logits_ld + t0 - (at - copy) * 4 * TT;
+#pragma unroll
+          for (int m = 0; m < MT; ++m) *reinterpret_cast<floatx4 *>(to + 4 * m) = kept[m];
+        }
+      }
+    } else if constexpr (LOGITS) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
         if (live[n]) {
@@ -252,7 +272,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int row = rb * RB + n * 16 + i;
-    if (!live[n]) continue;
+    if (!live[n] || copy) continue;
     const float inv = inverse_of(l_all[n]);
     if (a.slices == 1) {
       const int iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
@@ -508,48 +528,94 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
 }
 
 // ---- joining the slices, and the weights of single-token calls ------------------------------------------
-// A workgroup takes rows x, x + chunks, .. of a pool's R and, where logits were kept, the slots
-// 1024 x .. of that pool: mass[t] += sum over the rows of exp2(c s - c m) / l.
-template <typename T, bool LOGITS>
-__global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, int D, FastDiv by_chunks) {
-  __shared__ float2 stat[64];                              // (LOGITS: R <= 64)
-  const int bh = by_chunks.div(blockIdx.x), x = by_chunks.mod(blockIdx.x), b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, tid = threadIdx.x;
-  const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
-  const int G = (int)a.by_group.d;
-  auto joined = [&](int row) {                             // the row's reference and 1 / sum over all slices
-    float m = NOTHING_SEEN, l = 0.f;
-    for (int s = 0; s < a.slices; ++s) m = fmaxf(m, a.part_ml[((long)bh * a.slices + s) * a.R + row].x);
-    for (int s = 0; s < a.slices; ++s) {
-      const float2 ml = a.part_ml[((long)bh * a.slices + s) * a.R + row];
-      l += ml.y * exp2_fast(ml.x - m);
+// A workgroup takes 256 / d rows of a pool and, where logits were kept, 1024 slots of it: mass[t] += sum over the
+// rows of exp2(c s - ref) / sum.  Small calls are a chain of trips through memory, so slices are taken eight at a
+// time, all their loads together, and a slot's weight and first logit are asked for before the sums are known.
+struct Joined {
+  float ref, sum, out;
+};
+// the row's state over all slices, and element e of its output before the division (OUT)
+template <bool OUT> __device__ __forceinline__ Joined join_row(const StreamArgs &a, int bh, int row, int D, int e) {
+  constexpr int U = 8;
+  Joined j = {NOTHING_SEEN, 0.f, 0.f};
+  for (int s0 = 0; s0 < a.slices; s0 += U) {
+    float2 ml[U];
+    float o[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const long at = ((long)bh * a.slices + min(s0 + u, a.slices - 1)) * a.R + row;
+      ml[u] = a.part_ml[at];
+      if (OUT) o[u] = a.part[at * D + e];
     }
-    return make_float2(m, inverse_of(l));
-  };
-  if (a.slices > 1) {
-    const int per = 256 / D < 1 ? 1 : 256 / D;             // rows a workgroup takes at a time
-    for (int row = x * per + tid / D; row < nq * G && tid < per * D; row += (int)by_chunks.d * per) {
-      const float2 st = joined(row);
-      const int e = tid % D;
-      float o = 0.f;
-      for (int s = 0; s < a.slices; ++s) {
-        const long at = ((long)bh * a.slices + s) * a.R + row;
-        o += a.part[at * D + e] * exp2_fast(a.part_ml[at].x - st.x);
-      }
-      const int iq = a.by_group.div(row), gq = row - iq * G;
-      static_cast<T *>(a.out)[(((long)b * a.n_q + iq) * a.Hq + h * G + gq) * D + e] = (T)(o * st.y);
-      if (a.stats && e == 0) a.stats[(long)bh * a.R + row] = st;
+    float ref = j.ref;
+#pragma unroll
+    for (int u = 0; u < U; ++u) ref = fmaxf(ref, ml[u].x);          // (the last slice again and again is the same)
+    const float shrink = exp2_fast(j.ref - ref);
+    j.sum *= shrink, j.out *= shrink, j.ref = ref;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float by = s0 + u < a.slices ? exp2_fast(ml[u].x - ref) : 0.f;
+      if (s0 + u < a.slices) j.sum = fmaf(ml[u].y, by, j.sum);
+      if (OUT && s0 + u < a.slices) j.out = fmaf(o[u], by, j.out);
     }
   }
-  if (LOGITS) {
-    if (tid < a.R) stat[tid] = a.slices > 1 ? joined(tid) : a.stats[(long)bh * a.R + tid];
-    __syncthreads();
-    if (nq < 1) return;
-    for (int t = x * 1024 + tid; t < min(kv, x * 1024 + 1024); t += 256) {
-      float sum = 0.f;
-      for (int row = 0; row < a.R; ++row)
-        sum = fmaf(exp2_fast(fmaf(a.logits[((long)bh * a.R + row) * a.logits_ld + t], a.c, -stat[row].x)), stat[row].y, sum);
-      mass[(long)bh * a.N_cap + t] += sum;
+  return j;
+}
+
+template <typename T, bool LOGITS>
+__global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, int D, FastDiv by_chunks, FastDiv by_D) {
+  constexpr int SLOTS = 1024, U = SLOTS / 256;
+  __shared__ float2 stat[64];                              // (LOGITS: R <= 64)
+  const int bh = by_chunks.div(blockIdx.x), x = by_chunks.mod(blockIdx.x), tid = threadIdx.x;
+  const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, G = (int)a.by_group.d;
+  const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
+  float *m = mass + (long)bh * a.N_cap;
+  const float *logits = a.logits + (long)bh * a.R * a.logits_ld;
+  float before[U], first[U];
+  const bool slots = LOGITS && x * SLOTS < kv && nq > 0;
+  if (slots) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = min(x * SLOTS + u * 256 + tid, kv - 1);
+      before[u] = m[t];
+      first[u] = logits[t];
     }
+  }
+  if (a.slices > 1) {
+    const int mine = by_D.div(tid), row = x * by_D.div(256) + mine, e = tid - mine * D;
+    if (row < nq * G) {
+      const Joined j = join_row<true>(a, bh, row, D, e);
+      const float inv = inverse_of(j.sum);
+      const int iq = a.by_group.div(row), gq = row - iq * G;
+      static_cast<T *>(a.out)[(((long)b * a.n_q + iq) * a.Hq + h * G + gq) * D + e] = (T)(j.out * inv);
+      if (a.stats && e == 0) a.stats[(long)bh * a.R + row] = make_float2(j.ref, inv);
+    }
+  }
+  if (!slots) return;
+  if (tid < a.R) {
+    if (a.slices > 1) {
+      const Joined j = join_row<false>(a, bh, tid, D, 0);
+      stat[tid] = make_float2(j.ref, inverse_of(j.sum));
+    } else {
+      stat[tid] = a.stats[(long)bh * a.R + tid];
+    }
+  }
+  __syncthreads();
+  float sum[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) sum[u] = exp2_fast(fmaf(first[u], a.c, -stat[0].x)) * stat[0].y;
+  for (int row = 1; row < a.R; ++row) {
+    float s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) s[u] = logits[row * a.logits_ld + min(x * SLOTS + u * 256 + tid, kv - 1)];
+    const float2 st = stat[row];
+#pragma unroll
+    for (int u = 0; u < U; ++u) sum[u] = fmaf(exp2_fast(fmaf(s[u], a.c, -st.x)), st.y, sum[u]);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int t = x * SLOTS + u * 256 + tid;
+    if (t < kv) m[t] = before[u] + sum[u];
   }
 }
 
@@ -819,6 +885,8 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   a.q = c.q, a.K = c.K, a.V = c.V, a.k_tree = c.k_tree, a.v_tree = c.v_tree, a.out = c.out;
   a.visible = c.visible, a.q_len = c.q_len, a.kv_len = c.kv_len;
   a.n_q = c.n_q, a.R = c.n_q * c.group, a.Hq = d->H * c.group, a.N = d->N, a.N_cap = d->N_cap;
+  for (a.rows_p2 = 1; a.rows_p2 < a.R && a.rows_p2 < 16; a.rows_p2 *= 2) {
+  }
   a.nrb = p.nrb, a.slices = p.slices, a.total = (int)(BH * p.nrb * p.slices), a.per_xcd = div_up(a.total, 8);
   a.by_pair = ig_fast_div(p.nrb * p.slices), a.by_slices = ig_fast_div(p.slices);
   a.by_H = ig_fast_div(d->H), a.by_group = ig_fast_div(c.group);
@@ -881,17 +949,17 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   }
   if (p.slices > 1 || logits) {
     const int chunks = logits ? div_up(d->N, 1024) : 1;
-    const int rows = p.slices > 1 ? div_up((long)a.R * d->d, 256) : 1;
+    const int rows = p.slices > 1 ? div_up(a.R, 256 / d->d) : 1;
     const FastDiv by_chunks = ig_fast_div(chunks > rows ? chunks : rows);
     const dim3 jgrid((unsigned)(by_chunks.d * BH));
 #define JOIN(T)                                                                                      \
   {                                                                                                  \
     if (logits) {                                                                                    \
       auto k = attend_join<T, true>;                                                                 \
-      IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, c.mass, (int)d->d, by_chunks);                     \
+      IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, c.mass, (int)d->d, by_chunks, ig_fast_div(d->d));                     \
     } else {                                                                                         \
       auto k = attend_join<T, false>;                                                                \
-      IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, (float *)nullptr, (int)d->d, by_chunks);           \
+      IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, (float *)nullptr, (int)d->d, by_chunks, ig_fast_div(d->d));           \
     }                                                                                                \
   }
     if (d->dtype == IG_F16) JOIN(half_t) else JOIN(float)
