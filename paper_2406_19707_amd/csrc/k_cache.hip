@@ -78,7 +78,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   uint4 k[MT][KCH];
   unsigned v[VT][VW];
   // (tokens past the end are read from the last one: what they hold is never used, and is finite if that is)
-  auto load_k = [&](int tile) {
+  auto load_k = [&](int tile) __attribute__((always_inline)) {
     const bool drafted = TREE && tile >= cache_tiles;
     const T *base = drafted ? static_cast<const T *>(a.k_tree) + ((long)b * a.n_q * a.by_H.d + h) * D : Kc;
     const long stride = drafted ? (long)a.by_H.d * D : D;
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
       for (int c = 0; c < KCH; ++c) k[m][c] = src[c * 4 + g];
     }
   };
-  auto load_v = [&](int tile) {
+  auto load_v = [&](int tile) __attribute__((always_inline)) {
     const bool drafted = TREE && tile >= cache_tiles;
     const T *base = drafted ? static_cast<const T *>(a.v_tree) + ((long)b * a.n_q * a.by_H.d + h) * D : Vc;
     const long stride = drafted ? (long)a.by_H.d * D : D;
@@ -118,8 +118,9 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
     load_k(tile);
     load_v(tile);
   }
-  for (; tile < t_end; tile += 4) {
-    const bool more = tile + 4 < t_end;
+  // (`more` is known at compile time: the waits for a tile's values then leave the next one's keys in flight)
+  auto turn = [&](auto more_tiles) __attribute__((always_inline)) {
+    constexpr bool more = decltype(more_tiles)::value;
     floatx4 s[NT][MT];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -131,7 +132,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) s[n][m] = dot_step<T>(k[m][c], qf[n][c], s[n][m]);
-    if (more) load_k(tile + 4);
+    if constexpr (more) load_k(tile + 4);
 
     // masks, only where a tile holds something that some row does not see
     const bool drafted = TREE && tile >= cache_tiles;
@@ -223,8 +224,10 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
           for (int n = 0; n < NT; ++n)
             acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r][j]), s[n][0][r], acc[n][j], 0, 0, 0);
     }
-    if (more) load_v(tile + 4);
-  }
+    if constexpr (more) load_v(tile + 4);
+  };
+  for (; tile + 4 < t_end; tile += 4) turn(std::true_type());
+  if (tile < t_end) turn(std::false_type());
 
   // ---- the four waves' states joined: wave 0 ends up with that of the workgroup ----
 #pragma unroll
