@@ -10,7 +10,6 @@ struct StreamArgs {
   const uint64_t *visible;            // [B][n_q]
   const int32_t *q_len, *kv_len;      // [B], or NULL: n_q, N
   int n_q, R, Hq, N, N_cap;           // R = n_q * group query rows share a pool
-  int rows_p2;                        // R rounded up to a power of two, at most 16
   int nrb, slices, total, per_xcd;    // row blocks and slices of a pool, workgroups in all and of one XCD
   int paired;                         // attend_prompt: a workgroup takes two row blocks
   FastDiv by_pair, by_slices, by_H, by_group;

@@ -29,6 +29,10 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   constexpr int VW = CJ * (int)sizeof(T) / 4;             // words of a V row that a lane holds
   __shared__ __attribute__((aligned(16))) float box[RB * D];
   __shared__ float box_m[4][RB], box_l[4][RB];
+  // Logits of up to 16 rows wait in LDS, because a store before every tile's loads is one more thing that the wait for
+  // those waits for (one row, 160 pools of 32768: 490 us with stores after every tile, PLACE with them here, 441 without).
+  constexpr int LOGIT_BOX = LOGITS && NT == 1 ? 3072 : 4;
+  __shared__ __attribute__((aligned(16))) float box_s[4][LOGIT_BOX];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = lane & 15, g = lane >> 4;
 
@@ -48,14 +52,9 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   const T *q = static_cast<const T *>(a.q);
   uint4 qf[NT][KCH];
   int lim_min = 0x7fffffff, lim_max = 0;
-  // Kept logits, up to 16 rows: the columns that are left hold the rows again, and each copy keeps another tile's
-  // logits, so that they are stored once every `copies` tiles and by all lanes.  (One row, 32768 slots, 160 pools:
-  // stored after every tile by a sixteenth of the lanes they cost 48 of 490 us.)
-  const int rows_p2 = LOGITS && NT == 1 ? a.rows_p2 : 16, copies = 16 / rows_p2, copy = LOGITS && NT == 1 ? i / rows_p2 : 0;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    const int row = rb * RB + n * 16 + (LOGITS && NT == 1 ? i & (rows_p2 - 1) : i);
-    const int iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
+    const int row = rb * RB + n * 16 + i, iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
     live[n] = row < a.R && iq < nq;
     lim[n] = live[n] ? (TREE ? kv : max(0, kv - nq + iq + 1)) : 0x7fffffff;
     sees[n] = TREE && live[n] ? a.visible[(long)b * a.n_q + iq] & low_bits(nq) : 0;
@@ -111,8 +110,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
     for (int j = 0; j < CJ; ++j) acc[n][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
-  floatx4 kept[MT];
-  int count = 0;
+  int kept = 0;                                           // tiles in the wave's box of logits
   int tile = t_begin + w;
   if (tile < t_end) {
     load_k(tile);
@@ -155,17 +153,21 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
             if (t0 + 4 * m + r >= lim[n]) s[n][m][r] = -INFINITY;
     }
     if constexpr (LOGITS && NT == 1) {
-      const int at = count++ & (copies - 1);
+      if (live[0]) {
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) kept[m][r] = copy == at ? s[0][m][r] : kept[m][r];
-      if (at == copies - 1 || !more) {
-        if (live[0] && copy <= at) {
-          float *to = a.logits + ((long)bh * a.R + (i & (rows_p2 - 1))) * a.logits_ld + t0 - (at - copy) * 4 * TT;
-#pragma unroll
-          for (int m = 0; m < MT; ++m) *reinterpret_cast<floatx4 *>(to + 4 * m) = kept[m];
+        for (int m = 0; m < MT; ++m)
+          *reinterpret_cast<floatx4 *>(box_s[w] + (kept * a.R + i) * TT + VT * g + 4 * m) = s[0][m];
+      }
+      ++kept;
+      if (!more || (kept + 1) * a.R * TT > LOGIT_BOX) {
+        // (in the order the rows were written: R rows of a tile, then the wave's next tile)
+        for (int u = lane; u < kept * a.R * (TT / 4); u += 64) {
+          const int kr = u / (TT / 4), x = a.by_group.div(kr);       // (one query a sequence: R = group)
+          *reinterpret_cast<floatx4 *>(a.logits + ((long)bh * a.R + kr - x * a.R) * a.logits_ld +
+                                       (long)(tile - 4 * (kept - 1 - x)) * TT + u % (TT / 4) * 4) =
+              *reinterpret_cast<const floatx4 *>(box_s[w] + u * 4);
         }
+        kept = 0;
       }
     } else if constexpr (LOGITS) {
 #pragma unroll
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const int row = rb * RB + n * 16 + i;
-    if (!live[n] || copy) continue;
+    if (!live[n]) continue;
     const float inv = inverse_of(l_all[n]);
     if (a.slices == 1) {
       const int iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
@@ -888,8 +890,6 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   a.q = c.q, a.K = c.K, a.V = c.V, a.k_tree = c.k_tree, a.v_tree = c.v_tree, a.out = c.out;
   a.visible = c.visible, a.q_len = c.q_len, a.kv_len = c.kv_len;
   a.n_q = c.n_q, a.R = c.n_q * c.group, a.Hq = d->H * c.group, a.N = d->N, a.N_cap = d->N_cap;
-  for (a.rows_p2 = 1; a.rows_p2 < a.R && a.rows_p2 < 16; a.rows_p2 *= 2) {
-  }
   a.nrb = p.nrb, a.slices = p.slices, a.total = (int)(BH * p.nrb * p.slices), a.per_xcd = div_up(a.total, 8);
   a.by_pair = ig_fast_div(p.nrb * p.slices), a.by_slices = ig_fast_div(p.slices);
   a.by_H = ig_fast_div(d->H), a.by_group = ig_fast_div(c.group);
