@@ -168,7 +168,9 @@ __device__ __forceinline__ void load_to_lds(const void *from, unsigned offset, h
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(__builtin_amdgcn_readfirstlane(at)), "v"(offset),
                "s"((unsigned long long)hi << 32 | lo) : "memory");
 }
-__device__ __forceinline__ void wait_for_lds_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void wait_for_lds_loads() {      // all but the newest LEFT
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
+}
 
 // the other half wave's value and this one's: both in both
 __device__ __forceinline__ float both_max(float v) {

@@ -8,7 +8,7 @@
 namespace {
 
 // ---- few query rows, many cached rows ----------------------------------------------------------------
-// The R = n_q * group query rows that share a pool (b,h) are taken 16 NT at a time; the cached rows of a slice
+// The R = n_q * group query rows that share a pool (b,h) are taken 16 NT (16 or 32) at a time; the cached rows of a slice
 // are dealt to the four waves of a workgroup in tiles of 32 (float32: 16), and every wave keeps its own running
 // maximum, sum and output for all 16 NT rows until the waves' states are joined through LDS.
 //
@@ -310,11 +310,14 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
 // The reference of a row's weights only moves when its largest logit passes it by RISE (weights up to 2^RISE, far
 // inside half precision): the row's output, 16 registers for every 32 channels, is then scaled only now and then.
 constexpr float RISE = 6.f;
-constexpr int PROMPT_ROWS = 128, PROMPT_KEYS = 64;
+constexpr int PROMPT_KEYS = 64;
 
-template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void attend_prompt(StreamArgs a) {
-  constexpr int KS = D / 16, OB = D / 32, PC = D / 8, TK = PROMPT_KEYS;
-  __shared__ __attribute__((aligned(16))) half_t tiles[2][2][TK * D];
+template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void attend_prompt(StreamArgs a) {
+  constexpr int KS = D / 16, OB = D / 32, PC = D / 8, TK = PROMPT_KEYS, ROWS = NW * 32;
+  constexpr int SLOTS = NW == 8 ? 3 : 2, AHEAD = SLOTS - 1;      // tiles in LDS, and how many of them ahead of their use
+  constexpr int LOADS = PC / NW;                                  // of a wave, for a tile of K or of V
+  static_assert(LOADS >= 1, "every wave loads a part of a tile");
+  __shared__ __attribute__((aligned(16))) half_t tiles[SLOTS][2][TK * D];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = lane & 31, hb = lane >> 5;
   int work = xcd_order(blockIdx.x, a.per_xcd);
@@ -326,7 +329,7 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
   const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
 
   // what this lane fetches of every tile: this piece of this row first, then of 64 / PC rows further on, ..
-  const unsigned from_row = w * 16 + lane / PC, from_piece = (lane % PC) ^ piece_swap<D>(from_row);
+  const unsigned from_row = w * (64 / NW) + lane / PC, from_piece = (lane % PC) ^ piece_swap<D>(from_row);
   const unsigned k_base = row_base<D>(lane), v_base = column_base<D>(lane);
 
   // one row block; in a paired call the last with the first, the last but one with the second, ..
@@ -336,17 +339,17 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
       if (2 * unit >= a.nrb - 1) break;
       __syncthreads();                                    // the other waves are done with the tiles
     }
-    const int row = rb * PROMPT_ROWS + w * 32 + i, iq = a.by_group.div(row), gq = row - iq * G;
+    const int row = rb * ROWS + w * 32 + i, iq = a.by_group.div(row), gq = row - iq * G;
     const bool live = row < a.R && iq < nq;
     const int lim = live ? (TREE ? kv : max(0, kv - nq + iq + 1)) : 0x7fffffff;
     const unsigned long long sees = TREE && live ? a.visible[(long)b * a.n_q + iq] & low_bits(nq) : 0;
     const long row_at = (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * G + gq) * D;
     const int lim_min = wave_min_int(lim);
     // (what the row block's last live row sees)
-    const int last_row = min(min(a.R, nq * G), (rb + 1) * PROMPT_ROWS) - 1;
-    const int most = last_row < rb * PROMPT_ROWS ? 0 : (TREE ? kv : max(0, kv - nq + a.by_group.div(last_row) + 1));
+    const int last_row = min(min(a.R, nq * G), (rb + 1) * ROWS) - 1;
+    const int most = last_row < rb * ROWS ? 0 : (TREE ? kv : max(0, kv - nq + a.by_group.div(last_row) + 1));
     const int cache_tiles = (most + TK - 1) / TK;
-    const int tiles_all = cache_tiles + (TREE && last_row >= rb * PROMPT_ROWS ? (nq + TK - 1) / TK : 0);
+    const int tiles_all = cache_tiles + (TREE && last_row >= rb * ROWS ? (nq + TK - 1) / TK : 0);
     const int per = (tiles_all + a.slices - 1) / a.slices;
     const int t_begin = min(tiles_all, slice * per), t_end = min(tiles_all, t_begin + per);
 
@@ -356,9 +359,9 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
 #pragma unroll
       for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(half8, flip_sign<half_t>(src[2 * s + hb], a.flip));
     }
-    // tile `tile` of K or V into a slot of it
+    // tile `tile` of K or V into a slot (past the last one: the last one again, so that every turn has as many loads)
     auto fetch = [&](const void *pool, const void *nodes, int tile, half_t *to) __attribute__((always_inline)) {
-      if (tile >= t_end) return;
+      tile = min(tile, t_end - 1);
       const bool drafted = TREE && tile >= cache_tiles;
       const int stride = (drafted ? (int)a.by_H.d * D : D) * 2;
       const int t0 = (drafted ? tile - cache_tiles : tile) * TK, last = (drafted ? nq : kv) - 1 - t0;
@@ -366,10 +369,10 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
                                  : static_cast<const char *>(pool) + (long)bh * a.N_cap * D * 2;
       const unsigned r0 = opaque(from_row);
 #pragma unroll
-      for (int x = 0; x < PC / 4; ++x)       // (64 rows: offsets inside a tile fit 32 bits)
+      for (int x = 0; x < LOADS; ++x)       // (64 rows: offsets inside a tile fit 32 bits)
         load_to_lds(base + (long)t0 * stride,
                     (unsigned)(min((int)r0 + x * (64 / PC), last) * stride) + (from_piece ^ piece_swap<D>(x * (64 / PC))) * 16,
-                    to + (w * (PC / 4) + x) * 512);
+                    to + (w * LOADS + x) * 512);
     };
 
     floatx16 acc[OB];
@@ -472,36 +475,48 @@ template <int D, bool TREE> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) 
     };
     typedef std::true_type Y;
     typedef std::false_type N;
-    if (t_begin < t_end) {
-      half_t *const k0 = tiles[0][0], *const k1 = tiles[1][0], *const v0 = tiles[0][1], *const v1 = tiles[1][1];
-      fetch(a.K, a.k_tree, t_begin, k0);
-      wait_for_lds_loads();
-      __syncthreads();
-      fetch(a.K, a.k_tree, t_begin + 1, k1);
-      fetch(a.V, a.v_tree, t_begin, v0);
-      half_step(N(), Y(), N(), sB, 0, 0, pB, sA, k0, 0, pA, v0, 0);
-      half_step(Y(), Y(), N(), sA, t_begin, 0, pA, sB, k0, 32, pB, v0, 0);
-      // a turn: the logits of tile `tile`, the weights of its first and the last tile's second half, the last tile's output
-      auto turn_of = [&](int tile, half_t *k, half_t *v, half_t *k_free, half_t *v_free) __attribute__((always_inline)) {
-        wait_for_lds_loads();                             // these tiles are there ...
-        __syncthreads();                                  // ... in every wave's part, and the other slots are free
-        fetch(a.K, a.k_tree, tile + 1, k_free);
-        fetch(a.V, a.v_tree, tile, v_free);
-        half_step(Y(), Y(), Y(), sB, tile - 1, 1, pB, sA, k, 0, pA, v, 0);
-        half_step(Y(), Y(), Y(), sA, tile, 0, pA, sB, k, 32, pB, v, 32);
-      };
-      int tile = t_begin + 1;
-      for (; tile + 1 < t_end; tile += 2) {
-        turn_of(tile, k1, v0, k0, v1);
-        turn_of(tile + 1, k0, v1, k1, v0);
+    const int turns = t_end - t_begin;
+    if (turns > 0) {
+      fetch(a.K, a.k_tree, t_begin, tiles[0][0]);
+      if constexpr (AHEAD == 2) {
+        fetch(a.K, a.k_tree, t_begin + 1, tiles[1][0]);
+        fetch(a.V, a.v_tree, t_begin, tiles[0][1]);
       }
-      const bool odd = tile < t_end;
-      if (odd) turn_of(tile, k1, v0, k0, v1);
-      wait_for_lds_loads();
+      // Turn r: the logits of tile r, the weights of its first half and of the last tile's second half, the last tile's
+      // output.  Slots go round: tile r of K or V is in slot r % SLOTS.
+      auto begin_turn = [&](int r, auto slot) __attribute__((always_inline)) {
+        constexpr int S = decltype(slot)::value;
+        wait_for_lds_loads<(AHEAD - 1) * 2 * LOADS>();    // this turn's tiles are there ...
+        __syncthreads();                                  // ... in every wave's part, and the last turn's slots are free
+        fetch(a.K, a.k_tree, t_begin + r + AHEAD, tiles[(S + AHEAD) % SLOTS][0]);
+        fetch(a.V, a.v_tree, t_begin + r + AHEAD - 1, tiles[(S + AHEAD - 1) % SLOTS][1]);
+      };
+      auto turn_of = [&](int r, auto slot) __attribute__((always_inline)) {
+        constexpr int S = decltype(slot)::value;
+        begin_turn(r, slot);
+        const half_t *K = tiles[S][0], *V = tiles[(S + SLOTS - 1) % SLOTS][1];
+        half_step(Y(), Y(), Y(), sB, t_begin + r - 1, 1, pB, sA, K, 0, pA, V, 0);
+        half_step(Y(), Y(), Y(), sA, t_begin + r, 0, pA, sB, K, 32, pB, V, 32);
+      };
+      begin_turn(0, std::integral_constant<int, 0>());
+      half_step(N(), Y(), N(), sB, 0, 0, pB, sA, tiles[0][0], 0, pA, tiles[0][1], 0);
+      half_step(Y(), Y(), N(), sA, t_begin, 0, pA, sB, tiles[0][0], 32, pB, tiles[0][1], 0);
+      typedef std::integral_constant<int, 1> S1;
+      typedef std::integral_constant<int, 2 % SLOTS> S2;
+      typedef std::integral_constant<int, 0> S0;
+      int r = 1;
+      for (; r + SLOTS - 1 < turns; r += SLOTS) {
+        turn_of(r, S1());
+        turn_of(r + 1, S2());
+        if constexpr (SLOTS == 3) turn_of(r + 2, S0());
+      }
+      if (r < turns) turn_of(r, S1());
+      if (SLOTS == 3 && r + 1 < turns) turn_of(r + 1, S2());
+      wait_for_lds_loads<0>();
       __syncthreads();
-      const half_t *v = odd ? v1 : v0;
-      half_step(Y(), N(), Y(), sB, t_end - 1, 1, pB, sA, k0, 0, pA, v, 0);
-      half_step(N(), N(), Y(), sA, 0, 0, pA, sB, k0, 0, pB, v, 32);
+      const half_t *V = tiles[(turns - 1) % SLOTS][1];
+      half_step(Y(), N(), Y(), sB, t_end - 1, 1, pB, sA, V, 0, pA, V, 0);
+      half_step(N(), N(), Y(), sA, 0, 0, pA, sB, V, 0, pB, V, 32);
     }
 
     if (!live) continue;
@@ -570,7 +585,7 @@ template <bool OUT> __device__ __forceinline__ Joined join_row(const StreamArgs 
 template <typename T, bool LOGITS>
 __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, int D, FastDiv by_chunks, FastDiv by_D) {
   constexpr int SLOTS = 1024, U = SLOTS / 256;
-  __shared__ float2 stat[64];                              // (LOGITS: R <= 64)
+  __shared__ float2 stat[32];                              // (LOGITS: R <= 32)
   const int bh = by_chunks.div(blockIdx.x), x = by_chunks.mod(blockIdx.x), tid = threadIdx.x;
   const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, G = (int)a.by_group.d;
   const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
@@ -625,65 +640,73 @@ __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, in
 }
 
 // ---- the weights of many query rows ------------------------------------------------------------------
-// A wave keeps 32 (float32: 16) cached keys as the rows of S^T = K Q^T and takes every query row that sees
-// them: mass[t] += sum over rows of exp2(c s - c m) / l, with the rows' final maxima and sums.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void attend_mass(StreamArgs a, float *mass, FastDiv by_chunks) {
-  constexpr bool HALF = sizeof(T) == 2;
-  constexpr int TT = HALF ? 32 : 16, MT = TT / 16, KCH = D * (int)sizeof(T) / 64, VT = HALF ? 8 : 4;
+// Float32: a workgroup keeps 32 cached keys (d = 256: 16) as the rows of S^T = K Q^T; its waves take turns at the
+// query rows that see them, 16 at a time with the next 16 asked for: mass[t] += sum over rows of
+// exp2(c s - ref) / sum, with the rows' final references and sums.
+template <int D> constexpr int mass_keys() { return D <= 128 ? 32 : 16; }
+template <int D> __global__ __launch_bounds__(256) void attend_mass(StreamArgs a, float *mass, FastDiv by_chunks) {
+  constexpr int MT = mass_keys<D>() / 16, KCH = D / 16;
+  __shared__ float part[4][mass_keys<D>()];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = lane & 15, g = lane >> 4;
   const int bh = by_chunks.div(blockIdx.x), x = by_chunks.mod(blockIdx.x);
   const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, G = (int)a.by_group.d;
   const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
-  const int t0 = (x * 4 + w) * TT;
+  const int t0 = x * mass_keys<D>();
   if (t0 >= kv) return;
-  const T *Kc = static_cast<const T *>(a.K) + (long)bh * a.N_cap * D;
-  uint4 k[MT][KCH];
+  const float *Kc = static_cast<const float *>(a.K) + (long)bh * a.N_cap * D;
+  uint4 k[MT][KCH], q[KCH];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    const int t = min(t0 + (HALF ? 8 * (i >> 2) + 4 * m + (i & 3) : i), kv - 1);
+    const uint4 *src = reinterpret_cast<const uint4 *>(Kc + (long)min(t0 + m * 16 + i, kv - 1) * D);
 #pragma unroll
-    for (int c = 0; c < KCH; ++c) k[m][c] = reinterpret_cast<const uint4 *>(Kc + (long)t * D)[c * 4 + g];
+    for (int c = 0; c < KCH; ++c) k[m][c] = flip_sign<float>(src[c * 4 + g], a.flip);
   }
   float sum[MT][4] = {};
   // the first query that sees slot t0 is number t0 - (kv - nq)
   const int rows = nq * G, first = max(0, t0 - (kv - nq)) * G;
-  for (int r0 = first; r0 < rows; r0 += 16) {
-    const int row = min(r0 + i, rows - 1), iq = a.by_group.div(row), gq = row - iq * G;
-    const bool live = r0 + i < rows;
-    const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const T *>(a.q) + (((long)b * a.n_q + iq) * a.Hq + h * G + gq) * D);
-    const float2 st = a.stats[(long)bh * a.R + row];
-    const float ref = st.x, inv = live ? st.y : 0.f;
-    const int lim = kv - nq + iq + 1;
+  float2 st;
+  int iq;
+  auto ask = [&](int r0) __attribute__((always_inline)) {
+    const int row = min(r0 + i, rows - 1);
+    iq = a.by_group.div(row);
+    const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const float *>(a.q) + (((long)b * a.n_q + iq) * a.Hq + h * G + row - iq * G) * D);
+#pragma unroll
+    for (int c = 0; c < KCH; ++c) q[c] = src[c * 4 + g];
+    st = a.stats[(long)bh * a.R + row];
+  };
+  int r0 = first + 16 * w;
+  if (r0 < rows) ask(r0);
+  for (; r0 < rows; r0 += 64) {
     floatx4 s[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) s[m] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < KCH; ++c) {
-      const uint4 qf = flip_sign<T>(src[c * 4 + g], a.flip);
+    for (int c = 0; c < KCH; ++c)
 #pragma unroll
-      for (int m = 0; m < MT; ++m) s[m] = dot_step<T>(k[m][c], qf, s[m]);
-    }
+      for (int m = 0; m < MT; ++m) s[m] = dot_step<float>(k[m][c], q[c], s[m]);
+    const float ref = st.x, inv = st.y;
+    const int lim = r0 + i < rows ? kv - nq + iq + 1 : 0;
+    if (r0 + 64 < rows) ask(r0 + 64);
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float p = exp2_fast(fmaf(s[m][r], a.c, -ref));
-        sum[m][r] += live && t0 + VT * g + 4 * m + r < lim ? p * inv : 0.f;
-      }
+      for (int r = 0; r < 4; ++r)
+        if (t0 + m * 16 + 4 * g + r < lim) sum[m][r] = fmaf(exp2_fast(fmaf(s[m][r], a.c, -ref)), inv, sum[m][r]);
   }
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const float all = row16_sum(sum[m][r]);
-      const int t = t0 + VT * g + 4 * m + r;
-      if (i == 0 && t < kv) mass[(long)bh * a.N_cap + t] += all;
+      if (i == 0) part[w][m * 16 + 4 * g + r] = all;
     }
+  __syncthreads();
+  const int e = threadIdx.x;
+  if (e < mass_keys<D>() && t0 + e < kv) mass[(long)bh * a.N_cap + t0 + e] += (part[0][e] + part[1][e]) + (part[2][e] + part[3][e]);
 }
 
-// The same in half precision for calls of many rows: a wave keeps 64 keys, a workgroup 256, and the query rows
+// Half precision: a wave keeps 64 keys, a workgroup 256, and the query rows
 // come through LDS 64 at a time, one tile ahead.  As in attend_prompt it is a pipeline: while the weights of 32 rows
 // and 32 keys are worked out (an exponential and two fused multiply-adds a pair), the matrix units take the next
 // logits.
@@ -785,7 +808,7 @@ template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt
     if (tiles_n > 0) {
       fetch(0, tiles[0]);
       ask(0);
-      wait_for_lds_loads();
+      wait_for_lds_loads<0>();
       __syncthreads();
       Row rA = row_of(0, 0, st[0]), rB = row_of(0, 1, st[1]);
       auto turn_of = [&](auto has_last, int tile, half_t *q, half_t *q_free) __attribute__((always_inline)) {
@@ -800,7 +823,7 @@ template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt
         step(Y(), Y(), sA, rB, 0, sB, 1);
       };
       auto next_tile = [&]() __attribute__((always_inline)) {
-        wait_for_lds_loads();                             // the tile is there ...
+        wait_for_lds_loads<0>();                             // the tile is there ...
         __syncthreads();                                  // ... in every wave's part, and the other slot is free
         st_now[0] = st[0], st_now[1] = st[1];
       };
@@ -835,21 +858,29 @@ template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt
 
 int div_up(long n, long d) { return (int)((n + d - 1) / d); }
 
-// query rows a workgroup takes: 16, 32 or 64, what fits the registers beside the row's output
-int row_block(const ig_desc *d, long R) {
-  const int most = d->d > 128 ? 32 : 64;
-  return R <= 16 ? 16 : (R <= 32 || most == 32 ? 32 : 64);
+// Query rows a workgroup of attend_stream takes: 16 or 32.  (With 64 the registers run out: float32, 1024 rows over as
+// many, 121 us with 32 and 163 us with 64.)  In half precision attend_prompt takes over from there: trees of 32 to 64 nodes
+// over 4096, 128 pools, 66 to 67 us there, 101 to 105 us here; of 32 nodes and fewer the same in both.
+int row_block(long R) { return R <= 16 ? 16 : 32; }
+
+// The same for attend_prompt.  Eight waves, two tiles ahead, where most of what the rows see is seen by all of them and
+// there are rows for more than four (317 x 4 query rows over up to 9001: 225 against 235 us, trees of 63 x 4 nodes over 8191: 97
+// against 106); four for prompts, where a block of 256 rows works out more that its first rows do not see (2048 over 2048:
+// 397 against 367 us).
+int prompt_rows(const ig_desc *d, const CacheCall &c) {
+  return d->d >= 64 && d->d <= 128 && (long)c.n_q * c.group > 128 && (c.k_tree || 2 * (long)c.n_q <= d->N) ? 256 : 128;
 }
 
 // Slices the cached rows of a pool are cut into: the number for which the last workgroups end first, if a turn (64
 // rows of attend_prompt, four waves' tiles of attend_stream) takes a unit of time, a workgroup two more to start and
-// to leave its state, and two workgroups fit a compute unit.  (Four sequences of up to 9001 with 1268 query rows for
+// to leave its state, and a compute unit holds eight waves.  (Four sequences of up to 9001 with 1268 query rows for
 // each of 8 pools: 3 slices of 320 row blocks 1.5 times as fast as 2, which leave the second round a quarter full.)
-int slices_of(const ig_desc *d, bool prompt, long nrb, int n_keys) {
-  const long groups = d->B * (long)d->H * nrb, turns = div_up(n_keys, prompt ? 64 : (d->dtype == IG_F16 ? 128 : 64));
+int slices_of(const ig_desc *d, int prompt_rows, long nrb, int n_keys) {
+  const long groups = d->B * (long)d->H * nrb, slots = prompt_rows == 256 ? 256 : 512;
+  const long turns = div_up(n_keys, prompt_rows ? 64 : (d->dtype == IG_F16 ? 128 : 64));
   long best = 1, best_cost = -1;
   for (long s = 1; s <= 64 && s <= turns; ++s) {
-    const long cost = div_up(groups * s, 512) * (div_up(turns, s) + 2);
+    const long cost = div_up(groups * s, slots) * (div_up(turns, s) + 2);
     if (best_cost < 0 || cost < best_cost) best = s, best_cost = cost;
   }
   return (int)best;
@@ -859,15 +890,15 @@ int slices_of(const ig_desc *d, bool prompt, long nrb, int n_keys) {
 
 // Whether the logits of a call are kept for the weights (one query a sequence) instead of being worked out
 // again from the keys.
-static bool keeps_logits(const CacheCall &c) { return c.mass && c.n_q == 1 && c.group <= 64; }
+static bool keeps_logits(const CacheCall &c) { return c.mass && c.n_q == 1 && c.group <= 32; }
 
 CachePlan ig_cache_plan(const ig_desc *d, const CacheCall &c) {
   CachePlan p;
   const long R = (long)c.n_q * c.group, BH = (long)d->B * d->H;
-  p.prompt = d->dtype == IG_F16 && R > 64;
-  p.rb = p.prompt ? PROMPT_ROWS : row_block(d, R);
+  p.prompt = d->dtype == IG_F16 && R > 32;
+  p.rb = p.prompt ? prompt_rows(d, c) : row_block(R);
   p.nrb = div_up(R, p.rb);
-  p.slices = slices_of(d, p.prompt, p.nrb, d->N + (c.k_tree ? c.n_q : 0));
+  p.slices = slices_of(d, p.prompt ? p.rb : 0, p.nrb, d->N + (c.k_tree ? c.n_q : 0));
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -901,7 +932,7 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   a.logits = reinterpret_cast<float *>(ws + p.logits_at);
   a.logits_ld = p.logits_ld;
   // a causal call with workgroups to spare: each takes a late and an early row block, so that all take equally long
-  a.paired = p.prompt && !tree && p.slices == 1 && BH * p.nrb >= 1024 && 2 * c.n_q > d->N;
+  a.paired = p.prompt && !tree && p.slices == 1 && BH * p.nrb >= (p.rb == 256 ? 512 : 1024) && 2 * c.n_q > d->N;
   if (a.paired) {
     const int units = (p.nrb + 1) / 2;
     a.total = (int)(BH * units), a.per_xcd = div_up(a.total, 8), a.by_pair = ig_fast_div(units);
@@ -923,8 +954,7 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
 #define STREAM_ROWS(T, D)                                                                            \
   {                                                                                                  \
     if (p.rb == 16) STREAM(T, D, 1)                                                                  \
-    else if (p.rb == 32) STREAM(T, D, 2)                                                             \
-    else if constexpr (D <= 128) STREAM(T, D, 4)                                                     \
+    else STREAM(T, D, 2)                                                                             \
   }
 #define BY_DIM(T, DO)                                                                                \
   switch (d->d) {                                                                                    \
@@ -933,15 +963,23 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
     case 128: DO(T, 128) break;                                                                      \
     default: DO(T, 256) break;                                                                       \
   }
-#define PROMPT(T, D)                                                                                 \
+#define PROMPT_WAVES(D, NW)                                                                           \
   {                                                                                                  \
     if (tree) {                                                                                      \
-      auto k = attend_prompt<D, true>;                                                               \
-      IG_LAUNCH(ctx, IG_K_CACHE, k, grid, block, stream, a);                                         \
+      auto k = attend_prompt<D, NW, true>;                                                           \
+      IG_LAUNCH(ctx, IG_K_CACHE, k, grid, dim3(NW * 64), stream, a);                                 \
     } else {                                                                                         \
-      auto k = attend_prompt<D, false>;                                                              \
-      IG_LAUNCH(ctx, IG_K_CACHE, k, grid, block, stream, a);                                         \
+      auto k = attend_prompt<D, NW, false>;                                                          \
+      IG_LAUNCH(ctx, IG_K_CACHE, k, grid, dim3(NW * 64), stream, a);                                 \
     }                                                                                                \
+  }
+#define PROMPT(T, D)                                                                                 \
+  {                                                                                                  \
+    if constexpr (D == 64 || D == 128) {                                                             \
+      if (p.rb == 256) PROMPT_WAVES(D, 8)                                                            \
+      else PROMPT_WAVES(D, 4)                                                                        \
+    } else                                                                                           \
+      PROMPT_WAVES(D, 4)                                                                             \
   }
   if (p.prompt) {
     BY_DIM(half_t, PROMPT)
@@ -967,7 +1005,7 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   }
     if (d->dtype == IG_F16) JOIN(half_t) else JOIN(float)
   }
-  if (c.mass && !logits && p.prompt) {
+  if (c.mass && !logits && d->dtype == IG_F16) {
     // keys in pairs of blocks as the rows above: a prompt's first keys are seen by all of its rows, its last by few
     a.nrb = div_up(d->N, MASS_KEYS);
     a.paired = BH * a.nrb >= 1024 && 2 * c.n_q > d->N;
@@ -982,19 +1020,13 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   }
     BY_DIM(half_t, PROMPT_MASS)
   } else if (c.mass && !logits) {
-    const int tile = d->dtype == IG_F16 ? 32 : 16;
-    const FastDiv by_chunks = ig_fast_div(div_up(d->N, 4 * tile));
-    const dim3 mgrid((unsigned)(by_chunks.d * BH));
 #define MASS(T, D)                                                                                   \
   {                                                                                                  \
-    auto k = attend_mass<T, D>;                                                                      \
-    IG_LAUNCH(ctx, IG_K_CACHE, k, mgrid, block, stream, a, c.mass, by_chunks);                                  \
+    const FastDiv by_chunks = ig_fast_div(div_up(d->N, mass_keys<D>()));                             \
+    auto k = attend_mass<D>;                                                                         \
+    IG_LAUNCH(ctx, IG_K_CACHE, k, dim3((unsigned)(by_chunks.d * BH)), block, stream, a, c.mass, by_chunks);\
   }
-    if (d->dtype == IG_F16) {
-      BY_DIM(half_t, MASS)
-    } else {
-      BY_DIM(float, MASS)
-    }
+    BY_DIM(float, MASS)
   }
   return IG_OK;
 }
