@@ -27,12 +27,12 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   constexpr int KCH = D * (int)sizeof(T) / 64;            // 16-byte pieces of a row that a lane holds
   constexpr int VT = HALF ? 8 : 4;                        // tokens of a tile that a lane group supplies
   constexpr int VW = CJ * (int)sizeof(T) / 4;             // words of a V row that a lane holds
-  __shared__ __attribute__((aligned(16))) float box[RB * D];
+  // A wave's part of LDS: its outputs at the end (rows of D floats and 16 bytes that set their banks apart), until then
+  // logits of up to 16 rows, which wait here because a store before every tile's loads is one more thing that the wait
+  // for those waits for (one row, 160 pools of 32768: 501 us in all with stores after every tile, 482 so, 436 without).
+  constexpr int LDB = D + 4, LOGIT_BOX = LOGITS && NT == 1 ? 3072 : 0, BOX = RB * LDB > LOGIT_BOX ? RB * LDB : LOGIT_BOX;
+  __shared__ __attribute__((aligned(16))) float boxes[4][BOX];
   __shared__ float box_m[4][RB], box_l[4][RB];
-  // Logits of up to 16 rows wait in LDS, because a store before every tile's loads is one more thing that the wait for
-  // those waits for (one row, 160 pools of 32768: 490 us with stores after every tile, PLACE with them here, 441 without).
-  constexpr int LOGIT_BOX = LOGITS && NT == 1 ? 3072 : 4;
-  __shared__ __attribute__((aligned(16))) float box_s[4][LOGIT_BOX];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i = lane & 15, g = lane >> 4;
 
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
       if (live[0]) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
-          *reinterpret_cast<floatx4 *>(box_s[w] + (kept * a.R + i) * TT + VT * g + 4 * m) = s[0][m];
+          *reinterpret_cast<floatx4 *>(boxes[w] + (kept * a.R + i) * TT + VT * g + 4 * m) = s[0][m];
       }
       ++kept;
       if (!more || (kept + 1) * a.R * TT > LOGIT_BOX) {
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
           const int kr = u / (TT / 4), x = a.by_group.div(kr);       // (one query a sequence: R = group)
           *reinterpret_cast<floatx4 *>(a.logits + ((long)bh * a.R + kr - x * a.R) * a.logits_ld +
                                        (long)(tile - 4 * (kept - 1 - x)) * TT + u % (TT / 4) * 4) =
-              *reinterpret_cast<const floatx4 *>(box_s[w] + u * 4);
+              *reinterpret_cast<const floatx4 *>(boxes[w] + u * 4);
         }
         kept = 0;
       }
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   for (; tile + 4 < t_end; tile += 4) turn(std::true_type());
   if (tile < t_end) turn(std::false_type());
 
-  // ---- the four waves' states joined: wave 0 ends up with that of the workgroup ----
+  // ---- the four waves' states joined, and rows out: finished ones to `out`, the states of a slice to the workspace ----
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     l_run[n] += __shfl_xor(l_run[n], 16, 64);
@@ -240,63 +240,39 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
       box_m[w][n * 16 + i] = m_run[n];
       box_l[w][n * 16 + i] = l_run[n];
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float o[CJ];
+#pragma unroll
+      for (int j = 0; j < CJ; ++j) o[j] = acc[n][j][r];
+      store_words<CJ>(boxes[w] + (n * 16 + i) * LDB + (4 * g + r) * CJ, o);
+    }
   }
   __syncthreads();
-  float m_all[NT], l_all[NT];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int at = n * 16 + i;
+  for (int u = threadIdx.x; u < RB * (D / 4); u += 256) {
+    const int at = u / (D / 4), e = u % (D / 4) * 4, row = rb * RB + at;
+    const int iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
+    if (row >= a.R || iq >= nq) continue;
     const float m = fmaxf(fmaxf(box_m[0][at], box_m[1][at]), fmaxf(box_m[2][at], box_m[3][at]));
-    m_all[n] = m;
-    l_all[n] = 0.f;
+    float l = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < 4; ++x) l_all[n] += box_l[x][at] * exp2_fast(box_m[x][at] - m);
-    const float shrink = exp2_fast(m_run[n] - m);
-#pragma unroll
-    for (int j = 0; j < CJ; ++j) acc[n][j] *= shrink;
-  }
-  for (int x = 3; x >= 1; --x) {
-    if (w == x) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < CJ; ++j) *reinterpret_cast<floatx4 *>(box + ((n * CJ + j) * 64 + lane) * 4) = acc[n][j];
+    for (int x = 0; x < 4; ++x) {
+      const float by = exp2_fast(box_m[x][at] - m);
+      l = fmaf(box_l[x][at], by, l);
+      o += *reinterpret_cast<const floatx4 *>(boxes[x] + at * LDB + e) * by;
     }
-    __syncthreads();
-    if (w == 0) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < CJ; ++j) acc[n][j] += *reinterpret_cast<const floatx4 *>(box + ((n * CJ + j) * 64 + lane) * 4);
-    }
-    __syncthreads();
-  }
-  if (w) return;
-
-  // ---- rows out: finished ones to `out`, the states of a slice to the workspace ----
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int row = rb * RB + n * 16 + i;
-    if (!live[n]) continue;
-    const float inv = inverse_of(l_all[n]);
     if (a.slices == 1) {
-      const int iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
-      T *to = static_cast<T *>(a.out) + (((long)b * a.n_q + iq) * a.Hq + h * (int)a.by_group.d + gq) * D;
+      const float inv = inverse_of(l);
+      T v[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        T o[CJ];
-#pragma unroll
-        for (int j = 0; j < CJ; ++j) o[j] = (T)(acc[n][j][r] * inv);
-        store_words<VW>(to + (4 * g + r) * CJ, o);
-      }
-      if (g == 0 && a.stats) a.stats[(long)bh * a.R + row] = make_float2(m_all[n], inv);
+      for (int x = 0; x < 4; ++x) v[x] = (T)(o[x] * inv);
+      store_words<(int)sizeof(T)>(static_cast<T *>(a.out) + (((long)b * a.n_q + iq) * a.Hq + h * (int)a.by_group.d + gq) * D + e, v);
+      if (e == 0 && a.stats) a.stats[(long)bh * a.R + row] = make_float2(m, inv);
     } else {
-      const long at = ((long)bh * a.slices + slice) * a.R + row;
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int j = 0; j < CJ; ++j) a.part[at * D + (4 * g + r) * CJ + j] = acc[n][j][r];
-      if (g == 0) a.part_ml[at] = make_float2(m_all[n], l_all[n]);
+      const long to = ((long)bh * a.slices + slice) * a.R + row;
+      *reinterpret_cast<floatx4 *>(a.part + to * D + e) = o;
+      if (e == 0) a.part_ml[to] = make_float2(m, l);
     }
   }
 }
@@ -861,7 +837,9 @@ int div_up(long n, long d) { return (int)((n + d - 1) / d); }
 // Query rows a workgroup of attend_stream takes: 16 or 32.  (With 64 the registers run out: float32, 1024 rows over as
 // many, 121 us with 32 and 163 us with 64.)  In half precision attend_prompt takes over from there: trees of 32 to 64 nodes
 // over 4096, 128 pools, 66 to 67 us there, 101 to 105 us here; of 32 nodes and fewer the same in both.
-int row_block(long R) { return R <= 16 ? 16 : 32; }
+// (d = 256: 16 here, and from 17 rows on in half precision there.)
+int row_block(const ig_desc *d, long R) { return R <= 16 || d->d > 128 ? 16 : 32; }
+bool many_rows(const ig_desc *d, long R) { return d->dtype == IG_F16 && R > (d->d > 128 ? 16 : 32); }
 
 // The same for attend_prompt.  Eight waves, two tiles ahead, where most of what the rows see is seen by all of them and
 // there are rows for more than four (317 x 4 query rows over up to 9001: 225 against 235 us, trees of 63 x 4 nodes over 8191: 97
@@ -890,13 +868,13 @@ int slices_of(const ig_desc *d, int prompt_rows, long nrb, int n_keys) {
 
 // Whether the logits of a call are kept for the weights (one query a sequence) instead of being worked out
 // again from the keys.
-static bool keeps_logits(const CacheCall &c) { return c.mass && c.n_q == 1 && c.group <= 32; }
+static bool keeps_logits(const CacheCall &c, const CachePlan &p) { return c.mass && c.n_q == 1 && p.nrb == 1 && !p.prompt; }
 
 CachePlan ig_cache_plan(const ig_desc *d, const CacheCall &c) {
   CachePlan p;
   const long R = (long)c.n_q * c.group, BH = (long)d->B * d->H;
-  p.prompt = d->dtype == IG_F16 && R > 32;
-  p.rb = p.prompt ? prompt_rows(d, c) : row_block(R);
+  p.prompt = many_rows(d, R);
+  p.rb = p.prompt ? prompt_rows(d, c) : row_block(d, R);
   p.nrb = div_up(R, p.rb);
   p.slices = slices_of(d, p.prompt ? p.rb : 0, p.nrb, d->N + (c.k_tree ? c.n_q : 0));
   size_t at = 0;
@@ -909,13 +887,13 @@ CachePlan ig_cache_plan(const ig_desc *d, const CacheCall &c) {
   p.stats_at = take(c.mass ? BH * R * sizeof(float2) : 0);
   p.part_ml_at = take(p.slices > 1 ? BH * p.slices * R * sizeof(float2) : 0);
   p.part_at = take(p.slices > 1 ? BH * p.slices * R * d->d * sizeof(float) : 0);
-  p.logits_at = take(keeps_logits(c) ? BH * R * p.logits_ld * sizeof(float) : 0);
+  p.logits_at = take(keeps_logits(c, p) ? BH * R * p.logits_ld * sizeof(float) : 0);
   p.bytes = at;
   return p;
 }
 
 int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const CachePlan &p, char *ws, hipStream_t stream) {
-  const bool tree = c.k_tree != nullptr, logits = keeps_logits(c);
+  const bool tree = c.k_tree != nullptr, logits = keeps_logits(c, p);
   const long BH = (long)d->B * d->H;
   StreamArgs a = {};
   a.q = c.q, a.K = c.K, a.V = c.V, a.k_tree = c.k_tree, a.v_tree = c.v_tree, a.out = c.out;
@@ -954,7 +932,7 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
 #define STREAM_ROWS(T, D)                                                                            \
   {                                                                                                  \
     if (p.rb == 16) STREAM(T, D, 1)                                                                  \
-    else STREAM(T, D, 2)                                                                             \
+    else if constexpr (D <= 128) STREAM(T, D, 2)                                                     \
   }
 #define BY_DIM(T, DO)                                                                                \
   switch (d->d) {                                                                                    \

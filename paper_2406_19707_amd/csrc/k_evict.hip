@@ -73,7 +73,7 @@ template <typename T, int THREADS, int KPT, bool MOVE>
 __global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a) {
   constexpr int NW = THREADS / 64, U = KPT > 0 ? KPT : 8;
   __shared__ __attribute__((aligned(16))) unsigned hist[3][RADIX_WORDS];
-  __shared__ int w_eq[NW], w_src[NW], w_dst[NW];
+  __shared__ int w_safe[NW], w_eq[NW], w_src[NW], w_dst[NW];
   const int bh = blockIdx.x, b = a.by_H.div(bh), tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = length_of(a.kv_len, b, a.N, a.N_cap);
@@ -114,15 +114,28 @@ __global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a) {
   };
   if constexpr (KPT > 0) load(t0);
   for (int i = tid; i < 3 * RADIX_WORDS / 4; i += THREADS) reinterpret_cast<uint4 *>(&hist[0][0])[i] = make_uint4(0, 0, 0, 0);
+  // The protected slots, which all have one key, are counted by ballots and left out of the histograms, where whole
+  // waves of them would add to one word.
+  int safe = 0;
+  each([&](int, unsigned k, bool there) { safe += __popcll(__ballot(there && k == ~0u)); });
+  if (lane == 0) w_safe[w] = safe;
   __syncthreads();
+  safe = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) safe += w_safe[i];
 
   // slots with a key above lim stay, and the first `need` of those equal to it
   unsigned lim = 0;
-  int need = a.keep;
+  int need = a.keep - safe;
+  if (need <= 0) {                                        // (no room for others: the first `keep` of the protected)
+    lim = ~0u;
+    need = a.keep;
+  }
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
+    if (lim == ~0u && pass == 0) break;
     each([&](int, unsigned k, bool there) {
-      if (there) radix_add(hist[pass], pass, k, lim);
+      if (there && k != ~0u) radix_add(hist[pass], pass, k, lim);
     });
     __syncthreads();
     bool whole;
@@ -183,6 +196,72 @@ __global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a) {
     if (born) born[t] = born[s];
   }
   if constexpr (MOVE) move_rows<T, THREADS>(a, bh, from, to, 0, total);
+}
+
+// The eviction of a decode step, one slot too many (N = keep + 1): the slot with the smallest key, the highest of
+// equal ones, makes room for the last slot.  Bound by the trips through memory: the last slot's rows, weight and
+// position are asked for with the weights.
+template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void evict_one(EvictArgs a) {
+  constexpr int NW = THREADS / 64, U = 8, TILE = IG_WAVE * SlabElem<T>::TPL;
+  __shared__ unsigned w_key[NW];
+  __shared__ int w_slot[NW];
+  const int bh = blockIdx.x, b = a.by_H.div(bh), tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int n = length_of(a.kv_len, b, a.N, a.N_cap), last = a.keep;
+  float *mass = a.mass + (long)bh * a.N_cap;
+  int32_t *born = a.born ? a.born + (long)bh * a.N_cap : nullptr;
+  const int guard = a.protect_from ? a.protect_from[b] : 0;
+  u32x4 *K = static_cast<u32x4 *>(a.K) + (long)bh * a.N_cap * a.units, *V = static_cast<u32x4 *>(a.V) + (long)bh * a.N_cap * a.units;
+  const bool copies = tid < a.units;               // (the host: a row has at most 256 units)
+  u32x4 kv = {}, vv = {};
+  if (copies) {                                    // (slot `keep` is inside the pool: N_cap >= N > keep)
+    kv = K[(long)last * a.units + tid];
+    vv = V[(long)last * a.units + tid];
+  }
+  const float last_mass = mass[last];
+  const int last_born = born ? born[last] : 0;
+  unsigned best = ~0u;
+  int slot = -1;
+  for (int t0 = tid; t0 < a.N; t0 += THREADS * U) {
+    float m[U];
+    int age[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) m[i] = mass[min(t0 + i * THREADS, last)];
+    if (a.protect_from) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) age[i] = born[min(t0 + i * THREADS, last)];
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int t = t0 + i * THREADS;
+      const unsigned key = a.protect_from && age[i] >= guard ? ~0u : weight_key(m[i]);
+      if (t <= last && key <= best) best = key, slot = t;           // (a thread's slots come in ascending order)
+    }
+  }
+  auto lower = [&](unsigned key, int s) {
+    if (key < best || (key == best && s > slot)) best = key, slot = s;
+  };
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) lower(__shfl_xor(best, o, 64), __shfl_xor(slot, o, 64));
+  if (lane == 0) w_key[w] = best, w_slot[w] = slot;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NW; ++i) lower(w_key[i], w_slot[i]);
+  if (n <= a.keep || slot == last) return;         // nothing too many, or the last slot itself goes
+  if (copies) {
+    K[(long)slot * a.units + tid] = kv;
+    V[(long)slot * a.units + tid] = vv;
+  }
+  if (tid == 0) {
+    mass[slot] = last_mass;
+    if (born) born[slot] = last_born;
+  }
+  if (a.slab) {
+    const int h = a.by_H.mod(bh);
+    T *slab = static_cast<T *>(a.slab) + (long)bh * a.nTiles * a.r * TILE;
+    const T *row = static_cast<const T *>(a.K) + ((long)bh * a.N_cap + last) * a.d;
+    for (int c = tid; c < a.r; c += THREADS)
+      slab[((long)(slot / TILE) * a.r + c) * TILE + slot % TILE] = row[min(max(a.idx[h * a.r + c], 0), a.d - 1)];
+  }
 }
 
 constexpr int MOVE_ROWS = 64;      // rows a workgroup of evict_move takes
@@ -275,6 +354,21 @@ int ig_launch_evict(ig_ctx *ctx, const ig_desc *d, int keep, const int32_t *kv_l
   a.by_H = ig_fast_div(d->H), a.by_units = ig_fast_div(a.units);
   a.by_chunks = ig_fast_div((a.most + MOVE_ROWS - 1) / MOVE_ROWS);
   const bool one = a.most <= 16;         // few rows a pool: moved by the workgroup that found them
+  if (d->N == keep + 1 && a.units <= 256) {
+    // (256 threads take 8 slots each of 2048; the long pools' 1024 as many of 8192)
+#define ONE(T)                                                                                       \
+  {                                                                                                  \
+    if (d->N <= 4096) {                                                                              \
+      auto k = evict_one<T, 256>;                                                                    \
+      IG_LAUNCH(ctx, IG_K_EVICT, k, dim3(BH), dim3(256), s, a);                                      \
+    } else {                                                                                         \
+      auto k = evict_one<T, 1024>;                                                                   \
+      IG_LAUNCH(ctx, IG_K_EVICT, k, dim3(BH), dim3(1024), s, a);                                     \
+    }                                                                                                \
+  }
+    if (d->dtype == IG_F16) ONE(half_t) else ONE(float)
+    return IG_OK;
+  }
 #define SELECT(T, THREADS, KPT)                                                                       \
   {                                                                                                  \
     if (one) {                                                                                       \
