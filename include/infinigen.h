@@ -396,8 +396,10 @@ int ig_gather_attention(ig_ctx *ctx, const ig_desc *desc, const void *q, const v
  *    and rope are not used.
  *  - kv_len: device int32 [B], valid slots of each sequence, or NULL: N for all.  Clamped to [0, N]; N
  *    is the largest length the call may meet and sizes its grid.  N = 0 is allowed.
- *  - Rows of the valid slots are expected to be finite.  What lies in other slots is never used,
- *    whatever it holds.
+ *  - Rows of the valid slots are expected to be finite (an infinity or a NaN among them may reach rows
+ *    that do not see its slot) and logits above -6e29.  What lies in other slots, in query rows and nodes
+ *    behind the last one, is never used, whatever it holds.
+ *  - out must not overlap the inputs (IG_EINVAL).
  *  - mass: device float32 [B*H, N_cap], one sum per slot, zero-initialised by the caller.  born: device
  *    int32 [B*H, N_cap], the position of the token a slot holds (the stamps of IG_POLICY_FIFO). */
 

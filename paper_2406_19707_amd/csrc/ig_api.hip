@@ -977,12 +977,17 @@ int ig_reserve_cache(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_q) 
   int rc = check_cache(ctx, d, "ig_reserve_cache", group, n_q, false, nullptr);
   if (rc) return rc;
   if ((rc = set_device(ctx))) return rc;
-  // the largest workspace of any call this covers: with weights or a tree, any length and number of tokens up
-  // to these, any number of slots to keep
   return ig_ensure(ctx, (void **)&ctx->cache_ws, &ctx->cache_ws_bytes, ig_cache_reserve_bytes(d, group, n_q));
 }
 
 static int attend_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, void *stream) {
+  // (queries are read again after the first rows are out, pools by every row)
+  const size_t row = (size_t)d->d * ig_elem_bytes(d->dtype), q_bytes = (size_t)d->B * c.n_q * d->H * c.group * row;
+  const size_t pool_bytes = (size_t)d->B * d->H * d->N_cap * row, tree_bytes = (size_t)d->B * c.n_q * d->H * row;
+  const struct { const void *p; size_t n; } in[] = {{c.q, q_bytes}, {c.K, pool_bytes}, {c.V, pool_bytes}, {c.k_tree, tree_bytes}, {c.v_tree, tree_bytes}};
+  for (const auto &x : in)
+    if (x.p && (uintptr_t)c.out < (uintptr_t)x.p + x.n && (uintptr_t)x.p < (uintptr_t)c.out + q_bytes)
+      return ig_fail(ctx, IG_EINVAL, "out must not overlap the queries, keys or values");
   int rc = set_device(ctx);
   if (rc) return rc;
   const CachePlan p = ig_cache_plan(d, c);

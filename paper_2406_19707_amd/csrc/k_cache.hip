@@ -853,11 +853,14 @@ int prompt_rows(const ig_desc *d, const CacheCall &c) {
 // rows of attend_prompt, four waves' tiles of attend_stream) takes a unit of time, a workgroup two more to start and
 // to leave its state, and a compute unit holds eight waves.  (Four sequences of up to 9001 with 1268 query rows for
 // each of 8 pools: 3 slices of 320 row blocks 1.5 times as fast as 2, which leave the second round a quarter full.)
+// Never more than four rounds of workgroups, so that the states they leave are bounded (reserve_rows).
+constexpr long ROUNDS = 4;
+long slots_of(int prompt_rows) { return prompt_rows == 256 ? 256 : 512; }
 int slices_of(const ig_desc *d, int prompt_rows, long nrb, int n_keys) {
-  const long groups = d->B * (long)d->H * nrb, slots = prompt_rows == 256 ? 256 : 512;
+  const long groups = d->B * (long)d->H * nrb, slots = slots_of(prompt_rows);
   const long turns = div_up(n_keys, prompt_rows ? 64 : (d->dtype == IG_F16 ? 128 : 64));
   long best = 1, best_cost = -1;
-  for (long s = 1; s <= 64 && s <= turns; ++s) {
+  for (long s = 1; s <= 64 && s <= turns && (s == 1 || groups * s <= ROUNDS * slots); ++s) {
     const long cost = div_up(groups * s, slots) * (div_up(turns, s) + 2);
     if (best_cost < 0 || cost < best_cost) best = s, best_cost = cost;
   }
@@ -967,7 +970,7 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
     BY_DIM(float, STREAM_ROWS)
   }
   if (p.slices > 1 || logits) {
-    const int chunks = logits ? div_up(d->N, 1024) : 1;
+    const int chunks = logits && d->N ? div_up(d->N, 1024) : 1;
     const int rows = p.slices > 1 ? div_up(a.R, 256 / d->d) : 1;
     const FastDiv by_chunks = ig_fast_div(chunks > rows ? chunks : rows);
     const dim3 jgrid((unsigned)(by_chunks.d * BH));
@@ -983,7 +986,8 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   }
     if (d->dtype == IG_F16) JOIN(half_t) else JOIN(float)
   }
-  if (c.mass && !logits && d->dtype == IG_F16) {
+  if (!c.mass || logits || d->N == 0) return IG_OK;
+  if (d->dtype == IG_F16) {
     // keys in pairs of blocks as the rows above: a prompt's first keys are seen by all of its rows, its last by few
     a.nrb = div_up(d->N, MASS_KEYS);
     a.paired = BH * a.nrb >= 1024 && 2 * c.n_q > d->N;
@@ -997,7 +1001,7 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
     IG_LAUNCH(ctx, IG_K_CACHE, k, mgrid, block, stream, a, c.mass);                                  \
   }
     BY_DIM(half_t, PROMPT_MASS)
-  } else if (c.mass && !logits) {
+  } else {
 #define MASS(T, D)                                                                                   \
   {                                                                                                  \
     const FastDiv by_chunks = ig_fast_div(div_up(d->N, mass_keys<D>()));                             \
@@ -1009,29 +1013,18 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   return IG_OK;
 }
 
-// What ig_reserve_cache sizes the workspace for.  More rows mean fewer slices, so the largest need is not that of
-// the largest call: every number of tokens is looked at for which the pools are still cut into slices.
+// What ig_reserve_cache sizes the workspace for: any number of tokens, slots and slots to keep up to these.  Fewer rows
+// or slots can mean more slices, so this is a bound of the parts and not the largest call's plan: a call leaves states
+// of at most 64 slices of every row, and of at most ROUNDS rounds of workgroups.
 size_t ig_cache_reserve_bytes(const ig_desc *d, int group, int n_q) {
+  const long BH = (long)d->B * d->H, R = (long)n_q * group;
+  const long rounds = ROUNDS * (d->dtype == IG_F16 ? 256 * slots_of(256) > 128 * slots_of(128) ? 256 * slots_of(256) : 128 * slots_of(128)
+                                                   : 32 * slots_of(0));
+  const long rows = 64 * BH * R < rounds ? 64 * BH * R : rounds;
+  const size_t logits = group <= 32 ? (size_t)BH * group * (((long)d->N_cap + 63) / 64 * 64) * sizeof(float) : 0;
+  const size_t attention = (size_t)BH * R * sizeof(float2) + (size_t)rows * (sizeof(float2) + d->d * sizeof(float)) + logits + 4 * 256;
   ig_desc full = *d;
   full.N = d->N_cap;
-  const int half_keep = full.N / 2 < 1 ? 1 : full.N / 2;
-  size_t most = ig_evict_workspace(&full, half_keep);
-  static float weights;
-  auto look = [&](int n) {
-    CacheCall c = {};
-    c.group = group, c.n_q = n, c.mass = &weights;
-    const CachePlan p = ig_cache_plan(&full, c);
-    if (p.bytes > most) most = p.bytes;
-    if (n <= 64) {
-      c.mass = nullptr, c.k_tree = &weights;
-      const CachePlan t = ig_cache_plan(&full, c);
-      if (t.bytes > most) most = t.bytes;
-      return p.slices > 1 || t.slices > 1;
-    }
-    return p.slices > 1;
-  };
-  for (int n = 1; n <= n_q && look(n); ++n) {
-  }
-  look(n_q);
-  return most;
+  const size_t eviction = ig_evict_workspace(&full, full.N / 2 < 1 ? 1 : full.N / 2);
+  return attention > eviction ? attention : eviction;
 }

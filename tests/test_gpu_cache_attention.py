@@ -35,6 +35,11 @@ SHAPES = [
     (1, 2, 65, 1, 70, 0, None, None),              # more heads to a pool than the kept logits are for
     (2, 3, 1, 128, 640, 0, [640, 128], None),
     (2, 2, 2, 257, 513, 7, [513, 300], [257, 129]),
+    (2, 2, 1, 2, 300, 0, [300, 0], None),
+    (1, 2, 17, 1, 90, 3, None, None),
+    (2, 1, 32, 1, 33, 0, [0, 33], None),
+    (1, 1, 1, 33, 64, 0, None, None),
+    (1, 1, 5, 26, 128, 0, None, None),             # 130 rows that mostly see the same
 ]
 
 
@@ -64,6 +69,19 @@ def test_without_weights_is_the_same(ctx, n_q, N):
     a = run_attention(ctx, "f16", 128, 2, 2, 2, n_q, N, N, None, None, with_mass=True)
     b = run_attention(ctx, "f16", 128, 2, 2, 2, n_q, N, N, None, None, with_mass=False)
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_row_blocks_and_key_blocks_in_pairs(ctx, d):
+    """Calls large enough for workgroups to take two blocks each, an odd number of them."""
+    run_attention(ctx, "f16", d, 8, 64, 1, 300, 513, 514, [513, 300, 1, 0, 257, 512, 400, 299], [300, 300, 1, 300, 0, 129, 300, 299])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("n_q", [1, 5, 40])
+def test_no_slots(ctx, dtype, n_q):
+    """N = 0: every row that is there becomes zero, no weight changes."""
+    run_attention(ctx, dtype, 64, 2, 2, 2, n_q, 0, 7, None, [n_q, 0])
 
 
 def test_far_slots(ctx):
@@ -174,6 +192,9 @@ def test_refusals(ctx):
     attention(ig.IG_EDTYPE, ds=bad)
     with pytest.raises(AssertionError):
         ctx.ig_cache_attention(ds, 1, 4, q.transpose(1, 2), None, K, V, None, None, out)
+    attention(ig.IG_EINVAL, out=q)
+    attention(ig.IG_EINVAL, out=K.data_ptr() + 16)
+    tree(ig.IG_EINVAL, out=vt.data_ptr() + 32)
     torch.cuda.synchronize()
     assert (out == SENTINEL).all()
 
@@ -247,6 +268,7 @@ def test_reserved_covers_smaller_calls():
     held = c.ig_workspace_bytes()
     K, V = pools(B, H, d, N, "f16", [N], 1)
     q = rows((B, 100, H * G, d), "f16", 2)
+    kt = rows((B, 64, H, d), "f16", 3)
     out, mass = torch.empty_like(q), torch.zeros((B * H, N), device="cuda")
     bits = torch.zeros((B, 64), dtype=torch.int64, device="cuda")
     for n in (1, 2, 7, 8, 9, 16, 31, 32, 33, 64, 100):
@@ -254,7 +276,7 @@ def test_reserved_covers_smaller_calls():
             ds.N = length
             c.ig_cache_attention(ds, G, n, q, None, K, V, None, mass, out)
             if n <= 64:
-                c.ig_tree_attention(ds, G, n, q, q, q, bits, None, K, V, None, out)
+                c.ig_tree_attention(ds, G, n, q, kt, kt, bits, None, K, V, None, out)
     for keep in (1, 100, 1500, N - 1):
         c.ig_pool_evict(ds, keep, None, mass, None, None, None, None, K, V)
     torch.cuda.synchronize()
