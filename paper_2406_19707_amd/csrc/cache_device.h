@@ -37,18 +37,11 @@ __device__ __forceinline__ int xcd_order(int id, int per_xcd) { return (id & 7) 
 __device__ __forceinline__ int length_of(const int32_t *len, int b, int all, int most) {
   return len ? min(max(len[b], 0), min(all, most)) : all;
 }
+// slots that row `row` of a pool's query rows sees: those of a tree all, those of a prompt up to their own
+template <bool TREE> __device__ __forceinline__ int row_limit(const StreamArgs &a, int row, int kv, int nq) {
+  return TREE ? kv : max(0, kv - nq + a.by_group.div(row) + 1);
+}
 __device__ __forceinline__ unsigned long long low_bits(int n) { return n >= 64 ? ~0ull : (1ull << n) - 1; }
-
-__device__ __forceinline__ int wave_min_int(int v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
-  return __builtin_amdgcn_readfirstlane(v);
-}
-__device__ __forceinline__ int wave_max_int(int v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
-  return __builtin_amdgcn_readfirstlane(v);
-}
 
 // 2^x to the last bit but one; denormal results are zero (a weight of 2^-126 of the largest)
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -180,4 +173,13 @@ __device__ __forceinline__ float both_max(float v) {
 __device__ __forceinline__ float both_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// over the four lanes that hold a column of a 16x16 product: l, l + 16, l + 32, l + 48
+__device__ __forceinline__ float column_max(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return both_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float column_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return both_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }

@@ -45,31 +45,13 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d;
   const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
 
-  // what every row sees: slots below lim (and, in a tree, the nodes of its mask)
-  int lim[NT];
-  unsigned long long sees[NT];
-  bool live[NT];
-  const T *q = static_cast<const T *>(a.q);
-  uint4 qf[NT][KCH];
-  int lim_min = 0x7fffffff, lim_max = 0;
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int row = rb * RB + n * 16 + i, iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
-    live[n] = row < a.R && iq < nq;
-    lim[n] = live[n] ? (TREE ? kv : max(0, kv - nq + iq + 1)) : 0x7fffffff;
-    sees[n] = TREE && live[n] ? a.visible[(long)b * a.n_q + iq] & low_bits(nq) : 0;
-    lim_min = min(lim_min, lim[n]);
-    lim_max = max(lim_max, live[n] ? lim[n] : 0);
-    const uint4 *src = reinterpret_cast<const uint4 *>(
-        q + (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * (int)a.by_group.d + gq) * D);
-#pragma unroll
-    for (int c = 0; c < KCH; ++c) qf[n][c] = flip_sign<T>(src[c * 4 + g], a.flip);
-  }
-  lim_min = wave_min_int(lim_min);
-  lim_max = wave_max_int(lim_max);
-
-  const int cache_tiles = (min(lim_max, kv) + TT - 1) / TT;
-  const int tiles = cache_tiles + (TREE ? (nq + TT - 1) / TT : 0);
+  // What the rows see: slots below their limit, which does not fall from row to row (and, in a tree, the nodes of their
+  // masks).
+  const int first_row = rb * RB, last_row = min(min(a.R, nq * (int)a.by_group.d), first_row + RB) - 1;
+  const bool rows_here = last_row >= first_row;
+  const int lim_min = rows_here ? row_limit<TREE>(a, first_row, kv, nq) : 0x7fffffff;
+  const int cache_tiles = rows_here ? (min(row_limit<TREE>(a, last_row, kv, nq), kv) + TT - 1) / TT : 0;
+  const int tiles = cache_tiles + (TREE && rows_here ? (nq + TT - 1) / TT : 0);
   const int per = (tiles + a.slices - 1) / a.slices;
   const int t_begin = min(tiles, slice * per), t_end = min(tiles, t_begin + per);
 
@@ -100,6 +82,34 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
       load_words<VW>(base + min(t0 + VT * g + u, last) * stride + CJ * i, v[u]);
   };
 
+  // A short call is the trips through memory one after the other, so the first tile is asked for with the queries.
+  int lim[NT];
+  unsigned long long sees[NT];
+  bool live[NT];
+  uint4 qf[NT][KCH];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int row = rb * RB + n * 16 + i, iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
+    live[n] = row <= last_row;
+    lim[n] = live[n] ? row_limit<TREE>(a, row, kv, nq) : 0x7fffffff;
+    if (TREE) sees[n] = a.visible[(long)b * a.n_q + min(iq, a.n_q - 1)];
+    const uint4 *src = reinterpret_cast<const uint4 *>(
+        static_cast<const T *>(a.q) + (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * (int)a.by_group.d + gq) * D);
+#pragma unroll
+    for (int c = 0; c < KCH; ++c) qf[n][c] = src[c * 4 + g];
+  }
+  int tile = t_begin + w;
+  if (tile < t_end) {
+    load_k(tile);
+    load_v(tile);
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    if (TREE) sees[n] = live[n] ? sees[n] & low_bits(nq) : 0;
+#pragma unroll
+    for (int c = 0; c < KCH; ++c) qf[n][c] = flip_sign<T>(qf[n][c], a.flip);
+  }
+
   floatx4 acc[NT][CJ];
   float m_run[NT], l_run[NT];
 #pragma unroll
@@ -111,11 +121,6 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   }
 
   int kept = 0;                                           // tiles in the wave's box of logits
-  int tile = t_begin + w;
-  if (tile < t_end) {
-    load_k(tile);
-    load_v(tile);
-  }
   // (`more` is known at compile time: the waits for a tile's values then leave the next one's keys in flight)
   auto turn = [&](auto more_tiles) __attribute__((always_inline)) {
     constexpr bool more = decltype(more_tiles)::value;
@@ -185,8 +190,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, s[n][m][r]);
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      top = column_max(top);
       const float ref = fmaxf(m_run[n], top * a.c);
       if (__any(ref > m_run[n])) {
         const float shrink = exp2_fast(m_run[n] - ref);
@@ -234,8 +238,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   // ---- the four waves' states joined, and rows out: finished ones to `out`, the states of a slice to the workspace ----
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    l_run[n] += __shfl_xor(l_run[n], 16, 64);
-    l_run[n] += __shfl_xor(l_run[n], 32, 64);
+    l_run[n] = column_sum(l_run[n]);
     if (g == 0) {
       box_m[w][n * 16 + i] = m_run[n];
       box_l[w][n * 16 + i] = l_run[n];
@@ -317,13 +320,14 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
     }
     const int row = rb * ROWS + w * 32 + i, iq = a.by_group.div(row), gq = row - iq * G;
     const bool live = row < a.R && iq < nq;
-    const int lim = live ? (TREE ? kv : max(0, kv - nq + iq + 1)) : 0x7fffffff;
+    const int lim = live ? row_limit<TREE>(a, row, kv, nq) : 0x7fffffff;
     const unsigned long long sees = TREE && live ? a.visible[(long)b * a.n_q + iq] & low_bits(nq) : 0;
     const long row_at = (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * G + gq) * D;
-    const int lim_min = wave_min_int(lim);
+    // (limits do not fall from row to row)
+    const int first_row = rb * ROWS + w * 32, lim_min = row_limit<TREE>(a, first_row, kv, nq);
     // (what the row block's last live row sees)
     const int last_row = min(min(a.R, nq * G), (rb + 1) * ROWS) - 1;
-    const int most = last_row < rb * ROWS ? 0 : (TREE ? kv : max(0, kv - nq + a.by_group.div(last_row) + 1));
+    const int most = last_row < rb * ROWS ? 0 : row_limit<TREE>(a, last_row, kv, nq);
     const int cache_tiles = (most + TK - 1) / TK;
     const int tiles_all = cache_tiles + (TREE && last_row >= rb * ROWS ? (nq + TK - 1) / TK : 0);
     const int per = (tiles_all + a.slices - 1) / a.slices;
