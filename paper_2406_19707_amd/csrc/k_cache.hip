@@ -855,7 +855,8 @@ int prompt_rows(const ig_desc *d, const CacheCall &c) {
 
 // Slices the cached rows of a pool are cut into: the number for which the last workgroups end first, if a turn (64
 // rows of attend_prompt, four waves' tiles of attend_stream) takes a unit of time, a workgroup two more to start and
-// to leave its state, and a compute unit holds eight waves.  (Four sequences of up to 9001 with 1268 query rows for
+// to leave its state, the join three for every eight slices, and a compute unit holds eight waves.  (8 pools of 32768: 31 us
+// with 24 slices, 35 with 16, 36 with 64; 32 of 777: 8.8 with 8, 9.7 with 4, 11.2 with 16, 13.6 with one.)  (Four sequences of up to 9001 with 1268 query rows for
 // each of 8 pools: 3 slices of 320 row blocks 1.5 times as fast as 2, which leave the second round a quarter full.)
 // Never more than four rounds of workgroups, so that the states they leave are bounded (reserve_rows).
 constexpr long ROUNDS = 4;
@@ -865,7 +866,7 @@ int slices_of(const ig_desc *d, int prompt_rows, long nrb, int n_keys) {
   const long turns = div_up(n_keys, prompt_rows ? 64 : (d->dtype == IG_F16 ? 128 : 64));
   long best = 1, best_cost = -1;
   for (long s = 1; s <= 64 && s <= turns && (s == 1 || groups * s <= ROUNDS * slots); ++s) {
-    const long cost = div_up(groups * s, slots) * (div_up(turns, s) + 2);
+    const long cost = div_up(groups * s, slots) * (div_up(turns, s) + 2) + (s > 1 ? 3 * div_up(s, 8) : 0);
     if (best_cost < 0 || cost < best_cost) best = s, best_cost = cost;
   }
   return (int)best;
