@@ -386,9 +386,9 @@ int ig_gather_attention(ig_ctx *ctx, const ig_desc *desc, const void *q, const v
 
 /* ---- attention over a whole pool, eviction by its weights, drafted tokens -------------------- */
 
-/* Baseline to the lists: attention that sees every valid slot of a pool, the eviction by accumulated
- * attention weight that Section 2.3 and Section 5.1 compare with, and the verification of drafted
- * tokens over the same pool.  Common to the calls below:
+/* Beside the lists: attention that sees every valid slot of a pool, the eviction by accumulated
+ * attention weight of the fixed-budget cache that Section 5.3 compares with, and the verification of
+ * drafted tokens over the same pool.  Common to the calls below:
  *  - Pools in device memory, [B, H, N_cap, d] of desc->dtype; d = 32, 64, 128 or 256 (IG_ESHAPE
  *    otherwise) in the attention calls, any multiple of 16 bytes in the other two.
  *  - group >= 1 query heads share a pool: query head h * group + g reads pool head h (group = 1: as
@@ -396,9 +396,9 @@ int ig_gather_attention(ig_ctx *ctx, const ig_desc *desc, const void *q, const v
  *    and rope are not used.
  *  - kv_len: device int32 [B], valid slots of each sequence, or NULL: N for all.  Clamped to [0, N]; N
  *    is the largest length the call may meet and sizes its grid.  N = 0 is allowed.
- *  - Rows of the valid slots are expected to be finite (an infinity or a NaN among them may reach rows
- *    that do not see its slot) and logits above -6e29.  What lies in other slots, in query rows and nodes
- *    behind the last one, is never used, whatever it holds.
+ *  - Rows of the valid slots and of nodes that some node sees are expected to be finite (an infinity or a
+ *    NaN among them may reach rows that do not see it) and logits above -6e29.  What lies in other slots and
+ *    nodes, and in query rows behind the last one, is never used, whatever it holds.
  *  - out must not overlap the inputs (IG_EINVAL).
  *  - mass: device float32 [B*H, N_cap], one sum per slot, zero-initialised by the caller.  born: device
  *    int32 [B*H, N_cap], the position of the token a slot holds (the stamps of IG_POLICY_FIFO). */
@@ -432,7 +432,7 @@ int ig_reserve_cache(ig_ctx *ctx, const ig_desc *desc, int32_t group, int32_t n_
 /* ig_append_token for several rows and ragged sequences: the accepted path of a tree, or a prompt's rows.
  * For j < n_append[b], slot kv_len[b] + j of every pool of sequence b receives row path[b, j] of k_rows, v_rows
  * (device [B, n_rows, H, d], 16-byte aligned); slots >= N_cap are skipped.  path: device int32 [B, n_rows],
- * entries clamped to [0, n_rows), or NULL: row j.  n_append: device int32 [B], clamped to [0, n_rows], or
+ * entries clamped to [0, n_rows), or NULL: row j.  The rows must not overlap the pools (IG_EINVAL).  n_append: device int32 [B], clamped to [0, n_rows], or
  * NULL: n_rows.  Here kv_len is the length before the append (NULL: N).  mass, if given, restarts at 0 in
  * these slots, born, if given, becomes pos[b] + j (pos: device int32 [B], or NULL: the slot).  slab with
  * idx_dev, if given, receives the kept key channels as in ig_append_token.  The caller then adds n_append

@@ -43,6 +43,21 @@ template <bool TREE> __device__ __forceinline__ int row_limit(const StreamArgs &
 }
 __device__ __forceinline__ unsigned long long low_bits(int n) { return n >= 64 ? ~0ull : (1ull << n) - 1; }
 
+// Nodes of a sequence's tree that any node sees (by the whole wave; masks_of, asked for ahead of it, are the lanes'
+// nodes').  A node that none sees is never read: its weights are zero, but zero times what it holds need not be.
+__device__ __forceinline__ unsigned long long masks_of(const StreamArgs &a, int b, int nq) {
+  return a.visible[(long)b * a.n_q + min((int)(threadIdx.x & 63), a.n_q - 1)];
+}
+__device__ __forceinline__ unsigned long long nodes_seen(unsigned long long masks, int nq) {
+  unsigned long long v = (int)(threadIdx.x & 63) < nq ? masks & low_bits(nq) : 0;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v |= __shfl_xor(v, o, 64);
+  return (unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+         (unsigned)__builtin_amdgcn_readfirstlane((int)v);
+}
+// the node read for node j: itself, or the first one that is seen
+__device__ __forceinline__ int node_read(unsigned long long seen, int j) { return seen >> (j & 63) & 1 ? j : __builtin_ctzll(seen); }
+
 // 2^x to the last bit but one; denormal results are zero (a weight of 2^-126 of the largest)
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 

@@ -952,6 +952,10 @@ int ig_decode_step_overlapped(ig_ctx *ctx, const ig_desc *d, int n_layers, const
 
 // ---- attention over a whole pool, eviction by its weights, drafted tokens ----
 
+static bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
+  return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+
 // The descriptor of a call over whole pools: a cache without a token is allowed, group query heads share a pool.
 static int check_cache(ig_ctx *ctx, const ig_desc *d, const char *what, int group, int n_q, bool attends, void *stream) {
   if (!ctx) return IG_EINVAL;
@@ -986,7 +990,7 @@ static int attend_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, void 
   const size_t pool_bytes = (size_t)d->B * d->H * d->N_cap * row, tree_bytes = (size_t)d->B * c.n_q * d->H * row;
   const struct { const void *p; size_t n; } in[] = {{c.q, q_bytes}, {c.K, pool_bytes}, {c.V, pool_bytes}, {c.k_tree, tree_bytes}, {c.v_tree, tree_bytes}};
   for (const auto &x : in)
-    if (x.p && (uintptr_t)c.out < (uintptr_t)x.p + x.n && (uintptr_t)x.p < (uintptr_t)c.out + q_bytes)
+    if (x.p && overlap(c.out, q_bytes, x.p, x.n))
       return ig_fail(ctx, IG_EINVAL, "out must not overlap the queries, keys or values");
   int rc = set_device(ctx);
   if (rc) return rc;
@@ -1028,6 +1032,11 @@ int ig_append_rows(ig_ctx *ctx, const ig_desc *d, int32_t n_rows, const void *k_
   if (!k_rows || !v_rows || !Kpool || !Vpool) return ig_fail(ctx, IG_EINVAL, "ig_append_rows: NULL argument");
   if (slab && !idx_dev) return ig_fail(ctx, IG_EINVAL, "ig_append_rows: a slab needs idx_dev");
   if ((rc = check_aligned(ctx, "ig_append_rows", {k_rows, v_rows, Kpool, Vpool, slab}))) return rc;
+  const size_t row = (size_t)d->d * ig_elem_bytes(d->dtype), rows_bytes = (size_t)d->B * n_rows * d->H * row;
+  for (const void *in : {k_rows, v_rows})
+    for (const void *pool : {Kpool, Vpool})
+      if (overlap(in, rows_bytes, pool, (size_t)d->B * d->H * d->N_cap * row))
+        return ig_fail(ctx, IG_EINVAL, "ig_append_rows: the rows must not overlap the pools");
   if ((rc = set_device(ctx))) return rc;
   return ig_launch_append_rows(ctx, d, n_rows, k_rows, v_rows, path, n_append, kv_len, pos, idx_dev, slab, Kpool, Vpool,
                                mass, born, (hipStream_t)stream);

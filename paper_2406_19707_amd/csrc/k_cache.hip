@@ -1,6 +1,6 @@
 // Attention over a whole key / value pool: a prompt, a chunk of one or a single token with the accumulated
 // attention weight of every slot, and a tree of drafted tokens over the pool (Section 2.1, softmax(q K^T) V;
-// Section 2.3: the weights of earlier steps are what the eviction-based baselines rank a cache by).
+// Section 5.3 compares with a cache of a fixed budget, which ranks its entries by the weight that they have received).
 #include <type_traits>
 
 #include "cache_device.h"
@@ -20,6 +20,11 @@ namespace {
 //  - a lane loads the same CJ = d/16 channels of those eight V rows (a wave-wide load is four whole rows), and
 //    one byte permute each makes from them the pairs of tokens that V^T wants; row i of the output's block j is
 //    the channel CJ i + j.
+// Logits, weights' sums and outputs are float32; the weights are rounded to half precision for the second product,
+// relative to at most 2^-11 each, as the output is in the end.
+// Bound by memory: one token of 16 x 32 heads over 4096 slots 176 us = 6.1 TB/s, of 4 x 40 over 32768 437 us = 6.2 TB/s,
+// float32 8 x 32 over 4096 180 us = 6.0 (a copy of 4 GiB: 4.8 TB/s, a read of as much 6.2 at best); 16 nodes over 4096, 128
+// pools, 53 us = 5.1.  Small calls are the trips through memory in turn: 32 pools of 777, 5.3 us.
 template <typename T, int D, int NT, bool TREE, bool LOGITS>
 __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   constexpr bool HALF = sizeof(T) == 2;
@@ -50,23 +55,34 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   const int first_row = rb * RB, last_row = min(min(a.R, nq * (int)a.by_group.d), first_row + RB) - 1;
   const bool rows_here = last_row >= first_row;
   const int lim_min = rows_here ? row_limit<TREE>(a, first_row, kv, nq) : 0x7fffffff;
-  const int cache_tiles = rows_here ? (min(row_limit<TREE>(a, last_row, kv, nq), kv) + TT - 1) / TT : 0;
+  const int cached = rows_here ? row_limit<TREE>(a, last_row, kv, nq) : 0, cache_tiles = (cached + TT - 1) / TT;
   const int tiles = cache_tiles + (TREE && rows_here ? (nq + TT - 1) / TT : 0);
   const int per = (tiles + a.slices - 1) / a.slices;
-  const int t_begin = min(tiles, slice * per), t_end = min(tiles, t_begin + per);
+  const int t_begin = min(tiles, slice * per);
+  int t_end = min(tiles, t_begin + per);
+  // (what a slice with the nodes needs to know of them only holds it up where it begins with them)
+  unsigned long long seen = 0, masks = 0;
+  const bool nodes_here = TREE && t_end > cache_tiles, nodes_first = nodes_here && t_begin + 4 > cache_tiles;
+  if (nodes_here) masks = masks_of(a, b, nq);
+  auto find_nodes = [&]() __attribute__((always_inline)) {
+    seen = nodes_seen(masks, nq);
+    if (!seen) t_end = cache_tiles;
+  };
+  if (nodes_first) find_nodes();
 
   const T *Kc = static_cast<const T *>(a.K) + (long)bh * a.N_cap * D, *Vc = static_cast<const T *>(a.V) + (long)bh * a.N_cap * D;
   uint4 k[MT][KCH];
   unsigned v[VT][VW];
-  // (tokens past the end are read from the last one: what they hold is never used, and is finite if that is)
+  // (tokens past the last one that a row sees are read from that one: what they hold is never used, and is finite if that is)
   auto load_k = [&](int tile) __attribute__((always_inline)) {
     const bool drafted = TREE && tile >= cache_tiles;
     const T *base = drafted ? static_cast<const T *>(a.k_tree) + ((long)b * a.n_q * a.by_H.d + h) * D : Kc;
     const long stride = drafted ? (long)a.by_H.d * D : D;
-    const int t0 = (drafted ? tile - cache_tiles : tile) * TT, last = (drafted ? nq : kv) - 1;
+    const int t0 = (drafted ? tile - cache_tiles : tile) * TT, last = (drafted ? nq : cached) - 1;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      const int t = min(t0 + (HALF ? 8 * (i >> 2) + 4 * m + (i & 3) : i), last);
+      int t = min(t0 + (HALF ? 8 * (i >> 2) + 4 * m + (i & 3) : i), last);
+      if (TREE && drafted) t = node_read(seen, t);
       const uint4 *src = reinterpret_cast<const uint4 *>(base + t * stride);
 #pragma unroll
       for (int c = 0; c < KCH; ++c) k[m][c] = src[c * 4 + g];
@@ -76,10 +92,13 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
     const bool drafted = TREE && tile >= cache_tiles;
     const T *base = drafted ? static_cast<const T *>(a.v_tree) + ((long)b * a.n_q * a.by_H.d + h) * D : Vc;
     const long stride = drafted ? (long)a.by_H.d * D : D;
-    const int t0 = (drafted ? tile - cache_tiles : tile) * TT, last = (drafted ? nq : kv) - 1;
+    const int t0 = (drafted ? tile - cache_tiles : tile) * TT, last = (drafted ? nq : cached) - 1;
 #pragma unroll
-    for (int u = 0; u < VT; ++u)
-      load_words<VW>(base + min(t0 + VT * g + u, last) * stride + CJ * i, v[u]);
+    for (int u = 0; u < VT; ++u) {
+      int t = min(t0 + VT * g + u, last);
+      if (TREE && drafted) t = node_read(seen, t);
+      load_words<VW>(base + t * stride + CJ * i, v[u]);
+    }
   };
 
   // A short call is the trips through memory one after the other, so the first tile is asked for with the queries.
@@ -103,6 +122,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
     load_k(tile);
     load_v(tile);
   }
+  if (nodes_here && !nodes_first) find_nodes();
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     if (TREE) sees[n] = live[n] ? sees[n] & low_bits(nq) : 0;
@@ -288,6 +308,10 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
 // same one, so the weights never leave their lane.
 // The reference of a row's weights only moves when its largest logit passes it by RISE (weights up to 2^RISE, far
 // inside half precision): the row's output, 16 registers for every 32 channels, is then scaled only now and then.
+// Bound by the vector and matrix units together: 8 x 32 heads of 2048 tokens, d = 128, 360 us = 765 TFLOP/s of what is
+// seen (a library product of 8192 squared reaches 1107), the matrix units busy for 0.41 of the cycles and the vector units
+// for 0.52; d = 64 205 us, d = 256 and half the heads 442 us.  One half block after the other instead of the pipeline: 443 us;
+// tiles of 64 without blocks in pairs the same.
 constexpr float RISE = 6.f;
 constexpr int PROMPT_KEYS = 64;
 
@@ -331,7 +355,17 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
     const int cache_tiles = (most + TK - 1) / TK;
     const int tiles_all = cache_tiles + (TREE && last_row >= rb * ROWS ? (nq + TK - 1) / TK : 0);
     const int per = (tiles_all + a.slices - 1) / a.slices;
-    const int t_begin = min(tiles_all, slice * per), t_end = min(tiles_all, t_begin + per);
+    const int t_begin = min(tiles_all, slice * per);
+    int t_end = min(tiles_all, t_begin + per);
+    // (what a slice with the nodes needs to know of them only holds it up where it begins with them)
+    unsigned long long seen = 0, masks = 0;
+    const bool nodes_here = TREE && t_end > cache_tiles, nodes_first = nodes_here && t_begin + AHEAD > cache_tiles;
+    if (nodes_here) masks = masks_of(a, b, nq);
+    auto find_nodes = [&]() __attribute__((always_inline)) {
+      seen = nodes_seen(masks, nq);
+      if (!seen) t_end = cache_tiles;
+    };
+    if (nodes_first) find_nodes();
 
     half8 qf[KS];
     {
@@ -342,16 +376,20 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
     // tile `tile` of K or V into a slot (past the last one: the last one again, so that every turn has as many loads)
     auto fetch = [&](const void *pool, const void *nodes, int tile, half_t *to) __attribute__((always_inline)) {
       tile = min(tile, t_end - 1);
-      const bool drafted = TREE && tile >= cache_tiles;
-      const int stride = (drafted ? (int)a.by_H.d * D : D) * 2;
-      const int t0 = (drafted ? tile - cache_tiles : tile) * TK, last = (drafted ? nq : kv) - 1 - t0;
-      const char *base = drafted ? static_cast<const char *>(nodes) + ((long)b * a.n_q * a.by_H.d + h) * D * 2
-                                 : static_cast<const char *>(pool) + (long)bh * a.N_cap * D * 2;
       const unsigned r0 = opaque(from_row);
+      if (TREE && tile >= cache_tiles) {                  // (64 nodes at most: one tile)
+        const char *base = static_cast<const char *>(nodes) + ((long)b * a.n_q * a.by_H.d + h) * D * 2;
 #pragma unroll
-      for (int x = 0; x < LOADS; ++x)       // (64 rows: offsets inside a tile fit 32 bits)
-        load_to_lds(base + (long)t0 * stride,
-                    (unsigned)(min((int)r0 + x * (64 / PC), last) * stride) + (from_piece ^ piece_swap<D>(x * (64 / PC))) * 16,
+        for (int x = 0; x < LOADS; ++x)
+          load_to_lds(base, (unsigned)(node_read(seen, min((int)r0 + x * (64 / PC), nq - 1)) * (int)a.by_H.d * D * 2) +
+                                (from_piece ^ piece_swap<D>(x * (64 / PC))) * 16, to + (w * LOADS + x) * 512);
+        return;
+      }
+      const char *base = static_cast<const char *>(pool) + ((long)bh * a.N_cap + (long)tile * TK) * D * 2;
+      const int last = most - 1 - tile * TK;
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x)
+        load_to_lds(base, (unsigned)(min((int)r0 + x * (64 / PC), last) * D * 2) + (from_piece ^ piece_swap<D>(x * (64 / PC))) * 16,
                     to + (w * LOADS + x) * 512);
     };
 
@@ -455,13 +493,14 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
     };
     typedef std::true_type Y;
     typedef std::false_type N;
-    const int turns = t_end - t_begin;
-    if (turns > 0) {
+    if (t_end > t_begin) {
       fetch(a.K, a.k_tree, t_begin, tiles[0][0]);
       if constexpr (AHEAD == 2) {
         fetch(a.K, a.k_tree, t_begin + 1, tiles[1][0]);
         fetch(a.V, a.v_tree, t_begin, tiles[0][1]);
       }
+      if (nodes_here && !nodes_first) find_nodes();
+      const int turns = t_end - t_begin;
       // Turn r: the logits of tile r, the weights of its first half and of the last tile's second half, the last tile's
       // output.  Slots go round: tile r of K or V is in slot r % SLOTS.
       auto begin_turn = [&](int r, auto slot) __attribute__((always_inline)) {
@@ -530,7 +569,8 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
 // ---- joining the slices, and the weights of single-token calls ------------------------------------------
 // A workgroup takes 256 / d rows of a pool and, where logits were kept, 1024 slots of it: mass[t] += sum over the
 // rows of exp2(c s - ref) / sum.  Small calls are a chain of trips through memory, so slices are taken eight at a
-// time, all their loads together, and a slot's weight and first logit are asked for before the sums are known.
+// time, all their loads together, and a slot's weight and first logit are asked for before the sums are known (32 pools of
+// 777 slots, 7 slices: 8.6 -> 3.8 us; 160 pools of 32768: 17 us for 63 MB).
 struct Joined {
   float ref, sum, out;
 };
@@ -622,7 +662,8 @@ __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, in
 // ---- the weights of many query rows ------------------------------------------------------------------
 // Float32: a workgroup keeps 32 cached keys (d = 256: 16) as the rows of S^T = K Q^T; its waves take turns at the
 // query rows that see them, 16 at a time with the next 16 asked for: mass[t] += sum over rows of
-// exp2(c s - ref) / sum, with the rows' final references and sums.
+// exp2(c s - ref) / sum, with the rows' final references and sums.  Bound by the matrix units: 2 x 16 heads of 1024
+// tokens, d = 128, 108 us; 4 heads of 512, d = 64, 9.6 us (32 us with a wave for every 16 keys and nothing asked for ahead).
 template <int D> constexpr int mass_keys() { return D <= 128 ? 32 : 16; }
 template <int D> __global__ __launch_bounds__(256) void attend_mass(StreamArgs a, float *mass, FastDiv by_chunks) {
   constexpr int MT = mass_keys<D>() / 16, KCH = D / 16;
@@ -689,7 +730,9 @@ template <int D> __global__ __launch_bounds__(256) void attend_mass(StreamArgs a
 // Half precision: a wave keeps 64 keys, a workgroup 256, and the query rows
 // come through LDS 64 at a time, one tile ahead.  As in attend_prompt it is a pipeline: while the weights of 32 rows
 // and 32 keys are worked out (an exponential and two fused multiply-adds a pair), the matrix units take the next
-// logits.
+// logits.  The logits are worked out again because no weight is known before a row's last slot.  8 x 32 heads of 2048: 195 us,
+// vector units busy for 0.63 of the cycles and matrix units for 0.37; in 32-row tiles without the pipeline 274 us, with 16
+// query rows a product and no LDS 1149 us.
 constexpr int MASS_KEYS = 256, MASS_ROWS = 64;
 template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt_mass(StreamArgs a, float *mass) {
   constexpr int KS = D / 16, PC = D / 8;

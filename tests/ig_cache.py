@@ -127,19 +127,22 @@ def run_attention(ctx, dtype, d, B, H, group, n_q, N, N_cap, kv, nq, with_mass=T
     return out
 
 
-def run_tree(ctx, dtype, d, B, H, group, T, N, N_cap, kv, nt, visible, scale=None, seed=0):
+def run_tree(ctx, dtype, d, B, H, group, T, N, N_cap, kv, nt, visible, scale=None, seed=0, bad_nodes=()):
     scale = 1.5 / np.sqrt(d) if scale is None else scale
     lens, tlens = kv or [N] * B, nt or [T] * B
     K, V = pools(B, H, d, max(N_cap, 1), dtype, lens, seed)
     q, kt, vt = (rows((B, T, x, d), dtype, seed + 1 + x) for x in (H * group, H, H))
     for b, m in enumerate(tlens):
         q[b, m:], kt[b, m:], vt[b, m:] = float("nan"), float("nan"), float("inf")
+    clean = kt.clone(), vt.clone()
+    for j in bad_nodes:
+        kt[:, j], vt[:, j] = float("inf"), float("nan")
     out = torch.full_like(q, SENTINEL)
     before = out.clone()
     bits = torch.from_numpy(np.array(visible, np.uint64).view(np.int64)).cuda()
     ctx.ig_tree_attention(desc(B, H, d, N, N_cap, dtype, scale), group, T, q, kt, vt, bits, i32(nt), K, V, i32(kv), out)
     torch.cuda.synchronize()
-    check_attention(q, K, V, lens, tlens, group, float(np.float32(scale)), dtype, out, before, tree=(kt, vt, visible))
+    check_attention(q, K, V, lens, tlens, group, float(np.float32(scale)), dtype, out, before, tree=(*clean, visible))
 
 
 def random_tree(T, seed):

@@ -136,6 +136,15 @@ def test_tree_masks(ctx, dtype):
                  [[0 if i % 3 == 0 else (full if i % 3 == 1 else 1 << 63) for i in range(T)]] * 2)
 
 
+@pytest.mark.parametrize("dtype,group,d", [("f16", 1, 64), ("f16", 4, 64), ("f16", 3, 256), ("f32", 1, 128)])
+@pytest.mark.parametrize("kv", [[45, 3], [0, 45]])
+def test_nodes_that_none_sees_may_hold_anything(ctx, dtype, group, d, kv):
+    T, N = 40, 45
+    masks = [v & ~(1 << 7 | 1 << 39) for v in random_tree(T, 3)]
+    for visible in ([masks, masks], [masks, [0] * T]):
+        run_tree(ctx, dtype, d, 2, 2, group, T, N, N, kv, None, visible, bad_nodes=(7, 39))
+
+
 def test_a_chain_is_a_chunk(ctx):
     """A tree that is a chain gives the chunk's attention over the same keys."""
     B, H, G, T, N, d = 2, 2, 2, 24, 150, 64
@@ -195,6 +204,7 @@ def test_refusals(ctx):
     attention(ig.IG_EINVAL, out=q)
     attention(ig.IG_EINVAL, out=K.data_ptr() + 16)
     tree(ig.IG_EINVAL, out=vt.data_ptr() + 32)
+    tree(ig.IG_EINVAL, bits=bits.data_ptr() + 4)
     torch.cuda.synchronize()
     assert (out == SENTINEL).all()
 

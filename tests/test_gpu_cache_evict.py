@@ -218,6 +218,8 @@ def test_refusals(ctx):
         append(ig.IG_EINVAL, **{gone: None})
     append(ig.IG_EINVAL, slab=kr)
     append(ig.IG_EINVAL, k=kr.data_ptr() + 8)
+    append(ig.IG_EINVAL, k=K.data_ptr() + 16)
+    append(ig.IG_EINVAL, v=V)
     append(ig.IG_ESHAPE, ds=desc(B, H, d, -1, N, "f16"))
     refuse(ig.IG_ESHAPE, ctx.ig_reserve_cache, ds, 0, 1)
     refuse(ig.IG_ESHAPE, ctx.ig_reserve_cache, ds, 1, 0)
