@@ -129,13 +129,14 @@ template <int W> __device__ __forceinline__ half8 column_of(const unsigned (&v)[
 // A tile is rows of D halves with the 16-byte pieces of a row in another order: piece c of row r lies where piece
 // c ^ piece_swap(r) would.  16 rows' pieces of one column (what a wave reads of K or Q) and 64 bytes of four
 // consecutive rows (of V) then fall on different banks.  The swap of a sum of two rows without common bits is the
-// exclusive or of theirs, so a lane's addresses differ by exclusive ors and sums with constants, and one register
-// stands for all of them (`opaque` keeps the compiler from holding each in one of its own).
+// exclusive or of theirs, so a lane's address for rows further on, another half tile or another tile is the same one and
+// a constant.
 template <int D> __host__ __device__ constexpr int piece_swap(int row) {
   if constexpr (D == 32) return (row >> 2) & 3;
   else if constexpr (D == 64) return ((row >> 1) & 1) << 2 | ((row >> 2) & 3);
   else return (row & 3) << 2 | ((row >> 2) & 3);
 }
+// keeps the compiler from working out ahead, and holding, what is made from the value
 __device__ __forceinline__ unsigned opaque(unsigned v) {
   asm volatile("" : "+v"(v));
   return v;
@@ -147,24 +148,24 @@ __device__ __forceinline__ lds_bytes lds_at(const half_t *tile) {
   return (lds_bytes)(const __attribute__((address_space(3))) half_t *)tile;
 }
 // Rows of a 32-row block as a product's operand: lane i of either half takes piece 2 k + half of row i.
-template <int D> __device__ __forceinline__ unsigned row_base(int lane) {
+template <int D> __device__ __forceinline__ unsigned row_offset(int lane, int k) {
   const int i = lane & 31, hb = lane >> 5;
-  return i * D * 2 + ((hb ^ piece_swap<D>(i)) * 16);
+  return i * D * 2 + ((hb ^ piece_swap<D>(i)) * 16 ^ k << 5);
 }
-template <int D> __device__ __forceinline__ half8 row_piece(lds_bytes tile, unsigned base, int k) {
-  return *reinterpret_cast<const __attribute__((address_space(3))) half8 *>(tile + (base ^ (k << 5)));
+__device__ __forceinline__ half8 row_piece(const half_t *rows, unsigned offset) {
+  return *reinterpret_cast<const __attribute__((address_space(3))) half8 *>(lds_at(rows) + offset);
 }
 // Columns of 16 rows (0 .. 3, 8 .. 11 in the lower half wave, 4 .. 7, 12 .. 15 in the upper) as an operand: lane i
 // of a half takes column 32 o + i, four rows a call (x = 0: the first four).  The hardware's transposing read takes
 // 8 bytes of a row from each of 16 lanes, lane i's from row i / 4, and gives it column i of the four rows.
-template <int D> __device__ __forceinline__ unsigned column_base(int lane) {
+template <int D> __device__ __forceinline__ unsigned column_offset(int lane, int o, int x) {
   const int i = lane & 15, hb = lane >> 5, r = 4 * hb + (i >> 2), c = 2 * ((lane >> 4) & 1) + ((i >> 1) & 1);
-  return r * D * 2 + ((c ^ piece_swap<D>(r)) * 16) + (i & 1) * 8;
+  return r * D * 2 + ((c ^ piece_swap<D>(r)) * 16 ^ (o << 6 | x << 5)) + (i & 1) * 8;
 }
-template <int D> __device__ __forceinline__ uint2 column_rows(lds_bytes tile, unsigned base, int o, int x) {
+template <int D> __device__ __forceinline__ uint2 column_rows(const half_t *rows, unsigned offset, int x) {
   typedef __fp16 fp4 __attribute__((__vector_size__(8)));
-  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4f16(
-                                       (fp4 __attribute__((address_space(3))) *)(tile + 8 * x * D * 2 + (base ^ (o << 6 | x << 5)))));
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4f16((fp4 __attribute__((address_space(3))) *)(
+                                       lds_at(rows + 8 * x * D) + offset)));
 }
 // 64 pieces from memory to LDS without passing through registers: lane i's, `offset` bytes from `from`, to piece i
 // of `to` (from and to the same in all lanes).  Not the compiler's builtin, because it waits for every such load

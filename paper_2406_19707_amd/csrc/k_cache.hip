@@ -333,7 +333,14 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
 
   // what this lane fetches of every tile: this piece of this row first, then of 64 / PC rows further on, ..
   const unsigned from_row = w * (64 / NW) + lane / PC, from_piece = (lane % PC) ^ piece_swap<D>(from_row);
-  const unsigned k_base = row_base<D>(lane), v_base = column_base<D>(lane);
+  // (a tree's masks leave no registers for all of these: there they are made from the first ones)
+  unsigned k_at[KS], v_at[OB][2];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) k_at[k] = row_offset<D>(lane, k);
+#pragma unroll
+  for (int o = 0; o < OB; ++o)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) v_at[o][x] = column_offset<D>(lane, o, x);
 
   // one row block; in a paired call the last with the first, the last but one with the second, ..
   for (int turn = 0; turn < (a.paired ? 2 : 1); ++turn) {
@@ -413,18 +420,19 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
       half8 kf[KS];
       uint2 vt[2][OB][2];
       if constexpr (NEXT) {
-        const unsigned at = opaque(k_base);
+        const unsigned first = TREE ? opaque(k_at[0]) : 0;
 #pragma unroll
-        for (int k = 0; k < KS; ++k) kf[k] = row_piece<D>(lds_at(K + next_row * D), at, k);
+        for (int k = 0; k < KS; ++k) kf[k] = row_piece(K + next_row * D, TREE ? first ^ k << 5 : k_at[k]);
       }
       if constexpr (OLD) {
-        const unsigned at = opaque(v_base);
+        const unsigned first = TREE ? opaque(v_at[0][0]) : 0;
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int o = 0; o < OB; ++o)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) vt[k][o][x] = column_rows<D>(lds_at(V + (old_row + k * 16) * D), at, o, x);
+            for (int x = 0; x < 2; ++x)
+              vt[k][o][x] = column_rows<D>(V + (old_row + k * 16) * D, TREE ? first ^ (o << 6 | x << 5) : v_at[o][x], x);
       }
       floatx16 s;
       float shrink = 1.f;
@@ -446,7 +454,7 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
         }
         float top = s[0];
 #pragma unroll
-        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+        for (int e = 1; e < 16; ++e) top = __builtin_elementwise_maximum(top, s[e]);
         top = both_max(top) * a.c;
         const float to = top > ref + RISE ? top : ref;
         rises = __any(to != ref);
@@ -746,7 +754,9 @@ template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt
   const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
   const int rows = nq * G;
   const unsigned from_row = w * 16 + lane / PC, from_piece = (lane % PC) ^ piece_swap<D>(from_row);
-  const unsigned q_base = row_base<D>(lane);
+  unsigned q_at[KS];
+#pragma unroll
+  for (int k = 0; k < KS; ++k) q_at[k] = row_offset<D>(lane, k);
 
   // one block of keys; in a paired call the first with the last, the second with the last but one, ..
   for (int turn = 0; turn < (a.paired ? 2 : 1); ++turn) {
@@ -798,9 +808,8 @@ template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt
     floatx16 sums[2] = {}, sA = {}, sB = {};
     half8 qf[KS];
     auto read_rows = [&](const half_t *Q) __attribute__((always_inline)) {
-      const unsigned at = opaque(q_base);
 #pragma unroll
-      for (int k = 0; k < KS; ++k) qf[k] = row_piece<D>(lds_at(Q), at, k);
+      for (int k = 0; k < KS; ++k) qf[k] = row_piece(Q, q_at[k]);
     };
     // weights of the logits `now` (row, keys m) added to the sums, while `next` becomes the logits of the rows in qf and keys n
     auto step = [&](auto has_now, auto has_next, const floatx16 &now, const Row &row, int m, floatx16 &next, int n) __attribute__((always_inline)) {
