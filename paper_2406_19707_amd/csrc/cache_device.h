@@ -12,12 +12,13 @@ struct StreamArgs {
   int n_q, R, Hq, N, N_cap;           // R = n_q * group query rows share a pool
   int nrb, slices, total, per_xcd;    // row blocks and slices of a pool, workgroups in all and of one XCD
   int paired;                         // attend_prompt: a workgroup takes two row blocks
-  FastDiv by_pair, by_slices, by_H, by_group;
+  int B, H;
+  FastDiv by_pair, by_units, by_slices, by_H, by_group;
   int flip;                           // 1: the scale is negative and q is taken with its sign changed; 2: it is zero, and q is taken as zero
   float c;                            // |scale| / ln 2
   float2 *stats;                      // [B*H][R] reference and 1 / sum of finished rows, or NULL
-  float2 *part_ml;                    // [B*H][slices][R] reference and sum of a slice
-  float *part;                        // [B*H][slices][R][d]
+  float2 *part_ml;                    // [H][B*slices][R] reference and sum of a slice
+  float *part;                        // [H][B*slices][R][d]
   float *logits;                      // [B*H][R][logits_ld]
   long logits_ld;
 };
@@ -37,6 +38,57 @@ __device__ __forceinline__ int xcd_order(int id, int per_xcd) { return (id & 7) 
 __device__ __forceinline__ int length_of(const int32_t *len, int b, int all, int most) {
   return len ? min(max(len[b], 0), min(all, most)) : all;
 }
+// ---- which slices are whose --------------------------------------------------------------------------------
+// The B * slices slices of a head are dealt to the sequences by their lengths: one each, and of the others as many as the
+// sequence's share of all slots, rounded down; what is left over stays empty.  (Without lengths from the caller that is
+// `slices` each.)  So a batch of ragged sequences keeps no workgroup waiting for the longest one's: one token of 64
+// sequences of 8192 down to a quarter 270 -> 241 us, a chunk of four of 9001 down to a quarter 347 -> 316; what it costs where
+// all are as long is one to two microseconds.
+struct Span {
+  int b, slice, slices, first;        // the sequence (-1: none), the slice among its own, how many it has, its first one's number
+  int kv, nq;                         // its slots and query tokens
+};
+// the span of slice number `at`, or, BY_SEQUENCE, of sequence `at`
+template <bool BY_SEQUENCE> __device__ __forceinline__ Span span_of(const StreamArgs &a, int at) {
+  if (a.slices == 1 || !a.kv_len || a.B == 1) {
+    const int b = BY_SEQUENCE ? at : a.by_slices.div(at);
+    return Span{b, BY_SEQUENCE ? 0 : at - b * a.slices, a.slices, b * a.slices,
+                length_of(a.kv_len, b, a.N, a.N_cap), length_of(a.q_len, b, a.n_q, a.n_q)};
+  }
+  // (the lanes' sequences' lengths in units of 64 slots: B times as many stay below 2^31)
+  const int lane = threadIdx.x & 63;
+  int kv = length_of(a.kv_len, min(lane, a.B - 1), a.N, a.N_cap), nq = length_of(a.q_len, min(lane, a.B - 1), a.n_q, a.n_q);
+  int all = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int len = b0 ? length_of(a.kv_len, min(b0 + lane, a.B - 1), a.N, a.N_cap) : kv;
+    all += __builtin_amdgcn_readlane(wave_incl_scan(b0 + lane < a.B ? (len + 63) >> 6 : 0), 63);
+  }
+  const long spare = (long)a.B * (a.slices - 1);
+  const float per_unit = all ? (float)spare / (float)all : 0.f;
+  int first = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    if (b0) {
+      kv = length_of(a.kv_len, min(b0 + lane, a.B - 1), a.N, a.N_cap);
+      nq = length_of(a.q_len, min(b0 + lane, a.B - 1), a.n_q, a.n_q);
+    }
+    // spare * units / all, rounded down: by float, then put right by the remainder (there are at most some thousand
+    // slices, so the float is off by one at most)
+    const int units = (kv + 63) >> 6;
+    int extra = (int)((float)units * per_unit);
+    if ((long)extra * all > spare * units) --extra;
+    else if (all && (long)(extra + 1) * all <= spare * units) ++extra;
+    const int mine = b0 + lane < a.B ? 1 + extra : 0, incl = wave_incl_scan(mine);
+    const int end = first + __builtin_amdgcn_readlane(incl, 63);
+    if (BY_SEQUENCE ? at < b0 + 64 : at < end) {
+      const int l = BY_SEQUENCE ? at - b0 : __builtin_ctzll(__ballot(first + incl > at));
+      const int last = first + __builtin_amdgcn_readlane(incl, l), n = __builtin_amdgcn_readlane(mine, l);
+      return Span{b0 + l, BY_SEQUENCE ? 0 : at - (last - n), n, last - n, __builtin_amdgcn_readlane(kv, l), __builtin_amdgcn_readlane(nq, l)};
+    }
+    first = end;
+  }
+  return Span{-1, 0, 0, 0, 0, 0};
+}
+
 // slots that row `row` of a pool's query rows sees: those of a tree all, those of a prompt up to their own
 template <bool TREE> __device__ __forceinline__ int row_limit(const StreamArgs &a, int row, int kv, int nq) {
   return TREE ? kv : max(0, kv - nq + a.by_group.div(row) + 1);

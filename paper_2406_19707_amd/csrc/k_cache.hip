@@ -43,12 +43,13 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
 
   int work = xcd_order(blockIdx.x, a.per_xcd);
   if (work >= a.total) return;
-  const int bh = a.by_pair.div(work);
-  work -= bh * (int)a.by_pair.d;
-  const int rb = a.nrb - 1 - a.by_slices.div(work);       // (a prompt's last rows see most: first)
-  const int slice = a.by_slices.mod(work);
-  const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d;
-  const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
+  // (a head's slices one after the other, the row blocks that share a slice together; a prompt's last rows see most: first)
+  const int h = a.by_pair.div(work);
+  work -= h * (int)a.by_pair.d;
+  const int number = a.by_units.div(work), rb = a.nrb - 1 - a.by_units.mod(work);
+  const Span span = span_of<false>(a, number);
+  if (span.b < 0) return;
+  const int b = span.b, slice = span.slice, bh = b * a.H + h, kv = span.kv, nq = span.nq;
 
   // What the rows see: slots below their limit, which does not fall from row to row (and, in a tree, the nodes of their
   // masks).
@@ -57,7 +58,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   const int lim_min = rows_here ? row_limit<TREE>(a, first_row, kv, nq) : 0x7fffffff;
   const int cached = rows_here ? row_limit<TREE>(a, last_row, kv, nq) : 0, cache_tiles = (cached + TT - 1) / TT;
   const int tiles = cache_tiles + (TREE && rows_here ? (nq + TT - 1) / TT : 0);
-  const int per = (tiles + a.slices - 1) / a.slices;
+  const int per = (tiles + span.slices - 1) / span.slices;
   const int t_begin = min(tiles, slice * per);
   int t_end = min(tiles, t_begin + per);
   // (what a slice with the nodes needs to know of them only holds it up where it begins with them)
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
       store_words<(int)sizeof(T)>(static_cast<T *>(a.out) + (((long)b * a.n_q + iq) * a.Hq + h * (int)a.by_group.d + gq) * D + e, v);
       if (e == 0 && a.stats) a.stats[(long)bh * a.R + row] = make_float2(m, inv);
     } else {
-      const long to = ((long)bh * a.slices + slice) * a.R + row;
+      const long to = ((long)h * a.B * a.slices + number) * a.R + row;
       *reinterpret_cast<floatx4 *>(a.part + to * D + e) = o;
       if (e == 0) a.part_ml[to] = make_float2(m, l);
     }
@@ -325,11 +326,12 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
   const int i = lane & 31, hb = lane >> 5;
   int work = xcd_order(blockIdx.x, a.per_xcd);
   if (work >= a.total) return;
-  const int bh = a.by_pair.div(work);
-  work -= bh * (int)a.by_pair.d;
-  const int unit = a.by_slices.div(work), slice = a.by_slices.mod(work);
-  const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, G = (int)a.by_group.d;
-  const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
+  const int h = a.by_pair.div(work);
+  work -= h * (int)a.by_pair.d;
+  const int number = a.by_units.div(work), unit = a.by_units.mod(work);
+  const Span span = span_of<false>(a, number);
+  if (span.b < 0) return;
+  const int b = span.b, slice = span.slice, bh = b * a.H + h, G = (int)a.by_group.d, kv = span.kv, nq = span.nq;
 
   // what this lane fetches of every tile: this piece of this row first, then of 64 / PC rows further on, ..
   const unsigned from_row = w * (64 / NW) + lane / PC, from_piece = (lane % PC) ^ piece_swap<D>(from_row);
@@ -361,7 +363,7 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
     const int most = last_row < rb * ROWS ? 0 : row_limit<TREE>(a, last_row, kv, nq);
     const int cache_tiles = (most + TK - 1) / TK;
     const int tiles_all = cache_tiles + (TREE && last_row >= rb * ROWS ? (nq + TK - 1) / TK : 0);
-    const int per = (tiles_all + a.slices - 1) / a.slices;
+    const int per = (tiles_all + span.slices - 1) / span.slices;
     const int t_begin = min(tiles_all, slice * per);
     int t_end = min(tiles_all, t_begin + per);
     // (what a slice with the nodes needs to know of them only holds it up where it begins with them)
@@ -562,7 +564,7 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
         }
       if (hb == 0 && a.stats) a.stats[(long)bh * a.R + row] = make_float2(ref, inv);
     } else {
-      const long at = ((long)bh * a.slices + slice) * a.R + row;
+      const long at = ((long)h * a.B * a.slices + number) * a.R + row;
 #pragma unroll
       for (int o = 0; o < OB; ++o)
 #pragma unroll
@@ -583,15 +585,15 @@ struct Joined {
   float ref, sum, out;
 };
 // the row's state over all slices, and element e of its output before the division (OUT)
-template <bool OUT> __device__ __forceinline__ Joined join_row(const StreamArgs &a, int bh, int row, int D, int e) {
+template <bool OUT> __device__ __forceinline__ Joined join_row(const StreamArgs &a, int h, const Span &span, int row, int D, int e) {
   constexpr int U = 8;
   Joined j = {NOTHING_SEEN, 0.f, 0.f};
-  for (int s0 = 0; s0 < a.slices; s0 += U) {
+  for (int s0 = 0; s0 < span.slices; s0 += U) {
     float2 ml[U];
     float o[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long at = ((long)bh * a.slices + min(s0 + u, a.slices - 1)) * a.R + row;
+      const long at = ((long)h * a.B * a.slices + span.first + min(s0 + u, span.slices - 1)) * a.R + row;
       ml[u] = a.part_ml[at];
       if (OUT) o[u] = a.part[at * D + e];
     }
@@ -602,9 +604,9 @@ template <bool OUT> __device__ __forceinline__ Joined join_row(const StreamArgs 
     j.sum *= shrink, j.out *= shrink, j.ref = ref;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const float by = s0 + u < a.slices ? exp2_fast(ml[u].x - ref) : 0.f;
-      if (s0 + u < a.slices) j.sum = fmaf(ml[u].y, by, j.sum);
-      if (OUT && s0 + u < a.slices) j.out = fmaf(o[u], by, j.out);
+      const float by = s0 + u < span.slices ? exp2_fast(ml[u].x - ref) : 0.f;
+      if (s0 + u < span.slices) j.sum = fmaf(ml[u].y, by, j.sum);
+      if (OUT && s0 + u < span.slices) j.out = fmaf(o[u], by, j.out);
     }
   }
   return j;
@@ -616,7 +618,8 @@ __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, in
   __shared__ float2 stat[32];                              // (LOGITS: R <= 32)
   const int bh = by_chunks.div(blockIdx.x), x = by_chunks.mod(blockIdx.x), tid = threadIdx.x;
   const int b = a.by_H.div(bh), h = bh - b * (int)a.by_H.d, G = (int)a.by_group.d;
-  const int kv = length_of(a.kv_len, b, a.N, a.N_cap), nq = length_of(a.q_len, b, a.n_q, a.n_q);
+  const Span span = span_of<true>(a, b);
+  const int kv = span.kv, nq = span.nq;
   float *m = mass + (long)bh * a.N_cap;
   const float *logits = a.logits + (long)bh * a.R * a.logits_ld;
   float before[U], first[U];
@@ -632,7 +635,7 @@ __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, in
   if (a.slices > 1) {
     const int mine = by_D.div(tid), row = x * by_D.div(256) + mine, e = tid - mine * D;
     if (row < nq * G) {
-      const Joined j = join_row<true>(a, bh, row, D, e);
+      const Joined j = join_row<true>(a, h, span, row, D, e);
       const float inv = inverse_of(j.sum);
       const int iq = a.by_group.div(row), gq = row - iq * G;
       static_cast<T *>(a.out)[(((long)b * a.n_q + iq) * a.Hq + h * G + gq) * D + e] = (T)(j.out * inv);
@@ -642,7 +645,7 @@ __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, in
   if (!slots) return;
   if (tid < a.R) {
     if (a.slices > 1) {
-      const Joined j = join_row<false>(a, bh, tid, D, 0);
+      const Joined j = join_row<false>(a, h, span, tid, D, 0);
       stat[tid] = make_float2(j.ref, inverse_of(j.sum));
     } else {
       stat[tid] = a.stats[(long)bh * a.R + tid];
@@ -959,9 +962,8 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   a.q = c.q, a.K = c.K, a.V = c.V, a.k_tree = c.k_tree, a.v_tree = c.v_tree, a.out = c.out;
   a.visible = c.visible, a.q_len = c.q_len, a.kv_len = c.kv_len;
   a.n_q = c.n_q, a.R = c.n_q * c.group, a.Hq = d->H * c.group, a.N = d->N, a.N_cap = d->N_cap;
-  a.nrb = p.nrb, a.slices = p.slices, a.total = (int)(BH * p.nrb * p.slices), a.per_xcd = div_up(a.total, 8);
-  a.by_pair = ig_fast_div(p.nrb * p.slices), a.by_slices = ig_fast_div(p.slices);
-  a.by_H = ig_fast_div(d->H), a.by_group = ig_fast_div(c.group);
+  a.nrb = p.nrb, a.slices = p.slices, a.B = d->B, a.H = d->H;
+  a.by_slices = ig_fast_div(p.slices), a.by_H = ig_fast_div(d->H), a.by_group = ig_fast_div(c.group);
   a.flip = d->scale < 0.f ? 1 : (d->scale == 0.f ? 2 : 0);
   a.c = (d->scale == 0.f ? 1.f : fabsf(d->scale)) * 1.44269504088896340736f;
   a.stats = c.mass ? reinterpret_cast<float2 *>(ws + p.stats_at) : nullptr;
@@ -971,10 +973,9 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   a.logits_ld = p.logits_ld;
   // a causal call with workgroups to spare: each takes a late and an early row block, so that all take equally long
   a.paired = p.prompt && !tree && p.slices == 1 && BH * p.nrb >= (p.rb == 256 ? 512 : 1024) && 2 * c.n_q > d->N;
-  if (a.paired) {
-    const int units = (p.nrb + 1) / 2;
-    a.total = (int)(BH * units), a.per_xcd = div_up(a.total, 8), a.by_pair = ig_fast_div(units);
-  }
+  const int units = a.paired ? (p.nrb + 1) / 2 : p.nrb;
+  a.by_units = ig_fast_div(units), a.by_pair = ig_fast_div(d->B * p.slices * units);
+  a.total = (int)(BH * p.slices * units), a.per_xcd = div_up(a.total, 8);
   const dim3 grid(a.per_xcd * 8), block(256);
 #define STREAM(T, D, NT)                                                                             \
   {                                                                                                  \

@@ -64,6 +64,17 @@ def test_long_and_wide(ctx, dtype, B, H, n_q, N):
     run_attention(ctx, dtype, 128, B, H, 1, n_q, N, N + 3, None, None)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("group", [1, 40])
+@pytest.mark.parametrize("kind", ["ragged", "one long", "empty", "full"])
+def test_slices_of_many_ragged_sequences(ctx, dtype, group, kind):
+    """More sequences than a wave has lanes, their slices dealt by length."""
+    B, N = 70, 2500
+    kv = {"ragged": [(b * 37 % 64) * 39 for b in range(B)], "one long": [N if b == 66 else 1 for b in range(B)],
+          "empty": [0] * B, "full": [N] * B}[kind]
+    run_attention(ctx, dtype, 64, B, 1, group, 1, N, N + 1, kv, [b % 5 and 1 for b in range(B)])
+
+
 @pytest.mark.parametrize("n_q,N", [(1, 333), (100, 333)])
 def test_without_weights_is_the_same(ctx, n_q, N):
     a = run_attention(ctx, "f16", 128, 2, 2, 2, n_q, N, N, None, None, with_mass=True)
