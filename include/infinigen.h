@@ -399,7 +399,8 @@ int ig_gather_attention(ig_ctx *ctx, const ig_desc *desc, const void *q, const v
  *  - Rows of the valid slots and of nodes that some node sees are expected to be finite (an infinity or a
  *    NaN among them may reach rows that do not see it) and logits above -6e29.  What lies in other slots and
  *    nodes, and in query rows behind the last one, is never used, whatever it holds.
- *  - out must not overlap the inputs (IG_EINVAL).
+ *  - out must not overlap the inputs (IG_EINVAL).  At most 2^26 query rows (B * H * group * tokens; rows to
+ *    append likewise) and 2^24 elements of a token (H * group * d), IG_ESHAPE otherwise.
  *  - mass: device float32 [B*H, N_cap], one sum per slot, zero-initialised by the caller.  born: device
  *    int32 [B*H, N_cap], the position of the token a slot holds (the stamps of IG_POLICY_FIFO). */
 

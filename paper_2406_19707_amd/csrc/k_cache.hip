@@ -302,17 +302,16 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
 }
 
 // ---- many query rows, half precision -------------------------------------------------------------------
-// The same products on 32x32 matrix instructions: a wave takes 32 query rows, a workgroup 128 that share the
-// cached rows' tiles of 64, which come to LDS asynchronously, one ahead.  As above S^T = K Q^T and O^T = V^T P^T,
+// The same products on 32x32 matrix instructions: a wave takes 32 query rows, a workgroup 128 (256) that share the
+// cached rows' tiles of 64, which come to LDS asynchronously, one (two) ahead.  As above S^T = K Q^T and O^T = V^T P^T,
 // so that a query row is one lane of each half wave.  The accumulator of a 32-token block holds, in half h, the
 // tokens 8 x + 4 h + 0 .. 3; P^T takes them in that order, and V^T is read through LDS's transposing loads in the
 // same one, so the weights never leave their lane.
 // The reference of a row's weights only moves when its largest logit passes it by RISE (weights up to 2^RISE, far
 // inside half precision): the row's output, 16 registers for every 32 channels, is then scaled only now and then.
-// Bound by the vector and matrix units together: 8 x 32 heads of 2048 tokens, d = 128, 360 us = 765 TFLOP/s of what is
+// Bound by the vector and matrix units together: 8 x 32 heads of 2048 tokens, d = 128, 355 us = 775 TFLOP/s of what is
 // seen (a library product of 8192 squared reaches 1107), the matrix units busy for 0.41 of the cycles and the vector units
-// for 0.52; d = 64 205 us, d = 256 and half the heads 442 us.  One half block after the other instead of the pipeline: 443 us;
-// tiles of 64 without blocks in pairs the same.
+// for 0.52; d = 64 207 us, d = 256 and half the heads 433 us.  One half block after the other, row blocks not in pairs: 443 us.
 constexpr float RISE = 6.f;
 constexpr int PROMPT_KEYS = 64;
 
@@ -902,7 +901,7 @@ bool many_rows(const ig_desc *d, long R) { return d->dtype == IG_F16 && R > (d->
 
 // The same for attend_prompt.  Eight waves, two tiles ahead, where most of what the rows see is seen by all of them and
 // there are rows for more than four (317 x 4 query rows over up to 9001: 225 against 235 us, trees of 63 x 4 nodes over 8191: 97
-// against 106); four for prompts, where a block of 256 rows works out more that its first rows do not see (2048 over 2048:
+// against 106, before slices went by length); four for prompts, where a block of 256 rows works out more that its first rows do not see (2048 over 2048:
 // 397 against 367 us).
 int prompt_rows(const ig_desc *d, const CacheCall &c) {
   return d->d >= 64 && d->d <= 128 && (long)c.n_q * c.group > 128 && (c.k_tree || 2 * (long)c.n_q <= d->N) ? 256 : 128;

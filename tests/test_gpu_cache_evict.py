@@ -227,6 +227,20 @@ def test_refusals(ctx):
     assert torch.equal(K, K0)
 
 
+def test_profile_names_the_launches(ctx):
+    B, H, d, N = 1, 2, 64, 300
+    K, V = make_pools(B, H, d, N, "f16", 1)
+    q, mass = rows((B, 1, H, d), "f16", 2), torch.rand((B * H, N), device="cuda")
+    ds = desc(B, H, d, N, N, "f16")
+    ctx.ig_profile_begin()
+    ctx.ig_cache_attention(ds, 1, 1, q, None, K, V, None, mass, torch.empty_like(q))
+    ctx.ig_pool_evict(ds, 100, None, mass, None, None, None, None, K, V)
+    ctx.ig_profile_end()
+    for which, launches in ((ig.IG_K_CACHE, 2), (ig.IG_K_EVICT, 2)):
+        ms, n = ctx.ig_profile_read(which)
+        assert n == launches and ms > 0
+
+
 def test_budgeted_decoding_and_drafting(ctx):
     """The calls as they are used together, with a slab beside: a prompt with weights, the eviction to the budget,
     decode steps (append, attend with weights, evict by one), a drafted tree over the pool, its accepted path, and
