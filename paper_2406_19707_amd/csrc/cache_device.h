@@ -13,7 +13,8 @@ struct StreamArgs {
   int nrb, slices, total, per_xcd;    // row blocks and slices of a pool, workgroups in all and of one XCD
   int paired;                         // attend_prompt: a workgroup takes two row blocks
   int B, H;
-  FastDiv by_pair, by_units, by_slices, by_H, by_group;
+  FastDiv by_pair, by_units;          // workgroups of a head (prompt_mass: of a pool), of a slice
+  FastDiv by_slices, by_H, by_group;
   int flip;                           // 1: the scale is negative and q is taken with its sign changed; 2: it is zero, and q is taken as zero
   float c;                            // |scale| / ln 2
   float2 *stats;                      // [B*H][R] reference and 1 / sum of finished rows, or NULL

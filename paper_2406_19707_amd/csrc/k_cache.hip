@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   // A wave's part of LDS: its outputs at the end (rows of D floats and 16 bytes that set their banks apart), until then
   // logits of up to 16 rows, which wait here because a store before every tile's loads is one more thing that the wait
   // for those waits for (one row, 160 pools of 32768: 501 us in all with stores after every tile, 482 so, 436 without).
-  constexpr int LDB = D + 4, LOGIT_BOX = LOGITS && NT == 1 ? 3072 : 0, BOX = RB * LDB > LOGIT_BOX ? RB * LDB : LOGIT_BOX;
+  constexpr int LDB = D + 4, LOGIT_BOX = LOGITS && NT == 1 ? 3200 : 0, BOX = RB * LDB > LOGIT_BOX ? RB * LDB : LOGIT_BOX;
   __shared__ __attribute__((aligned(16))) float boxes[4][BOX];
   __shared__ float box_m[4][RB], box_l[4][RB];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -412,7 +412,7 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
 
     // The 32-token half blocks of the tiles are a pipeline: while the weights of one are worked out on the vector
     // units, the matrix units take the logits of the next and the output of the one before.
-    //   now: logits in, weights out (half block `now_at` of the sequence of tiles); next: the logits of `next_row` ..
+    //   now: logits in, weights out (half `now_half` of tile `now_tile`); next: the logits of rows `next_row` ..
     //   of tile K; out: acc += the weights `old` times rows `old_row` .. of tile V
     auto half_step = [&](auto has_now, auto has_next, auto has_old, const floatx16 &now, int now_tile, int now_half,
                          half8 (&weights)[2], floatx16 &next, const half_t *K, int next_row, const half8 (&old)[2],
