@@ -576,43 +576,46 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
 }
 
 // ---- joining the slices, and the weights of single-token calls ------------------------------------------
-// A workgroup takes 256 / d rows of a pool and, where logits were kept, 1024 slots of it: mass[t] += sum over the
+// A workgroup takes 1024 / d rows of a pool, four elements a thread, and, where logits were kept, 1024 slots of it: mass[t] += sum over the
 // rows of exp2(c s - ref) / sum.  Small calls are a chain of trips through memory, so slices are taken eight at a
 // time, all their loads together, and a slot's weight and first logit are asked for before the sums are known (32 pools of
 // 777 slots, 7 slices: 8.6 -> 3.8 us; 160 pools of 32768: 17 us for 63 MB).
 struct Joined {
-  float ref, sum, out;
+  float ref, sum;
+  floatx4 out;
 };
-// the row's state over all slices, and element e of its output before the division (OUT)
+// the row's state over all slices, and elements e .. e + 3 of its output before the division (OUT)
 template <bool OUT> __device__ __forceinline__ Joined join_row(const StreamArgs &a, int h, const Span &span, int row, int D, int e) {
   constexpr int U = 8;
-  Joined j = {NOTHING_SEEN, 0.f, 0.f};
+  Joined j = {NOTHING_SEEN, 0.f, {0.f, 0.f, 0.f, 0.f}};
   for (int s0 = 0; s0 < span.slices; s0 += U) {
     float2 ml[U];
-    float o[U];
+    floatx4 o[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const long at = ((long)h * a.B * a.slices + span.first + min(s0 + u, span.slices - 1)) * a.R + row;
       ml[u] = a.part_ml[at];
-      if (OUT) o[u] = a.part[at * D + e];
+      if (OUT) o[u] = *reinterpret_cast<const floatx4 *>(a.part + at * D + e);
     }
     float ref = j.ref;
 #pragma unroll
     for (int u = 0; u < U; ++u) ref = fmaxf(ref, ml[u].x);          // (the last slice again and again is the same)
     const float shrink = exp2_fast(j.ref - ref);
-    j.sum *= shrink, j.out *= shrink, j.ref = ref;
+    j.sum *= shrink, j.ref = ref;
+    if (OUT) j.out *= shrink;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float by = s0 + u < span.slices ? exp2_fast(ml[u].x - ref) : 0.f;
-      if (s0 + u < span.slices) j.sum = fmaf(ml[u].y, by, j.sum);
-      if (OUT && s0 + u < span.slices) j.out = fmaf(o[u], by, j.out);
-    }
+    for (int u = 0; u < U; ++u)
+      if (s0 + u < span.slices) {
+        const float by = exp2_fast(ml[u].x - ref);
+        j.sum = fmaf(ml[u].y, by, j.sum);
+        if (OUT) j.out += o[u] * by;
+      }
   }
   return j;
 }
 
 template <typename T, bool LOGITS>
-__global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, int D, FastDiv by_chunks, FastDiv by_D) {
+__global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, int D, FastDiv by_chunks, FastDiv by_fours) {
   constexpr int SLOTS = 1024, U = SLOTS / 256;
   __shared__ float2 stat[32];                              // (LOGITS: R <= 32)
   const int bh = by_chunks.div(blockIdx.x), x = by_chunks.mod(blockIdx.x), tid = threadIdx.x;
@@ -632,12 +635,15 @@ __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, in
     }
   }
   if (a.slices > 1) {
-    const int mine = by_D.div(tid), row = x * by_D.div(256) + mine, e = tid - mine * D;
+    const int mine = by_fours.div(tid), row = x * by_fours.div(256) + mine, e = (tid - mine * (int)by_fours.d) * 4;
     if (row < nq * G) {
       const Joined j = join_row<true>(a, h, span, row, D, e);
       const float inv = inverse_of(j.sum);
       const int iq = a.by_group.div(row), gq = row - iq * G;
-      static_cast<T *>(a.out)[(((long)b * a.n_q + iq) * a.Hq + h * G + gq) * D + e] = (T)(j.out * inv);
+      T v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = (T)(j.out[k] * inv);
+      store_words<(int)sizeof(T)>(static_cast<T *>(a.out) + (((long)b * a.n_q + iq) * a.Hq + h * G + gq) * D + e, v);
       if (a.stats && e == 0) a.stats[(long)bh * a.R + row] = make_float2(j.ref, inv);
     }
   }
@@ -1028,17 +1034,17 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   }
   if (p.slices > 1 || logits) {
     const int chunks = logits && d->N ? div_up(d->N, 1024) : 1;
-    const int rows = p.slices > 1 ? div_up(a.R, 256 / d->d) : 1;
+    const int rows = p.slices > 1 ? div_up(a.R, 1024 / d->d) : 1;
     const FastDiv by_chunks = ig_fast_div(chunks > rows ? chunks : rows);
     const dim3 jgrid((unsigned)(by_chunks.d * BH));
 #define JOIN(T)                                                                                      \
   {                                                                                                  \
     if (logits) {                                                                                    \
       auto k = attend_join<T, true>;                                                                 \
-      IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, c.mass, (int)d->d, by_chunks, ig_fast_div(d->d));                     \
+      IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, c.mass, (int)d->d, by_chunks, ig_fast_div(d->d / 4));                     \
     } else {                                                                                         \
       auto k = attend_join<T, false>;                                                                \
-      IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, (float *)nullptr, (int)d->d, by_chunks, ig_fast_div(d->d));           \
+      IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, (float *)nullptr, (int)d->d, by_chunks, ig_fast_div(d->d / 4));           \
     }                                                                                                \
   }
     if (d->dtype == IG_F16) JOIN(half_t) else JOIN(float)
