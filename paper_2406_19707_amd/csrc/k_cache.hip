@@ -576,46 +576,47 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
 }
 
 // ---- joining the slices, and the weights of single-token calls ------------------------------------------
-// A workgroup takes 1024 / d rows of a pool, four elements a thread, and, where logits were kept, 1024 slots of it: mass[t] += sum over the
-// rows of exp2(c s - ref) / sum.  Small calls are a chain of trips through memory, so slices are taken eight at a
-// time, all their loads together, and a slot's weight and first logit are asked for before the sums are known (32 pools of
-// 777 slots, 7 slices: 8.6 -> 3.8 us; 160 pools of 32768: 17 us for 63 MB).
-struct Joined {
-  float ref, sum;
-  floatx4 out;
+// A workgroup takes 256 E / d rows of a pool, E elements a thread, and, where logits were kept, 1024 slots of it:
+// mass[t] += sum over the rows of exp2(c s - ref) / sum.  Small calls are a chain of trips through memory, so slices are
+// taken eight at a time, all their loads together, and a slot's weight and first logit are asked for before the sums are
+// known (32 pools of 777 slots, 7 slices: 8.6 -> 4.3 us; 160 pools of 32768: 19 us for 63 MB).
+template <int E> struct Joined {
+  float ref, sum, out[E ? E : 1];
 };
-// the row's state over all slices, and elements e .. e + 3 of its output before the division (OUT)
-template <bool OUT> __device__ __forceinline__ Joined join_row(const StreamArgs &a, int h, const Span &span, int row, int D, int e) {
+// the row's state over all slices, and elements e .. e + E - 1 of its output before the division
+template <int E> __device__ __forceinline__ Joined<E> join_row(const StreamArgs &a, int h, const Span &span, int row, int D, int e) {
   constexpr int U = 8;
-  Joined j = {NOTHING_SEEN, 0.f, {0.f, 0.f, 0.f, 0.f}};
+  Joined<E> j = {NOTHING_SEEN, 0.f, {}};
   for (int s0 = 0; s0 < span.slices; s0 += U) {
     float2 ml[U];
-    floatx4 o[U];
+    unsigned o[U][E ? E : 1];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const long at = ((long)h * a.B * a.slices + span.first + min(s0 + u, span.slices - 1)) * a.R + row;
       ml[u] = a.part_ml[at];
-      if (OUT) o[u] = *reinterpret_cast<const floatx4 *>(a.part + at * D + e);
+      if constexpr (E > 0) load_words<E>(a.part + at * D + e, o[u]);
     }
     float ref = j.ref;
 #pragma unroll
     for (int u = 0; u < U; ++u) ref = fmaxf(ref, ml[u].x);          // (the last slice again and again is the same)
     const float shrink = exp2_fast(j.ref - ref);
     j.sum *= shrink, j.ref = ref;
-    if (OUT) j.out *= shrink;
+#pragma unroll
+    for (int k = 0; k < E; ++k) j.out[k] *= shrink;
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (s0 + u < span.slices) {
         const float by = exp2_fast(ml[u].x - ref);
         j.sum = fmaf(ml[u].y, by, j.sum);
-        if (OUT) j.out += o[u] * by;
+#pragma unroll
+        for (int k = 0; k < E; ++k) j.out[k] = fmaf(__uint_as_float(o[u][k]), by, j.out[k]);
       }
   }
   return j;
 }
 
-template <typename T, bool LOGITS>
-__global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, int D, FastDiv by_chunks, FastDiv by_fours) {
+template <typename T, int E, bool LOGITS>
+__global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, int D, FastDiv by_chunks, FastDiv by_threads) {
   constexpr int SLOTS = 1024, U = SLOTS / 256;
   __shared__ float2 stat[32];                              // (LOGITS: R <= 32)
   const int bh = by_chunks.div(blockIdx.x), x = by_chunks.mod(blockIdx.x), tid = threadIdx.x;
@@ -635,22 +636,23 @@ __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, in
     }
   }
   if (a.slices > 1) {
-    const int mine = by_fours.div(tid), row = x * by_fours.div(256) + mine, e = (tid - mine * (int)by_fours.d) * 4;
+    const int mine = by_threads.div(tid), row = x * by_threads.div(256) + mine, e = (tid - mine * (int)by_threads.d) * E;
     if (row < nq * G) {
-      const Joined j = join_row<true>(a, h, span, row, D, e);
+      const Joined<E> j = join_row<E>(a, h, span, row, D, e);
       const float inv = inverse_of(j.sum);
       const int iq = a.by_group.div(row), gq = row - iq * G;
-      T v[4];
+      T *to = static_cast<T *>(a.out) + (((long)b * a.n_q + iq) * a.Hq + h * G + gq) * D + e, v[E];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = (T)(j.out[k] * inv);
-      store_words<(int)sizeof(T)>(static_cast<T *>(a.out) + (((long)b * a.n_q + iq) * a.Hq + h * G + gq) * D + e, v);
+      for (int k = 0; k < E; ++k) v[k] = (T)(j.out[k] * inv);
+      if constexpr (E == 1) *to = v[0];
+      else store_words<E * (int)sizeof(T) / 4>(to, v);
       if (a.stats && e == 0) a.stats[(long)bh * a.R + row] = make_float2(j.ref, inv);
     }
   }
   if (!slots) return;
   if (tid < a.R) {
     if (a.slices > 1) {
-      const Joined j = join_row<false>(a, h, span, tid, D, 0);
+      const Joined<0> j = join_row<0>(a, h, span, tid, D, 0);
       stat[tid] = make_float2(j.ref, inverse_of(j.sum));
     } else {
       stat[tid] = a.stats[(long)bh * a.R + tid];
@@ -906,9 +908,9 @@ int row_block(const ig_desc *d, long R) { return R <= 16 || d->d > 128 ? 16 : 32
 bool many_rows(const ig_desc *d, long R) { return d->dtype == IG_F16 && R > (d->d > 128 ? 16 : 32); }
 
 // The same for attend_prompt.  Eight waves, two tiles ahead, where most of what the rows see is seen by all of them and
-// there are rows for more than four (317 x 4 query rows over up to 9001: 225 against 235 us, trees of 63 x 4 nodes over 8191: 97
-// against 106, before slices went by length); four for prompts, where a block of 256 rows works out more that its first rows do not see (2048 over 2048:
-// 397 against 367 us).
+// there are rows for more than four (317 x 4 query rows over up to 9001: 225 against 235 us, trees of 63 x 4 nodes over
+// 8191: 97 against 106, before slices went by length); four for prompts, where a block of 256 rows works out more that its
+// first rows do not see (2048 over 2048: 397 against 367 us).
 int prompt_rows(const ig_desc *d, const CacheCall &c) {
   return d->d >= 64 && d->d <= 128 && (long)c.n_q * c.group > 128 && (c.k_tree || 2 * (long)c.n_q <= d->N) ? 256 : 128;
 }
@@ -1034,18 +1036,23 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   }
   if (p.slices > 1 || logits) {
     const int chunks = logits && d->N ? div_up(d->N, 1024) : 1;
-    const int rows = p.slices > 1 ? div_up(a.R, 1024 / d->d) : 1;
-    const FastDiv by_chunks = ig_fast_div(chunks > rows ? chunks : rows);
+    // four elements a thread where that leaves workgroups for two a compute unit (a chunk of 317 x 4 rows, 32 pools: 38 us
+    // with one, 15 with four), one where the trip through memory is what takes the time (13 rows, 32 pools: 4.2 us with
+    // four, 3.2 with one; a call for one token over 777 slots 11.0 and 10.3)
+    const int E = !logits && BH * div_up(a.R, 1024 / d->d) >= 512 ? 4 : 1;
+    const int rows = p.slices > 1 ? div_up(a.R, 256 * E / d->d) : 1;
+    const FastDiv by_chunks = ig_fast_div(chunks > rows ? chunks : rows), by_threads = ig_fast_div(d->d / E);
     const dim3 jgrid((unsigned)(by_chunks.d * BH));
+#define JOIN_AS(T, E, LOGITS)                                                                        \
+  {                                                                                                  \
+    auto k = attend_join<T, E, LOGITS>;                                                              \
+    IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, c.mass, (int)d->d, by_chunks, by_threads);\
+  }
 #define JOIN(T)                                                                                      \
   {                                                                                                  \
-    if (logits) {                                                                                    \
-      auto k = attend_join<T, true>;                                                                 \
-      IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, c.mass, (int)d->d, by_chunks, ig_fast_div(d->d / 4));                     \
-    } else {                                                                                         \
-      auto k = attend_join<T, false>;                                                                \
-      IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, (float *)nullptr, (int)d->d, by_chunks, ig_fast_div(d->d / 4));           \
-    }                                                                                                \
+    if (logits) JOIN_AS(T, 1, true)                                                                  \
+    else if (E == 4) JOIN_AS(T, 4, false)                                                            \
+    else JOIN_AS(T, 1, false)                                                                        \
   }
     if (d->dtype == IG_F16) JOIN(half_t) else JOIN(float)
   }
