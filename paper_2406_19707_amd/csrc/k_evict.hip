@@ -1,15 +1,18 @@
 // Eviction of a pool's slots by accumulated attention weight (Section 5.3: the cache of a fixed budget that the
 // rehearsal is compared with), and the append of several rows to ragged sequences.
+#include <type_traits>
+
 #include "cache_device.h"
 
 namespace {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-// order-preserving image of a weight: larger <-> larger unsigned, -0 as +0, NaN below everything
+// order-preserving image of a weight: larger <-> larger unsigned, -0 as +0, NaN below everything; between 1 and +inf's
+// 0xff800000, so that 0 and ~0u are left for slots that are ranked without their weight
 __device__ __forceinline__ unsigned weight_key(float s) {
   const unsigned b = __float_as_uint(s + 0.0f);
-  return s != s ? 0u : ((b & 0x80000000u) ? ~b : (b | 0x80000000u));
+  return s != s ? 1u : ((b & 0x80000000u) ? ~b : (b | 0x80000000u));
 }
 
 struct EvictArgs {
@@ -89,18 +92,31 @@ __global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a) {
   const int chunk = KPT > 0 ? KPT * 64 : ((n + THREADS - 1) / THREADS) * 64;
   const int t0 = min(n, w * chunk), t1 = min(n, t0 + chunk);
   unsigned key[U];
-  auto load = [&](int t) {
-    float m[U];
-    int age[U];
+  // (protected slots rank before all others; where there are more of them than may stay, they alone are ranked)
+  bool crowded = false;
+  unsigned apart = ~0u;                                   // the key of slots that are decided without their weight
+  auto load = [&](int t, auto together) {                 // so many at a time
+    constexpr int P = decltype(together)::value;
 #pragma unroll
-    for (int i = 0; i < U; ++i) m[i] = mass[min(t + i * 64 + lane, n - 1)];
-    if (a.protect_from) {
+    for (int i0 = 0; i0 < U; i0 += P) {
+      float m[P];
+      int age[P];
+      if (P < U) t = (int)opaque(t);                      // (not all addresses ahead)
 #pragma unroll
-      for (int i = 0; i < U; ++i) age[i] = born[min(t + i * 64 + lane, n - 1)];
+      for (int i = 0; i < P; ++i) m[i] = mass[min(t + (i0 + i) * 64 + lane, n - 1)];
+      if (a.protect_from) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) age[i] = born[min(t + (i0 + i) * 64 + lane, n - 1)];
+      }
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const bool safe = a.protect_from && age[i] >= guard;
+        key[i0 + i] = safe == crowded ? weight_key(m[i]) : apart;
+        if (P < U) keep_here(key[i0 + i]);
+      }
     }
-#pragma unroll
-    for (int i = 0; i < U; ++i) key[i] = a.protect_from && age[i] >= guard ? ~0u : weight_key(m[i]);
   };
+  typedef std::integral_constant<int, U> all_of_them;
   // f(slot, its key, whether there is such a slot) in order of the slots, 64 a call
   auto each = [&](auto &&f) {
     if constexpr (KPT > 0) {
@@ -108,13 +124,13 @@ __global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a) {
       for (int i = 0; i < U; ++i) f(t0 + i * 64 + lane, key[i], t0 + i * 64 + lane < t1);
     } else {
       for (int t = t0; t < t1; t += U * 64) {
-        load(t);
+        load(t, all_of_them());
 #pragma unroll
         for (int i = 0; i < U; ++i) f(t + i * 64 + lane, key[i], t + i * 64 + lane < t1);
       }
     }
   };
-  if constexpr (KPT > 0) load(t0);
+  if constexpr (KPT > 0) load(t0, all_of_them());
   for (int i = tid; i < 3 * RADIX_WORDS / 4; i += THREADS) reinterpret_cast<uint4 *>(&hist[0][0])[i] = make_uint4(0, 0, 0, 0);
   // The protected slots, which all have one key, are counted by ballots and left out of the histograms, where whole
   // waves of them would add to one word.
@@ -129,15 +145,21 @@ __global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a) {
   // slots with a key above lim stay, and the first `need` of those equal to it
   unsigned lim = 0;
   int need = a.keep - safe;
-  if (need <= 0) {                                        // (no room for others: the first `keep` of the protected)
+  if (need == 0) {                                        // (the protected slots, all of them, and no others)
     lim = ~0u;
     need = a.keep;
+  } else if (need < 0) {
+    crowded = true;
+    apart = 0;
+    need = a.keep;
+    // (four at a time: all together need registers that the other path has not)
+    if constexpr (KPT > 0) load(t0, std::integral_constant<int, 4>());
   }
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     if (lim == ~0u && pass == 0) break;
     each([&](int, unsigned k, bool there) {
-      if (there && k != ~0u) radix_add(hist[pass], pass, k, lim);
+      if (there && k != apart) radix_add(hist[pass], pass, k, lim);
     });
     __syncthreads();
     bool whole;
@@ -200,13 +222,12 @@ __global__ __launch_bounds__(THREADS) void evict_select(EvictArgs a) {
   if constexpr (MOVE) move_rows<T, THREADS>(a, bh, from, to, 0, total);
 }
 
-// The eviction of a decode step, one slot too many (N = keep + 1): the slot with the smallest key, the highest of
-// equal ones, makes room for the last slot.  Bound by the trips through memory: the last slot's rows, weight and
+// The eviction of a decode step, one slot too many (N = keep + 1): the slot that ranks last makes room for the last
+// slot.  Bound by the trips through memory: the last slot's rows, weight and
 // position are asked for with the weights.  256 pools of 2049 slots: 5.2 us, 10.1 with the radix selection.
 template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void evict_one(EvictArgs a) {
   constexpr int NW = THREADS / 64, U = 8, TILE = IG_WAVE * SlabElem<T>::TPL;
-  __shared__ unsigned w_key[NW];
-  __shared__ int w_slot[NW];
+  __shared__ unsigned long long w_best[NW];
   const int bh = blockIdx.x, b = a.by_H.div(bh), tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int n = length_of(a.kv_len, b, a.N, a.N_cap), last = a.keep;
   float *mass = a.mass + (long)bh * a.N_cap;
@@ -221,8 +242,11 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void ev
   }
   const float last_mass = mass[last];
   const int last_born = born ? born[last] : 0;
-  unsigned best = ~0u;
-  int slot = -1;
+  // protection, weight and, in reverse, slot: the smallest goes
+  auto rank_of = [](bool safe, unsigned key, int s) {
+    return (unsigned long long)safe << 63 | (unsigned long long)key << 31 | (unsigned)(0x7fffffff - s);
+  };
+  unsigned long long best = ~0ull;
   for (int t0 = tid; t0 < a.N; t0 += THREADS * U) {
     float m[U];
     int age[U];
@@ -235,19 +259,20 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void ev
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int t = t0 + i * THREADS;
-      const unsigned key = a.protect_from && age[i] >= guard ? ~0u : weight_key(m[i]);
-      if (t <= last && key <= best) best = key, slot = t;           // (a thread's slots come in ascending order)
+      const unsigned long long rank = rank_of(a.protect_from && age[i] >= guard, weight_key(m[i]), t);
+      if (t <= last && rank < best) best = rank;
     }
   }
-  auto lower = [&](unsigned key, int s) {
-    if (key < best || (key == best && s > slot)) best = key, slot = s;
-  };
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) lower(__shfl_xor(best, o, 64), __shfl_xor(slot, o, 64));
-  if (lane == 0) w_key[w] = best, w_slot[w] = slot;
+  for (int o = 32; o >= 1; o >>= 1) {
+    const unsigned long long other = __shfl_xor(best, o, 64);
+    best = other < best ? other : best;
+  }
+  if (lane == 0) w_best[w] = best;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < NW; ++i) lower(w_key[i], w_slot[i]);
+  for (int i = 0; i < NW; ++i) best = w_best[i] < best ? w_best[i] : best;
+  const int slot = 0x7fffffff - (int)(best & 0x7fffffff);
   if (n <= a.keep || slot == last) return;         // nothing too many, or the last slot itself goes
   if (copies) {
     K[(long)slot * a.units + tid] = kv;
