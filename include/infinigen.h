@@ -399,6 +399,10 @@ int ig_gather_attention(ig_ctx *ctx, const ig_desc *desc, const void *q, const v
  *  - Rows of the valid slots and of nodes that some node sees are expected to be finite (an infinity or a
  *    NaN among them may reach rows that do not see it) and logits above -6e29.  What lies in other slots and
  *    nodes, and in query rows behind the last one, is never used, whatever it holds.
+ *  - Logits, softmax sums, `mass` and the sum over V are float32.  With IG_F16 the weights are rounded to half
+ *    precision where they multiply V (not in the sums): by at most 2^-11 of themselves down to 2^-23 of a row's
+ *    largest weight (calls of up to 16 query rows a pool: 2^-28), by at most 2^-34 of the largest below that
+ *    (for logits below 10^4; beyond, a larger share of the weights is below, and from 2^22 on that is 2^-25).
  *  - out must not overlap the inputs (IG_EINVAL).  At most 2^26 query rows (B * H * group * tokens; rows to
  *    append likewise) and 2^24 elements of a token (H * group * d), IG_ESHAPE otherwise.
  *  - mass: device float32 [B*H, N_cap], one sum per slot, zero-initialised by the caller.  born: device

@@ -28,6 +28,13 @@ struct StreamArgs {
 // that has seen nothing has NOTHING_SEEN, against which every weight is zero, and a sum of zero.
 constexpr float NOTHING_SEEN = -1e30f;
 
+// The reference for a largest c s of `top`: `lift` below it where weights are rounded to half precision, whose range above
+// one would else lie idle while small weights lose their bits.  Less for logits of 2^20 and more, where the reference's own
+// rounding (2^-24 of it) could carry a weight out of that range, and none from 2^22 on.
+__device__ __forceinline__ float lifted(float top, float lift) {
+  return lift == 0.f ? top : fmaf(-lift, __builtin_amdgcn_fmed3f(fmaf(fabsf(top), -0x1p-22f, 1.f), 0.f, 1.f), top);
+}
+
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 

@@ -20,8 +20,9 @@ namespace {
 //  - a lane loads the same CJ = d/16 channels of those eight V rows (a wave-wide load is four whole rows), and
 //    one byte permute each makes from them the pairs of tokens that V^T wants; row i of the output's block j is
 //    the channel CJ i + j.
-// Logits, weights' sums and outputs are float32; the weights are rounded to half precision for the second product,
-// relative to at most 2^-11 each, as the output is in the end.
+// Logits, weights' sums and outputs are float32; in half precision the weights are rounded for the second product, which
+// takes no other type at its rate: by at most 2^-11 of themselves, as the output is in the end, where they are above 2^-28 of
+// the row's largest (LIFT), and by at most 2^-39 of it below.
 // Bound by memory: one token of 16 x 32 heads over 4096 slots 176 us = 6.1 TB/s, of 4 x 40 over 32768 437 us = 6.2 TB/s,
 // float32 8 x 32 over 4096 180 us = 6.0 (a copy of 4 GiB: 4.8 TB/s, a read of as much 6.2 at best); 16 nodes over 4096, 128
 // pools, 53 us = 5.1.  Small calls are the trips through memory in turn: 32 pools of 777, 5.3 us.
@@ -30,6 +31,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   constexpr bool HALF = sizeof(T) == 2;
   constexpr int TT = HALF ? 32 : 16, MT = TT / 16, CJ = D / 16, RB = 16 * NT;
   constexpr int KCH = D * (int)sizeof(T) / 64;            // 16-byte pieces of a row that a lane holds
+  constexpr float LIFT = HALF ? 14.f : 0.f;               // (weights up to 2^14, half precision reaches 2^15)
   constexpr int VT = HALF ? 8 : 4;                        // tokens of a tile that a lane group supplies
   constexpr int VW = CJ * (int)sizeof(T) / 4;             // words of a V row that a lane holds
   // A wave's part of LDS: its outputs at the end (rows of D floats and 16 bytes that set their banks apart), until then
@@ -212,7 +214,7 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, s[n][m][r]);
       top = column_max(top);
-      const float ref = fmaxf(m_run[n], top * a.c);
+      const float ref = fmaxf(m_run[n], lifted(top * a.c, LIFT));
       if (__any(ref > m_run[n])) {
         const float shrink = exp2_fast(m_run[n] - ref);
         l_run[n] *= shrink;
@@ -307,12 +309,13 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
 // so that a query row is one lane of each half wave.  The accumulator of a 32-token block holds, in half h, the
 // tokens 8 x + 4 h + 0 .. 3; P^T takes them in that order, and V^T is read through LDS's transposing loads in the
 // same one, so the weights never leave their lane.
-// The reference of a row's weights only moves when its largest logit passes it by RISE (weights up to 2^RISE, far
-// inside half precision): the row's output, 16 registers for every 32 channels, is then scaled only now and then.
+// The reference of a row's weights only moves when its largest logit has risen by RISE: the row's output, 16 registers for
+// every 32 channels, is then scaled only now and then.  It lies LIFT below that logit, so that weights reach 2^15 at most, and
+// those above 2^-23 of the largest keep all of half precision's bits (below: to 2^-34 of it).
 // Bound by the vector and matrix units together: 8 x 32 heads of 2048 tokens, d = 128, 355 us = 775 TFLOP/s of what is
 // seen (a library product of 8192 squared reaches 1107), the matrix units busy for 0.41 of the cycles and the vector units
 // for 0.52; d = 64 207 us, d = 256 and half the heads 433 us.  One half block after the other, row blocks not in pairs: 443 us.
-constexpr float RISE = 6.f;
+constexpr float RISE = 6.f, PROMPT_LIFT = 9.f;
 constexpr int PROMPT_KEYS = 64;
 
 template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void attend_prompt(StreamArgs a) {
@@ -456,7 +459,7 @@ template <int D, int NW, bool TREE> __global__ __launch_bounds__(NW * 64, D <= 1
         float top = s[0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) top = __builtin_elementwise_maximum(top, s[e]);
-        top = both_max(top) * a.c;
+        top = lifted(both_max(top) * a.c, PROMPT_LIFT);
         const float to = top > ref + RISE ? top : ref;
         rises = __any(to != ref);
         shrink = exp2_fast(ref - to);
