@@ -397,8 +397,8 @@ int ig_gather_attention(ig_ctx *ctx, const ig_desc *desc, const void *q, const v
  *  - kv_len: device int32 [B], valid slots of each sequence, or NULL: N for all.  Clamped to [0, N]; N
  *    is the largest length the call may meet and sizes its grid.  N = 0 is allowed.
  *  - Rows of the valid slots and of nodes that some node sees are expected to be finite (an infinity or a
- *    NaN among them may reach rows that do not see it) and logits above -6e29.  What lies in other slots and
- *    nodes, and in query rows behind the last one, is never used, whatever it holds.
+ *    NaN among them may reach rows that do not see it) and logits between -1e8 and 1e8.  What lies in other
+ *    slots and nodes, and in query rows behind the last one, is never used, whatever it holds.
  *  - Logits, softmax sums, `mass` and the sum over V are float32.  With IG_F16 the weights are rounded to half
  *    precision where they multiply V (not in the sums): by at most 2^-11 of themselves down to 2^-23 of a row's
  *    largest weight (calls of up to 16 query rows a pool: 2^-28), by at most 2^-34 of the largest below that
