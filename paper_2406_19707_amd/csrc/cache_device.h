@@ -241,6 +241,14 @@ template <int LEFT> __device__ __forceinline__ void wait_for_lds_loads() {      
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory");
 }
 
+// Between lanes of one wave that write LDS and others of it that read there (or the other way round): a wave's accesses to
+// LDS are done in their order, so nothing waits, but the compiler must not change that order.
+__device__ __forceinline__ void lanes_exchange() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // the other half wave's value and this one's: both in both
 __device__ __forceinline__ float both_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);

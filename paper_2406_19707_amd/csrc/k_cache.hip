@@ -189,12 +189,14 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
       ++kept;
       if (!more || (kept + 1) * a.R * TT > LOGIT_BOX) {
         // (in the order the rows were written: R rows of a tile, then the wave's next tile)
+        lanes_exchange();
         for (int u = lane; u < kept * a.R * (TT / 4); u += 64) {
           const int kr = u / (TT / 4), x = a.by_group.div(kr);       // (one query a sequence: R = group)
           *reinterpret_cast<floatx4 *>(a.logits + ((long)bh * a.R + kr - x * a.R) * a.logits_ld +
                                        (long)(tile - 4 * (kept - 1 - x)) * TT + u % (TT / 4) * 4) =
               *reinterpret_cast<const floatx4 *>(boxes[w] + u * 4);
         }
+        lanes_exchange();                                 // (the box is written again, by the next tile or by the outputs)
         kept = 0;
       }
     } else if constexpr (LOGITS) {
