@@ -956,13 +956,16 @@ static bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes
   return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
 }
 
-// The descriptor of a call over whole pools: a cache without a token is allowed, group query heads share a pool.
-static int check_cache(ig_ctx *ctx, const ig_desc *d, const char *what, int group, int n_q, bool attends, void *stream) {
+// The descriptor of a call over whole pools: a cache without a token is allowed, group query heads share a pool, r
+// counts only where there is a slab, alpha and rope nowhere.
+static int check_cache(ig_ctx *ctx, const ig_desc *d, const char *what, int group, int n_q, bool attends, bool slab, void *stream) {
   if (!ctx) return IG_EINVAL;
   ctx->call_stream = (hipStream_t)stream;
   if (!d) return ig_fail(ctx, IG_EINVAL, "descriptor is NULL");
   ig_desc one = *d;
   if (one.N == 0 && one.N_cap >= 1) one.N = 1;
+  if (!slab) one.r = 1;
+  one.alpha = 0.f, one.rope = 0;
   if (int rc = check_desc(ctx, &one)) return rc;
   if (group < 1 || n_q < 1) return ig_fail(ctx, IG_ESHAPE, "%s: group = %d, %d tokens", what, group, n_q);
   // (row and workgroup numbers are 32-bit; a pool has at most n_q * group rows and 64 slices of each 16 of them)
@@ -978,7 +981,7 @@ static int check_cache(ig_ctx *ctx, const ig_desc *d, const char *what, int grou
 }
 
 int ig_reserve_cache(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_q) {
-  int rc = check_cache(ctx, d, "ig_reserve_cache", group, n_q, false, nullptr);
+  int rc = check_cache(ctx, d, "ig_reserve_cache", group, n_q, false, false, nullptr);
   if (rc) return rc;
   if ((rc = set_device(ctx))) return rc;
   return ig_ensure(ctx, (void **)&ctx->cache_ws, &ctx->cache_ws_bytes, ig_cache_reserve_bytes(d, group, n_q));
@@ -1002,7 +1005,7 @@ static int attend_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, void 
 int ig_cache_attention(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_q, const void *q, const int32_t *q_len,
                        const void *Kpool, const void *Vpool, const int32_t *kv_len, float *mass, void *out,
                        void *stream) {
-  int rc = check_cache(ctx, d, "ig_cache_attention", group, n_q, true, stream);
+  int rc = check_cache(ctx, d, "ig_cache_attention", group, n_q, true, false, stream);
   if (rc) return rc;
   if (!q || !Kpool || !Vpool || !out) return ig_fail(ctx, IG_EINVAL, "ig_cache_attention: NULL argument");
   if ((rc = check_aligned(ctx, "ig_cache_attention", {q, Kpool, Vpool, out}))) return rc;
@@ -1012,7 +1015,7 @@ int ig_cache_attention(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_q
 int ig_tree_attention(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_tree, const void *q, const void *k_tree,
                       const void *v_tree, const uint64_t *visible, const int32_t *tree_len, const void *Kpool,
                       const void *Vpool, const int32_t *kv_len, void *out, void *stream) {
-  int rc = check_cache(ctx, d, "ig_tree_attention", group, n_tree, true, stream);
+  int rc = check_cache(ctx, d, "ig_tree_attention", group, n_tree, true, false, stream);
   if (rc) return rc;
   if (n_tree > 64) return ig_fail(ctx, IG_ESHAPE, "ig_tree_attention: %d nodes, at most 64", n_tree);
   if (!q || !k_tree || !v_tree || !visible || !Kpool || !Vpool || !out)
@@ -1027,7 +1030,7 @@ int ig_append_rows(ig_ctx *ctx, const ig_desc *d, int32_t n_rows, const void *k_
                    const int32_t *path, const int32_t *n_append, const int32_t *kv_len, const int32_t *pos,
                    const int32_t *idx_dev, void *slab, void *Kpool, void *Vpool, float *mass, int32_t *born,
                    void *stream) {
-  int rc = check_cache(ctx, d, "ig_append_rows", 1, n_rows, false, stream);
+  int rc = check_cache(ctx, d, "ig_append_rows", 1, n_rows, false, slab != nullptr, stream);
   if (rc) return rc;
   if (!k_rows || !v_rows || !Kpool || !Vpool) return ig_fail(ctx, IG_EINVAL, "ig_append_rows: NULL argument");
   if (slab && !idx_dev) return ig_fail(ctx, IG_EINVAL, "ig_append_rows: a slab needs idx_dev");
@@ -1045,7 +1048,7 @@ int ig_append_rows(ig_ctx *ctx, const ig_desc *d, int32_t n_rows, const void *k_
 int ig_pool_evict(ig_ctx *ctx, const ig_desc *d, int32_t keep, const int32_t *kv_len, float *mass, int32_t *born,
                   const int32_t *protect_from, const int32_t *idx_dev, void *slab, void *Kpool, void *Vpool,
                   void *stream) {
-  int rc = check_cache(ctx, d, "ig_pool_evict", 1, 1, false, stream);
+  int rc = check_cache(ctx, d, "ig_pool_evict", 1, 1, false, slab != nullptr, stream);
   if (rc) return rc;
   if (keep < 1) return ig_fail(ctx, IG_ESHAPE, "ig_pool_evict: keep = %d", keep);
   if (!mass || !Kpool || !Vpool) return ig_fail(ctx, IG_EINVAL, "ig_pool_evict: NULL argument");
