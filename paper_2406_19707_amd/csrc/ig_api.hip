@@ -988,13 +988,15 @@ int ig_reserve_cache(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_q) 
 }
 
 static int attend_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, void *stream) {
-  // (queries are read again after the first rows are out, pools by every row)
+  // (queries, masks and lengths are read again after the first rows are out, pools by every row; the weights are another output)
   const size_t row = (size_t)d->d * ig_elem_bytes(d->dtype), q_bytes = (size_t)d->B * c.n_q * d->H * c.group * row;
   const size_t pool_bytes = (size_t)d->B * d->H * d->N_cap * row, tree_bytes = (size_t)d->B * c.n_q * d->H * row;
-  const struct { const void *p; size_t n; } in[] = {{c.q, q_bytes}, {c.K, pool_bytes}, {c.V, pool_bytes}, {c.k_tree, tree_bytes}, {c.v_tree, tree_bytes}};
-  for (const auto &x : in)
-    if (x.p && overlap(c.out, q_bytes, x.p, x.n))
-      return ig_fail(ctx, IG_EINVAL, "out must not overlap the queries, keys or values");
+  const struct { const void *p; size_t n; } others[] = {
+      {c.q, q_bytes}, {c.K, pool_bytes}, {c.V, pool_bytes}, {c.k_tree, tree_bytes}, {c.v_tree, tree_bytes},
+      {c.visible, (size_t)d->B * c.n_q * sizeof(uint64_t)}, {c.q_len, d->B * sizeof(int32_t)}, {c.kv_len, d->B * sizeof(int32_t)},
+      {c.mass, (size_t)d->B * d->H * d->N_cap * sizeof(float)}};
+  for (const auto &x : others)
+    if (x.p && overlap(c.out, q_bytes, x.p, x.n)) return ig_fail(ctx, IG_EINVAL, "out must not overlap the inputs or mass");
   int rc = set_device(ctx);
   if (rc) return rc;
   const CachePlan p = ig_cache_plan(d, c);

@@ -60,3 +60,31 @@ def test_a_slab_needs_its_channels(ctx, r):
     idx, slab, mass = i32([0]), torch.zeros(1 << 16, dtype=torch.uint8, device="cuda"), torch.zeros((1, 16), device="cuda")
     refused(ig.IG_ESHAPE, ctx.ig_append_rows, ds, 1, x, x, None, None, None, None, idx, slab, K, V)
     refused(ig.IG_ESHAPE, ctx.ig_pool_evict, ds, 4, None, mass, None, None, idx, slab, K, V)
+
+
+def test_out_apart_from_every_input(ctx):
+    """The masks, the lengths and the weights too."""
+    B, H, d, N = 2, 2, 64, 16
+    ds = desc(B, H, d, N, N, "f16")
+    K, V = pools(B, H, d, N, "f16", [N] * B, 1)
+    q, kt = rows((B, 4, H, d), "f16", 2), rows((B, 4, H, d), "f16", 3)
+    out = torch.full_like(q, SENTINEL)
+    inside = out.view(-1)[64:]                     # 16-byte aligned, and in the output's last bytes
+    ends = out.view(-1)[-8:]
+    bits = torch.zeros((B, 4), dtype=torch.int64, device="cuda")
+    lens, mass = i32([1, 1]), torch.zeros((B * H, N), device="cuda")
+    for at in (inside, ends, out.data_ptr() - 4):
+        refused(ig.IG_EINVAL, ctx.ig_cache_attention, ds, 1, 4, q, at, K, V, lens, mass, out)
+        refused(ig.IG_EINVAL, ctx.ig_cache_attention, ds, 1, 4, q, lens, K, V, at, mass, out)
+        refused(ig.IG_EINVAL, ctx.ig_cache_attention, ds, 1, 4, q, lens, K, V, lens, at, out)
+        refused(ig.IG_EINVAL, ctx.ig_tree_attention, ds, 1, 4, q, kt, kt, bits, at, K, V, lens, out)
+        refused(ig.IG_EINVAL, ctx.ig_tree_attention, ds, 1, 4, q, kt, kt, bits, lens, K, V, at, out)
+    for at in (inside, ends, out.data_ptr() - 8):
+        refused(ig.IG_EINVAL, ctx.ig_tree_attention, ds, 1, 4, q, kt, kt, at, lens, K, V, lens, out)
+    torch.cuda.synchronize()
+    assert (out == SENTINEL).all()
+    # next to each other is apart
+    both = torch.zeros(out.numel() * 2 + B * H * N * 4, dtype=torch.uint8, device="cuda")
+    o, m = both[:out.numel() * 2], both[out.numel() * 2:]
+    ctx.ig_cache_attention(ds, 1, 4, q, None, K, V, None, m, o)
+    torch.cuda.synchronize()
