@@ -959,6 +959,8 @@ CachePlan ig_cache_plan(const ig_desc *d, const CacheCall &c) {
     return here;
   };
   p.logits_ld = ((long)d->N + 63) / 64 * 64;
+  const int mass_block = d->dtype == IG_F16 ? MASS_KEYS : (d->d <= 128 ? mass_keys<128>() : mass_keys<256>());
+  p.mass_groups = c.mass && !keeps_logits(c, p) ? BH * div_up(d->N, mass_block) : 0;
   p.stats_at = take(c.mass ? BH * R * sizeof(float2) : 0);
   p.part_ml_at = take(p.slices > 1 ? BH * p.slices * R * sizeof(float2) : 0);
   p.part_at = take(p.slices > 1 ? BH * p.slices * R * d->d * sizeof(float) : 0);

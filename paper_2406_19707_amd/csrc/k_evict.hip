@@ -364,8 +364,11 @@ template <typename T> __global__ __launch_bounds__(256) void append_rows(AppendA
 }
 
 int most_moves(const ig_desc *d, int keep) { return keep < d->N - keep ? keep : d->N - keep; }
+int move_chunks(const ig_desc *d, int keep) { return (most_moves(d, keep) + MOVE_ROWS - 1) / MOVE_ROWS; }
 
 }  // namespace
+
+long ig_evict_move_groups(const ig_desc *d, int keep) { return d->N <= keep ? 0 : d->B * (long)d->H * move_chunks(d, keep); }
 
 size_t ig_evict_workspace(const ig_desc *d, int keep) {
   return (size_t)d->B * d->H * (1 + 2 * (size_t)most_moves(d, keep)) * sizeof(int32_t);
@@ -382,7 +385,7 @@ int ig_launch_evict(ig_ctx *ctx, const ig_desc *d, int keep, const int32_t *kv_l
   a.H = d->H, a.N = d->N, a.N_cap = d->N_cap, a.keep = keep, a.most = most_moves(d, keep);
   a.units = d->d * ig_elem_bytes(d->dtype) / 16, a.d = d->d, a.r = d->r, a.nTiles = (d->N_cap + tile - 1) / tile;
   a.by_H = ig_fast_div(d->H), a.by_units = ig_fast_div(a.units);
-  a.by_chunks = ig_fast_div((a.most + MOVE_ROWS - 1) / MOVE_ROWS);
+  a.by_chunks = ig_fast_div(move_chunks(d, keep));
   const bool one = a.most <= 16;         // few rows a pool: moved by the workgroup that found them
   if (d->N == keep + 1 && a.units <= 256) {
     // (256 threads take 8 slots each of 2048; the long pools' 1024 as many of 8192)
