@@ -36,7 +36,6 @@ __device__ __forceinline__ float lifted(float top, float lift) {
 }
 
 typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 
 // Workgroups go to the eight XCDs in turn; this gives every XCD one contiguous run of the work, so that what
 // shares keys and values shares an L2.
@@ -157,20 +156,15 @@ template <int W> __device__ __forceinline__ void load_words(const void *from, un
   }
 }
 template <int W, typename T, int N> __device__ __forceinline__ void store_words(void *to, const T (&from)[N]) {
-  static_assert(W * 4 == N * sizeof(T), "whole words");
-  if constexpr (W == 1) {
-    struct one { unsigned v; };
-    *static_cast<unsigned *>(to) = __builtin_bit_cast(unsigned, half2v{(half_t)from[0], (half_t)from[1]});
-  } else {
-    typedef T vecT __attribute__((ext_vector_type(W == 2 ? 8 / sizeof(T) : 16 / sizeof(T))));
-    constexpr int PER = sizeof(vecT) / sizeof(T);
+  static_assert(W * 4 == N * sizeof(T) && W >= 2, "whole words, two or more");
+  typedef T vecT __attribute__((ext_vector_type(W == 2 ? 8 / sizeof(T) : 16 / sizeof(T))));
+  constexpr int PER = sizeof(vecT) / sizeof(T);
 #pragma unroll
-    for (int i = 0; i < N / PER; ++i) {
-      vecT x;
+  for (int i = 0; i < N / PER; ++i) {
+    vecT x;
 #pragma unroll
-      for (int e = 0; e < PER; ++e) x[e] = from[i * PER + e];
-      static_cast<vecT *>(to)[i] = x;
-    }
+    for (int e = 0; e < PER; ++e) x[e] = from[i * PER + e];
+    static_cast<vecT *>(to)[i] = x;
   }
 }
 

@@ -986,7 +986,8 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   a.logits = reinterpret_cast<float *>(ws + p.logits_at);
   a.logits_ld = p.logits_ld;
   // a causal call with workgroups to spare: each takes a late and an early row block, so that all take equally long
-  a.paired = p.prompt && !tree && p.slices == 1 && BH * p.nrb >= (p.rb == 256 ? 512 : 1024) && 2 * c.n_q > d->N;
+  // (blocks of 128 rows: prompt_rows)
+  a.paired = p.prompt && !tree && p.slices == 1 && BH * p.nrb >= 1024 && 2 * c.n_q > d->N;
   const int units = a.paired ? (p.nrb + 1) / 2 : p.nrb;
   a.by_units = ig_fast_div(units), a.by_pair = ig_fast_div(d->B * p.slices * units);
   a.total = (int)(BH * p.slices * units), a.per_xcd = div_up(a.total, 8);
