@@ -225,10 +225,14 @@ template <int D> __device__ __forceinline__ uint2 column_rows(const half_t *rows
 // of `to` (from and to the same in all lanes).  Not the compiler's builtin, because it waits for every such load
 // before any transposing read, also of other LDS; nothing is written but LDS, and who reads it waits
 // (wait_for_lds_loads, then a barrier where other waves loaded part of it).
+// The compiler does not see what the instruction needs: one wait state after a write of m0, and five after a vector
+// instruction (a spilled register's return, say) wrote the address.  The address goes through a scalar move, which is the one
+// and for which the hardware itself waits in place of the others.
 __device__ __forceinline__ void load_to_lds(const void *from, unsigned offset, half_t *to) {
   const unsigned at = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)to;
   const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)from), hi = __builtin_amdgcn_readfirstlane((unsigned)((uintptr_t)from >> 32));
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(__builtin_amdgcn_readfirstlane(at)), "v"(offset),
+  unsigned long long moved;
+  asm volatile("s_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0" : "=&s"(moved) : "{m0}"(__builtin_amdgcn_readfirstlane(at)), "v"(offset),
                "s"((unsigned long long)hi << 32 | lo) : "memory");
 }
 template <int LEFT> __device__ __forceinline__ void wait_for_lds_loads() {      // all but the newest LEFT
