@@ -12,6 +12,7 @@ struct StreamArgs {
   int n_q, R, Hq, N, N_cap;           // R = n_q * group query rows share a pool
   int nrb, slices, total, per_xcd;    // row blocks and slices of a pool, workgroups in all and of one XCD
   int paired;                         // attend_prompt: a workgroup takes two row blocks
+  int turn_shift;                     // a workgroup takes 64 << turn_shift slots a turn
   int B, H;
   FastDiv by_pair, by_units;          // workgroups of a head (prompt_mass: of a pool), of a slice
   FastDiv by_slices, by_H, by_group;
@@ -47,10 +48,11 @@ __device__ __forceinline__ int length_of(const int32_t *len, int b, int all, int
 }
 // ---- which slices are whose --------------------------------------------------------------------------------
 // The B * slices slices of a head are dealt to the sequences by their lengths: one each, and of the others as many as the
-// sequence's share of all slots, rounded down; what is left over stays empty.  (Without lengths from the caller that is
-// `slices` each.)  So a batch of ragged sequences keeps no workgroup waiting for the longest one's: one token of 64
+// sequence's share of all slots, rounded down, but no more than it has turns of a workgroup and MOST_SLICES at most; what is
+// left over stays empty.  (Without lengths from the caller that is `slices` each.)  So a batch of ragged sequences keeps no workgroup waiting for the longest one's: one token of 64
 // sequences of 8192 down to a quarter 270 -> 241 us, a chunk of four of 9001 down to a quarter 347 -> 316; what it costs where
 // all are as long is one to two microseconds.
+constexpr int MOST_SLICES = 64;
 struct Span {
   int b, slice, slices, first;        // the sequence (-1: none), the slice among its own, how many it has, its first one's number
   int kv, nq;                         // its slots and query tokens
@@ -84,6 +86,9 @@ template <bool BY_SEQUENCE> __device__ __forceinline__ Span span_of(const Stream
     int extra = (int)((float)units * per_unit);
     if ((long)extra * all > spare * units) --extra;
     else if (all && (long)(extra + 1) * all <= spare * units) ++extra;
+    // (a slice without slots leaves a state all the same, and the join reads the states eight at a time, one after the other: a
+    // token of one sequence of 32768 and 15 of 64 with weights 59 us with 358 slices for the long one, 26 with 64)
+    extra = max(0, min(extra, min(MOST_SLICES, (units + a.turn_shift) >> a.turn_shift) - 1));
     const int mine = b0 + lane < a.B ? 1 + extra : 0, incl = wave_incl_scan(mine);
     const int end = first + __builtin_amdgcn_readlane(incl, 63);
     if (BY_SEQUENCE ? at < b0 + 64 : at < end) {

@@ -932,7 +932,7 @@ int slices_of(const ig_desc *d, int prompt_rows, long nrb, int n_keys) {
   const long groups = d->B * (long)d->H * nrb, slots = slots_of(prompt_rows);
   const long turns = div_up(n_keys, prompt_rows ? 64 : (d->dtype == IG_F16 ? 128 : 64));
   long best = 1, best_cost = -1;
-  for (long s = 1; s <= 64 && s <= turns && (s == 1 || groups * s <= ROUNDS * slots); ++s) {
+  for (long s = 1; s <= MOST_SLICES && s <= turns && (s == 1 || groups * s <= ROUNDS * slots); ++s) {
     const long cost = div_up(groups * s, slots) * (div_up(turns, s) + 2) + (s > 1 ? 3 * div_up(s, 8) : 0);
     if (best_cost < 0 || cost < best_cost) best = s, best_cost = cost;
   }
@@ -977,6 +977,7 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   a.visible = c.visible, a.q_len = c.q_len, a.kv_len = c.kv_len;
   a.n_q = c.n_q, a.R = c.n_q * c.group, a.Hq = d->H * c.group, a.N = d->N, a.N_cap = d->N_cap;
   a.nrb = p.nrb, a.slices = p.slices, a.B = d->B, a.H = d->H;
+  a.turn_shift = !p.prompt && d->dtype == IG_F16;
   a.by_slices = ig_fast_div(p.slices), a.by_H = ig_fast_div(d->H), a.by_group = ig_fast_div(c.group);
   a.flip = d->scale < 0.f ? 1 : (d->scale == 0.f ? 2 : 0);
   a.c = (d->scale == 0.f ? 1.f : fabsf(d->scale)) * 1.44269504088896340736f;
@@ -1098,7 +1099,7 @@ size_t ig_cache_reserve_bytes(const ig_desc *d, int group, int n_q) {
   const long BH = (long)d->B * d->H, R = (long)n_q * group;
   const long rounds = ROUNDS * (d->dtype == IG_F16 ? 256 * slots_of(256) > 128 * slots_of(128) ? 256 * slots_of(256) : 128 * slots_of(128)
                                                    : 32 * slots_of(0));
-  const long rows = 64 * BH * R < rounds ? 64 * BH * R : rounds;
+  const long rows = MOST_SLICES * BH * R < rounds ? MOST_SLICES * BH * R : rounds;
   const size_t logits = group <= 32 ? (size_t)BH * group * (((long)d->N_cap + 63) / 64 * 64) * sizeof(float) : 0;
   const size_t attention = (size_t)BH * R * sizeof(float2) + (size_t)rows * (sizeof(float2) + d->d * sizeof(float)) + logits + 4 * 256;
   ig_desc full = *d;
