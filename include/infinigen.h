@@ -394,8 +394,9 @@ int ig_gather_attention(ig_ctx *ctx, const ig_desc *desc, const void *q, const v
  *  - group >= 1 query heads share a pool: query head h * group + g reads pool head h (group = 1: as
  *    many query heads as pools).  B, H of the descriptor count pools; r is only used with a slab, alpha
  *    and rope are not used.
- *  - kv_len: device int32 [B], valid slots of each sequence, or NULL: N for all.  Clamped to [0, N]; N
- *    is the largest length the call may meet and sizes its grid.  N = 0 is allowed.
+ *  - kv_len: device int32 [B], valid slots of each sequence, or NULL: N for all.  Clamped to [0, N] (in
+ *    ig_append_rows, where it is the length before the append, to [0, N_cap]); N is the largest length the
+ *    call may meet and sizes its grid.  N = 0 is allowed.
  *  - Rows of the valid slots and of nodes that some node sees are expected to be finite (an infinity or a
  *    NaN among them may reach rows that do not see it) and logits between -1e8 and 1e8.  What lies in other
  *    slots and nodes, and in query rows behind the last one, is never used, whatever it holds.
@@ -426,7 +427,9 @@ int ig_cache_attention(ig_ctx *ctx, const ig_desc *desc, int32_t group, int32_t 
  * q, out: device [B, n_tree, H*group, d]; k_tree, v_tree: device [B, n_tree, H, d], the nodes' keys
  * (skewed, like the pool's) and values; all 16-byte aligned.  visible: device uint64 [B, n_tree].
  * tree_len: device int32 [B], nodes of each sequence, clamped to [0, n_tree], or NULL: n_tree; rows from
- * there on are left as they were, bits from there on are not used.  A node that sees nothing gets zeros. */
+ * there on are left as they were, bits from there on are not used.  A node that sees nothing gets zeros.
+ * Nodes add nothing to any slot's weight: which of them are accepted is not known yet.  A caller that wants
+ * the accepted tokens' queries to count attends them once more with ig_cache_attention after ig_append_rows. */
 int ig_tree_attention(ig_ctx *ctx, const ig_desc *desc, int32_t group, int32_t n_tree, const void *q,
                       const void *k_tree, const void *v_tree, const uint64_t *visible,
                       const int32_t *tree_len, const void *Kpool, const void *Vpool, const int32_t *kv_len,
@@ -437,13 +440,13 @@ int ig_tree_attention(ig_ctx *ctx, const ig_desc *desc, int32_t group, int32_t n
 int ig_reserve_cache(ig_ctx *ctx, const ig_desc *desc, int32_t group, int32_t n_q);
 
 /* ig_append_token for several rows and ragged sequences: the accepted path of a tree, or a prompt's rows.
- * For j < n_append[b], slot kv_len[b] + j of every pool of sequence b receives row path[b, j] of k_rows, v_rows
- * (device [B, n_rows, H, d], 16-byte aligned); slots >= N_cap are skipped.  path: device int32 [B, n_rows],
- * entries clamped to [0, n_rows), or NULL: row j.  The rows must not overlap the pools (IG_EINVAL).  n_append: device int32 [B], clamped to [0, n_rows], or
- * NULL: n_rows.  Here kv_len is the length before the append (NULL: N).  mass, if given, restarts at 0 in
- * these slots, born, if given, becomes pos[b] + j (pos: device int32 [B], or NULL: the slot).  slab with
- * idx_dev, if given, receives the kept key channels as in ig_append_token.  The caller then adds n_append
- * to kv_len. */
+ * For j < n_append[b], slot kv_len[b] + j of every pool of sequence b receives row path[b, j] of k_rows,
+ * v_rows (device [B, n_rows, H, d], 16-byte aligned); slots >= N_cap are skipped.  path: device int32
+ * [B, n_rows], entries clamped to [0, n_rows), or NULL: row j.  The rows must not overlap the pools
+ * (IG_EINVAL).  n_append: device int32 [B], clamped to [0, n_rows], or NULL: n_rows.  Here kv_len is the
+ * length before the append, clamped to [0, N_cap] (NULL: N).  mass, if given, restarts at 0 in these slots,
+ * born, if given, becomes pos[b] + j (pos: device int32 [B], or NULL: the slot).  slab with idx_dev, if
+ * given, receives the kept key channels as in ig_append_token.  The caller then adds n_append to kv_len. */
 int ig_append_rows(ig_ctx *ctx, const ig_desc *desc, int32_t n_rows, const void *k_rows, const void *v_rows,
                    const int32_t *path, const int32_t *n_append, const int32_t *kv_len, const int32_t *pos,
                    const int32_t *idx_dev, void *slab, void *Kpool, void *Vpool, float *mass, int32_t *born,
@@ -455,7 +458,8 @@ int ig_append_rows(ig_ctx *ctx, const ig_desc *desc, int32_t n_rows, const void 
  * evicted slots < keep: K and V rows, mass, born (may be NULL) and, if slab is given (with idx_dev), the kept
  * key channels.  Pools with at most `keep` valid slots are left as they are; the caller takes kv_len[b] =
  * min(kv_len[b], keep) from there.  Every pool of a sequence keeps its own slots.  With kv_len = keep + 1
- * this is the eviction of a decode step: one slot a pool. */
+ * this is the eviction of a decode step: one slot a pool.  Where N itself is keep + 1 a kernel for one slot
+ * takes it, in about half the time of the selection that a larger N gets. */
 int ig_pool_evict(ig_ctx *ctx, const ig_desc *desc, int32_t keep, const int32_t *kv_len, float *mass,
                   int32_t *born, const int32_t *protect_from, const int32_t *idx_dev, void *slab, void *Kpool,
                   void *Vpool, void *stream);

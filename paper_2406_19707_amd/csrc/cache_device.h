@@ -49,9 +49,9 @@ __device__ __forceinline__ int length_of(const int32_t *len, int b, int all, int
 // ---- which slices are whose --------------------------------------------------------------------------------
 // The B * slices slices of a head are dealt to the sequences by their lengths: one each, and of the others as many as the
 // sequence's share of all slots, rounded down, but no more than it has turns of a workgroup and MOST_SLICES at most; what is
-// left over stays empty.  (Without lengths from the caller that is `slices` each.)  So a batch of ragged sequences keeps no workgroup waiting for the longest one's: one token of 64
-// sequences of 8192 down to a quarter 270 -> 241 us, a chunk of four of 9001 down to a quarter 347 -> 316; what it costs where
-// all are as long is one to two microseconds.
+// left over stays empty.  (Without lengths from the caller that is `slices` each.)  So a batch of ragged sequences keeps no
+// workgroup waiting for the longest one's: one token of 64 sequences of 8192 down to a quarter 270 -> 241 us, a chunk of four
+// of 9001 down to a quarter 347 -> 316; what it costs where all are as long is one to two microseconds.
 constexpr int MOST_SLICES = 64;
 struct Span {
   int b, slice, slices, first;        // the sequence (-1: none), the slice among its own, how many it has, its first one's number

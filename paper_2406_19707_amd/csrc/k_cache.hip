@@ -37,6 +37,9 @@ __global__ __launch_bounds__(256) void attend_stream(StreamArgs a) {
   // A wave's part of LDS: its outputs at the end (rows of D floats and 16 bytes that set their banks apart), until then
   // logits of up to 16 rows, which wait here because a store before every tile's loads is one more thing that the wait
   // for those waits for (one row, 160 pools of 32768: 501 us in all with stores after every tile, 482 so, 436 without).
+  // (At d = 32, in float32 also 64, it is the box that limits the waves of a SIMD, to three.  That costs nothing: with half as
+  // large a box 512 pools of 8192, d = 32, 64 and 128, take 116, 211 and 391 us, with this one 116, 208 and 384; float32, 512 of
+  // 4096, 108, 200 and 378 with both.)
   constexpr int LDB = D + 4, LOGIT_BOX = LOGITS && NT == 1 ? 3200 : 0, BOX = RB * LDB > LOGIT_BOX ? RB * LDB : LOGIT_BOX;
   __shared__ __attribute__((aligned(16))) float boxes[4][BOX];
   __shared__ float box_m[4][RB], box_l[4][RB];
@@ -685,8 +688,10 @@ __global__ __launch_bounds__(256) void attend_join(StreamArgs a, float *mass, in
 // ---- the weights of many query rows ------------------------------------------------------------------
 // Float32: a workgroup keeps 32 cached keys (d = 256: 16) as the rows of S^T = K Q^T; its waves take turns at the
 // query rows that see them, 16 at a time with the next 16 asked for: mass[t] += sum over rows of
-// exp2(c s - ref) / sum, with the rows' final references and sums.  Bound by the matrix units: 2 x 16 heads of 1024
-// tokens, d = 128, 108 us; 4 heads of 512, d = 64, 9.6 us (32 us with a wave for every 16 keys and nothing asked for ahead).
+// exp2(c s - ref) / sum, with the rows' final references and sums.  2 x 16 heads of
+// 1024 tokens, d = 128, 108 us = 40 TFLOP/s, a quarter of what a library product reaches in float32: every 32 keys read the query
+// rows again, and two waves a SIMD with 16 rows asked for ahead have to hide that.  4 heads of 512, d = 64, 9.6 us (32 us with a
+// wave for every 16 keys and nothing asked for ahead).
 template <int D> constexpr int mass_keys() { return D <= 128 ? 32 : 16; }
 template <int D> __global__ __launch_bounds__(256) void attend_mass(StreamArgs a, float *mass, FastDiv by_chunks) {
   constexpr int MT = mass_keys<D>() / 16, KCH = D / 16;
@@ -906,8 +911,10 @@ template <int D> __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void prompt
 int div_up(long n, long d) { return (int)((n + d - 1) / d); }
 
 // Query rows a workgroup of attend_stream takes: 16 or 32.  (With 64 the registers run out: float32, 1024 rows over as
-// many, 121 us with 32 and 163 us with 64.)  In half precision attend_prompt takes over from there: trees of 32 to 64 nodes
-// over 4096, 128 pools, 66 to 67 us there, 101 to 105 us here; of 32 nodes and fewer the same in both.
+// many, 121 us with 32 and 163 us with 64.)  In half precision attend_prompt takes over from there: trees of 33 to 64 nodes
+// over 4096, 128 pools, 62 to 67 us there, 101 to 105 us here in two blocks.  Up to 32 nodes: the same pools with 17, 24 and
+// 32, 63, 62 and 63 us here, 72, 63 and 61 there; 512 pools 185 to 187 here, 203 to 218 there; d = 64, 128 pools, 29 to 30
+// here, 35 there; only small calls the other way round (8 pools of 1024: 12.5 to 13.5 here, 11 to 12 there).
 // (d = 256: 16 here, and from 17 rows on in half precision there.)
 int row_block(const ig_desc *d, long R) { return R <= 16 || d->d > 128 ? 16 : 32; }
 bool many_rows(const ig_desc *d, long R) { return d->dtype == IG_F16 && R > (d->d > 128 ? 16 : 32); }
@@ -923,9 +930,12 @@ int prompt_rows(const ig_desc *d, const CacheCall &c) {
 // Slices the cached rows of a pool are cut into: the number for which the last workgroups end first, if a turn (64
 // rows of attend_prompt, four waves' tiles of attend_stream) takes a unit of time, a workgroup two more to start and
 // to leave its state, the join three for every eight slices, and a compute unit holds eight waves.  (8 pools of 32768: 31 us
-// with 24 slices, 35 with 16, 36 with 64; 32 of 777: 8.8 with 8, 9.7 with 4, 11.2 with 16, 13.6 with one.)  (Four sequences of up to 9001 with 1268 query rows for
-// each of 8 pools: 3 slices of 320 row blocks 1.5 times as fast as 2, which leave the second round a quarter full.)
-// Never more than four rounds of workgroups, so that the states they leave are bounded (reserve_rows).
+// with 24 slices, 35 with 16, 36 with 64; 32 of 777: 8.8 with 8, 9.7 with 4, 11.2 with 16, 13.6 with one.  Four sequences
+// of up to 9001 with 1268 query rows for each of 8 pools: 3 slices of 320 row blocks 1.5 times as fast as 2, which leave the
+// second round a quarter full.)  Eight waves is what d = 128 holds, up to 16 rows or from 33 on, and where all of this was
+// measured.  With 17 to 32 rows there, and at d = 256, it holds four, at d = 32 and 64 from 8 to 32: what the model calls a
+// round is then off by as much.
+// Never more than four rounds of workgroups, so that the states they leave are bounded (ig_cache_reserve_bytes).
 constexpr long ROUNDS = 4;
 long slots_of(int prompt_rows) { return prompt_rows == 256 ? 256 : 512; }
 int slices_of(const ig_desc *d, int prompt_rows, long nrb, int n_keys) {

@@ -291,7 +291,7 @@ template <typename T, int THREADS> __global__ __launch_bounds__(THREADS) void ev
   }
 }
 
-// Bound by memory: 512 pools, about 725 rows of 256 bytes of K and of V each, 78 us = 5.0 TB/s.
+// Bound by memory: 512 pools, about 725 rows of 256 bytes of K and of V each, 80 us = 4.9 TB/s.
 constexpr int MOVE_ROWS = 64;      // rows a workgroup of evict_move takes
 
 template <typename T> __global__ __launch_bounds__(256) void evict_move(EvictArgs a) {
