@@ -404,10 +404,10 @@ int ig_gather_attention(ig_ctx *ctx, const ig_desc *desc, const void *q, const v
  *    precision where they multiply V (not in the sums): by at most 2^-11 of themselves down to 2^-23 of a row's
  *    largest weight (calls of up to 16 query rows a pool: 2^-28), by at most 2^-34 of the largest below that
  *    (for logits below 10^4; beyond, a larger share of the weights is below, and from 2^22 on that is 2^-25).
- *  - out must not overlap the inputs or mass (IG_EINVAL).  Less than 2^22 pools (B * H), at most 2^26 query rows
- *    (B * H * group * tokens; rows to append likewise) and 2^24 elements of a token (H * group * d), IG_ESHAPE
- *    otherwise; and for B * H * N beyond what a launch takes: the weights of several float32 tokens from about
- *    2^29 on (d = 256: 2^28), an eviction from about 2^30 on at the earliest.
+ *  - out must not overlap the inputs or mass (IG_EINVAL).  At most 2^26 query rows (B * H * group * tokens; rows to
+ *    append likewise) and 2^24 elements of a token (H * group * d), IG_ESHAPE otherwise; and for what a launch
+ *    of less than 2^32 threads does not take: the weights of several float32 tokens for B * H * N from about 2^29
+ *    on (d = 256: 2^28), an eviction for B * H from 2^23 or B * H * N from about 2^30 on.
  *  - mass: device float32 [B*H, N_cap], one sum per slot, zero-initialised by the caller.  born: device
  *    int32 [B*H, N_cap], the position of the token a slot holds (the stamps of IG_POLICY_FIFO). */
 

@@ -971,8 +971,6 @@ static int check_cache(ig_ctx *ctx, const ig_desc *d, const char *what, int grou
   // (row and workgroup numbers are 32-bit; a pool has at most n_q * group rows and 64 slices of each 16 of them)
   if ((double)group * n_q * d->H * d->B > 1073741824.0 / 16)
     return ig_fail(ctx, IG_ESHAPE, "%s: too many query rows", what);
-  // (a launch has less than 2^32 threads, an eviction's workgroup for a pool up to 1024)
-  if ((long)d->B * d->H >= 1 << 22) return ig_fail(ctx, IG_ESHAPE, "%s: B * H = %ld pools, at most 2^22 - 1", what, (long)d->B * d->H);
   // (offsets among 64 tokens' rows are 32-bit)
   if ((double)group * d->H * d->d > 16777216.0) return ig_fail(ctx, IG_ESHAPE, "%s: a token's heads are too many", what);
   if ((double)d->B * d->H * ((double)d->N_cap / 16 + 64) > 1073741824.0)
@@ -991,7 +989,7 @@ int ig_reserve_cache(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_q) 
 
 static int attend_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, void *stream) {
   const CachePlan p = ig_cache_plan(d, c);
-  if (p.mass_groups >= 1 << 24) return ig_fail(ctx, IG_ESHAPE, "B * H * N too large for the weights of several tokens");
+  if (p.threads > IG_MOST_THREADS) return ig_fail(ctx, IG_ESHAPE, "B * H, or B * H * N, is too large for a launch");
   // (queries, masks and lengths are read again after the first rows are out, pools by every row; the weights are another output)
   const size_t row = (size_t)d->d * ig_elem_bytes(d->dtype), q_bytes = (size_t)d->B * c.n_q * d->H * c.group * row;
   const size_t pool_bytes = (size_t)d->B * d->H * d->N_cap * row, tree_bytes = (size_t)d->B * c.n_q * d->H * row;
@@ -1037,6 +1035,7 @@ int ig_append_rows(ig_ctx *ctx, const ig_desc *d, int32_t n_rows, const void *k_
                    void *stream) {
   int rc = check_cache(ctx, d, "ig_append_rows", 1, n_rows, false, slab != nullptr, stream);
   if (rc) return rc;
+  if (ig_append_threads(d, n_rows) > IG_MOST_THREADS) return ig_fail(ctx, IG_ESHAPE, "ig_append_rows: B * H is too large for a launch");
   if (!k_rows || !v_rows || !Kpool || !Vpool) return ig_fail(ctx, IG_EINVAL, "ig_append_rows: NULL argument");
   if (slab && !idx_dev) return ig_fail(ctx, IG_EINVAL, "ig_append_rows: a slab needs idx_dev");
   if ((rc = check_aligned(ctx, "ig_append_rows", {k_rows, v_rows, Kpool, Vpool, slab}))) return rc;
@@ -1056,7 +1055,8 @@ int ig_pool_evict(ig_ctx *ctx, const ig_desc *d, int32_t keep, const int32_t *kv
   int rc = check_cache(ctx, d, "ig_pool_evict", 1, 1, false, slab != nullptr, stream);
   if (rc) return rc;
   if (keep < 1) return ig_fail(ctx, IG_ESHAPE, "ig_pool_evict: keep = %d", keep);
-  if (ig_evict_move_groups(d, keep) >= 1 << 24) return ig_fail(ctx, IG_ESHAPE, "ig_pool_evict: B * H * N too large");
+  if (ig_evict_threads(d, keep) > IG_MOST_THREADS)
+    return ig_fail(ctx, IG_ESHAPE, "ig_pool_evict: B * H, or B * H * N, is too large for a launch");
   if (!mass || !Kpool || !Vpool) return ig_fail(ctx, IG_EINVAL, "ig_pool_evict: NULL argument");
   if (protect_from && !born) return ig_fail(ctx, IG_EINVAL, "ig_pool_evict: protect_from needs born");
   if (slab && !idx_dev) return ig_fail(ctx, IG_EINVAL, "ig_pool_evict: a slab needs idx_dev");

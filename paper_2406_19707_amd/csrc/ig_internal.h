@@ -297,7 +297,7 @@ struct CacheCall {
 struct CachePlan {
   bool prompt;
   int rb, nrb, slices;
-  long logits_ld, mass_groups;                  // mass_groups: workgroups of 256 threads of the weights' launch, 0 without one
+  long logits_ld, threads;                      // threads: of the largest launch
   size_t stats_at, part_ml_at, part_at, logits_at, bytes;      // parts of the workspace
 };
 CachePlan ig_cache_plan(const ig_desc *d, const CacheCall &c);
@@ -305,7 +305,10 @@ size_t ig_cache_reserve_bytes(const ig_desc *d, int group, int n_q);
 int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const CachePlan &p, char *ws, hipStream_t s);
 // eviction by weight and the append of rows (k_evict.hip)
 size_t ig_evict_workspace(const ig_desc *d, int keep);
-long ig_evict_move_groups(const ig_desc *d, int keep);      // workgroups of 256 threads that move rows, at most
+// threads of a call's largest launch; one takes IG_MOST_THREADS at most
+constexpr long IG_MOST_THREADS = 0xffffffffl;
+long ig_evict_threads(const ig_desc *d, int keep);
+long ig_append_threads(const ig_desc *d, int n_rows);
 int ig_launch_evict(ig_ctx *ctx, const ig_desc *d, int keep, const int32_t *kv_len, float *mass, int32_t *born,
                     const int32_t *protect_from, const int32_t *idx, void *slab, void *Kpool, void *Vpool, char *ws,
                     hipStream_t s);

@@ -969,8 +969,13 @@ CachePlan ig_cache_plan(const ig_desc *d, const CacheCall &c) {
     return here;
   };
   p.logits_ld = ((long)d->N + 63) / 64 * 64;
+  // the rows' launch, the join's (of many workgroups only without slices, for kept logits) and the weights'
+  const bool logits = keeps_logits(c, p);
   const int mass_block = d->dtype == IG_F16 ? MASS_KEYS : (d->d <= 128 ? mass_keys<128>() : mass_keys<256>());
-  p.mass_groups = c.mass && !keeps_logits(c, p) ? BH * div_up(d->N, mass_block) : 0;
+  p.threads = (BH * p.slices * p.nrb + 8) * (p.prompt && p.rb == 256 ? 512 : 256);
+  const long join = logits ? BH * div_up(d->N, 1024) * 256 : 0, mass = c.mass && !logits ? (BH * div_up(d->N, mass_block) + 8) * 256 : 0;
+  p.threads = p.threads > join ? p.threads : join;
+  p.threads = p.threads > mass ? p.threads : mass;
   p.stats_at = take(c.mass ? BH * R * sizeof(float2) : 0);
   p.part_ml_at = take(p.slices > 1 ? BH * p.slices * R * sizeof(float2) : 0);
   p.part_at = take(p.slices > 1 ? BH * p.slices * R * d->d * sizeof(float) : 0);

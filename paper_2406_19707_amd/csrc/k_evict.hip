@@ -365,10 +365,18 @@ template <typename T> __global__ __launch_bounds__(256) void append_rows(AppendA
 
 int most_moves(const ig_desc *d, int keep) { return keep < d->N - keep ? keep : d->N - keep; }
 int move_chunks(const ig_desc *d, int keep) { return (most_moves(d, keep) + MOVE_ROWS - 1) / MOVE_ROWS; }
+int append_chunks(int n_rows) { return (n_rows + APPEND_ROWS - 1) / APPEND_ROWS; }
+// one slot too many at most, in every pool
+bool evicts_one(const ig_desc *d, int keep) { return d->N == keep + 1 && d->d * ig_elem_bytes(d->dtype) / 16 <= 256; }
 
 }  // namespace
 
-long ig_evict_move_groups(const ig_desc *d, int keep) { return d->N <= keep ? 0 : d->B * (long)d->H * move_chunks(d, keep); }
+long ig_evict_threads(const ig_desc *d, int keep) {
+  if (d->N <= keep) return 0;
+  const long a_pool = d->N > 4096 ? 1024 : (evicts_one(d, keep) ? 256 : 512), moves = evicts_one(d, keep) ? 0 : move_chunks(d, keep) * 256l;
+  return d->B * (long)d->H * (a_pool > moves ? a_pool : moves);
+}
+long ig_append_threads(const ig_desc *d, int n_rows) { return d->B * (long)d->H * append_chunks(n_rows) * 256; }
 
 size_t ig_evict_workspace(const ig_desc *d, int keep) {
   return (size_t)d->B * d->H * (1 + 2 * (size_t)most_moves(d, keep)) * sizeof(int32_t);
@@ -387,7 +395,7 @@ int ig_launch_evict(ig_ctx *ctx, const ig_desc *d, int keep, const int32_t *kv_l
   a.by_H = ig_fast_div(d->H), a.by_units = ig_fast_div(a.units);
   a.by_chunks = ig_fast_div(move_chunks(d, keep));
   const bool one = a.most <= 16;         // few rows a pool: moved by the workgroup that found them
-  if (d->N == keep + 1 && a.units <= 256) {
+  if (evicts_one(d, keep)) {
     // (256 threads take 8 slots each of 2048; the long pools' 1024 as many of 8192)
 #define ONE(T)                                                                                       \
   {                                                                                                  \
@@ -438,7 +446,7 @@ int ig_launch_append_rows(ig_ctx *ctx, const ig_desc *d, int n_rows, const void 
   a.H = d->H, a.N = d->N, a.N_cap = d->N_cap, a.n_rows = n_rows, a.d = d->d, a.r = d->r;
   a.units = d->d * ig_elem_bytes(d->dtype) / 16, a.nTiles = (d->N_cap + tile - 1) / tile;
   a.by_H = ig_fast_div(d->H), a.by_units = ig_fast_div(a.units);
-  a.by_chunks = ig_fast_div((n_rows + APPEND_ROWS - 1) / APPEND_ROWS);
+  a.by_chunks = ig_fast_div(append_chunks(n_rows));
   const dim3 grid((unsigned)(BH * (long)a.by_chunks.d)), block(256);
   if (d->dtype == IG_F16) {
     auto k = append_rows<half_t>;

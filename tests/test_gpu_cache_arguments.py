@@ -94,11 +94,11 @@ def test_more_than_a_launch_takes(ctx):
     """Refused for its size before anything else: every call here also has an argument that is refused later."""
     x = torch.zeros(1 << 12, dtype=torch.float16, device="cuda")
     bad = x.data_ptr() + 2
-    many = desc(1 << 11, 1 << 11, 64, 1, 1, "f16")
-    refused(ig.IG_ESHAPE, ctx.ig_cache_attention, many, 1, 1, bad, None, x, x, None, None, x)
-    refused(ig.IG_ESHAPE, ctx.ig_tree_attention, many, 1, 1, bad, x, x, x, None, x, x, None, x)
-    refused(ig.IG_ESHAPE, ctx.ig_append_rows, many, 1, bad, x, None, None, None, None, None, None, x, x)
-    refused(ig.IG_ESHAPE, ctx.ig_pool_evict, desc(1 << 11, 1 << 11, 64, 2, 2, "f16"), 1, None, x, None, None, None, None, bad, x)
+    # 2^23 pools: too many for a selection's 512 threads each, not for 256
+    refused(ig.IG_ESHAPE, ctx.ig_pool_evict, desc(1 << 12, 1 << 11, 64, 3, 3, "f16"), 1, None, x, None, None, None, None, bad, x)
+    refused(ig.IG_EINVAL, ctx.ig_pool_evict, desc(1 << 12, 1 << 11, 64, 3, 3, "f16"), 2, None, x, None, None, None, None, bad, x)
+    refused(ig.IG_EINVAL, ctx.ig_cache_attention, desc(1 << 12, 1 << 11, 64, 1, 1, "f16"), 1, 1, bad, None, x, x, None, None, x)
+    refused(ig.IG_EINVAL, ctx.ig_append_rows, desc(1 << 12, 1 << 11, 64, 1, 1, "f16"), 1, bad, x, None, None, None, None, None, None, x, x)
     # 2^29 float32 slots in blocks of 32 keys: 2^24 workgroups; out is q, which is looked at afterwards
     refused(ig.IG_ESHAPE, ctx.ig_cache_attention, desc(1, 1 << 9, 32, 1 << 20, 1 << 20, "f32"), 1, 2, x, None, x, x, None, x, x)
     refused(ig.IG_EINVAL, ctx.ig_cache_attention, desc(1, 1 << 9, 32, 1 << 20, 1 << 20, "f32"), 1, 2, x, None, x, x, None, None, x)
@@ -106,5 +106,3 @@ def test_more_than_a_launch_takes(ctx):
     # 2^31 slots, half of them kept: 2^24 blocks of 64 rows that could move
     refused(ig.IG_ESHAPE, ctx.ig_pool_evict, desc(1, 1 << 9, 8, 1 << 22, 1 << 22, "f16"), 1 << 21, None, x, None, None, None, None, bad, x)
     refused(ig.IG_EINVAL, ctx.ig_pool_evict, desc(1, 1 << 9, 8, 1 << 22, 1 << 22, "f16"), 1 << 20, None, x, None, None, None, None, bad, x)
-    # with less than 2^22 pools the same small call is taken as far as its bad argument
-    refused(ig.IG_EINVAL, ctx.ig_cache_attention, desc(1 << 11, (1 << 11) - 1, 64, 1, 1, "f16"), 1, 1, bad, None, x, x, None, None, x)
