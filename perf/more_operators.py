@@ -13,7 +13,7 @@ own = False
 
 _DT = {"f16": torch.float16, "f32": torch.float32}
 _MOST = {"i8": 127.0, "e4m3": 448.0}             # the largest code
-_LEAST = 2.0 ** -100                             # the smallest scale
+_LEAST = 2.0 ** -80                              # the smallest scale
 _ctx = None
 
 
