@@ -76,11 +76,11 @@ enum {
   IG_K_SELECT = 3,   /* threshold + compaction from a score buffer (long sequences) */
   IG_K_GATHER = 4,
   IG_K_ATTENTION = 5,
-  IG_K_BUILD = 6,    /* ig_wq_build / ig_slab_build */
+  IG_K_BUILD = 6,    /* ig_wq_build / ig_slab_build / ig_append_rows / ig_append_pages / ig_rotate_rows */
   IG_K_COPY = 7,     /* ig_copy_bytes */
   IG_K_READ = 8,     /* ig_read_bytes */
   IG_K_LAYER = 9,    /* ig_layer_step: next layer's scan + this layer's prefetch and attention, one launch */
-  IG_K_CACHE = 10,   /* ig_cache_attention, ig_tree_attention: every launch of a call */
+  IG_K_CACHE = 10,   /* ig_cache_attention, ig_tree_attention, ig_page_attention: every launch of a call */
   IG_K_EVICT = 11,   /* ig_pool_evict */
   IG_K_COUNT = 12
 };
@@ -463,6 +463,100 @@ int ig_append_rows(ig_ctx *ctx, const ig_desc *desc, int32_t n_rows, const void 
 int ig_pool_evict(ig_ctx *ctx, const ig_desc *desc, int32_t keep, const int32_t *kv_len, float *mass,
                   int32_t *born, const int32_t *protect_from, const int32_t *idx_dev, void *slab, void *Kpool,
                   void *Vpool, void *stream);
+
+/* ---- rotary embedding on the device; a cache in pages of 8-bit codes ------------------------- */
+
+/* The comparison systems of Section 5 include caches held in fewer bits; these calls keep one in 8 bits for each value, in
+ * pages with a scale for each page and head, and serve it: rotate, append, attend, read back.  A page is the unit of
+ * allocation as well: a sequence's slot t is slot t % page_size of page table[b, t / page_size]. */
+
+/* How the frequencies of ig_rotary_frequencies follow from theta^(-2c/dims), c < dims/2: */
+enum {
+  IG_ROPE_PLAIN = 0,      /* as they are (factor, low, high and original are not used) */
+  IG_ROPE_LINEAR = 1,     /* divided by factor: positions are interpolated (low, high and original are not used) */
+  IG_ROPE_NTK = 2,        /* base theta * factor^(dims / (dims - 2)), so that the slowest pair is divided by factor
+                             and the fastest not at all; dims > 2 (low, high and original are not used) */
+  IG_ROPE_RAMP = 3,       /* divided by factor for pairs that turn at most `low` times over `original` positions, as they
+                             are for those that turn at least `high` times, and in between a mixture whose share is
+                             linear in c (arXiv 2309.00071, with the magnitude 0.1 ln(factor) + 1 given there) */
+  IG_ROPE_WAVELENGTH = 4  /* the same ends, and in between a mixture whose share is linear in the number of turns */
+};
+
+/* Host call: freq[c], c < dims/2 (host, double), the angle of one position, and the magnitude (1 but for IG_ROPE_RAMP; may be
+ * NULL).  dims even; theta > 1; factor >= 1, 0 < low < high and original >= 1 where they are used.  ctx may be NULL. */
+int ig_rotary_frequencies(ig_ctx *ctx, int dims, double theta, int kind, double factor, double low, double high,
+                          int32_t original, double *freq, float *magnitude);
+
+/* A rotary embedding: channels 0 .. dims-1 of every row are dims/2 pairs, (c, c + dims/2) or, interleaved, (2c, 2c + 1); a pair
+ * (a, b) at position p becomes magnitude * (a cos - b sin, b cos + a sin) of the angle p * freq[c].  The others stay.  Angles
+ * are worked out and reduced in double, sine and cosine and the products in float32; rows are rounded once. */
+typedef struct {
+  int32_t dims;         /* even, 2 .. d */
+  int32_t interleaved;  /* 0 or 1 */
+  float magnitude;      /* finite */
+  const double *freq;   /* device [dims/2], 8-byte aligned: ig_rotary_frequencies' */
+} ig_rotary;
+
+/* Rotation of n tokens' rows: x, out device [n, heads, d] of `dtype` with x_stride, out_stride elements from one token to the
+ * next (0: heads * d), both 16-byte aligned and strides a multiple of 16 bytes.  pos: device int32 [n].  d a multiple of 16, at most
+ * 1024.  out may be x with the same stride, else the two must not overlap.  inverse = 1: the transpose (the angle's sign
+ * changed), i.e. the gradient of x from that of out. */
+int ig_rotate_rows(ig_ctx *ctx, int dtype, int32_t n, int32_t heads, int32_t d, const ig_rotary *rotary, int inverse,
+                   const int32_t *pos, const void *x, int64_t x_stride, void *out, int64_t out_stride, void *stream);
+
+/* What a code stands for: IG_CODE_I8 two's complement -127 .. 127, IG_CODE_E4M3 the 8-bit float with 4 exponent bits, no infinity
+ * and 448 as its largest value (no NaN among a sequence's slots); each times the scale of its page and head. */
+enum { IG_CODE_I8 = 0, IG_CODE_E4M3 = 1 };
+typedef struct {
+  int32_t n_pages;       /* pages in the pool */
+  int32_t page_size;     /* slots of a page: 16, 32, 64 or 128 */
+  int32_t table_stride;  /* entries of a sequence's row of the table; N_cap <= table_stride * page_size */
+  int32_t code;          /* IG_CODE_* */
+  const int32_t *table;  /* device [B, table_stride]: pages of each sequence, in order */
+  void *K, *V;           /* device [n_pages, H, page_size, d], a byte each, 16-byte aligned */
+  float *K_scale, *V_scale;  /* device [n_pages, H]: powers of two, 2^-80 .. 2^120 (any other value is read as the power of
+                                two at or below it, within these bounds) */
+} ig_pages;
+
+/* Common to the calls below: B, H, d, N, N_cap, dtype and (attention) scale of the descriptor are used as in the calls over whole
+ * pools, with N_cap the slots a sequence may have; d = 32, 64, 128 or 256.  Entries of the table outside [0, n_pages) are
+ * clamped into it where slots are read, and nothing is written through them.  Entries of pages that a sequence does not reach are
+ * not looked at.  Several sequences may share pages that are only read; a page that a call appends to belongs to one sequence.
+ *
+ * Appends rows to ragged sequences as ig_append_rows does, rotated and rounded to 8 bits on the way.  For j < n_append[b], slot
+ * kv_len[b] + j of sequence b receives k_rows[b, j] rotated at pos[b] + j (pos: device int32 [B], or NULL: the slot), and
+ * v_rows[b, j]; slots >= N_cap are skipped.  rotary NULL: keys are taken as they are.
+ * q (or NULL): device [B, n_rows, H*group, d], rotated at the same positions into q_out (dense; may be q where that is dense too),
+ * rows j < n_append[b] of it; the others are left as they were.  Without q, group and q_out are not used.
+ * k_rows, v_rows: device [B, n_rows, H, d].  row_stride: elements from one token to the next of q, k_rows and v_rows alike (the
+ * parts of one projection's output), or 0: each is dense.  n_append, kv_len as in ig_append_rows.
+ * The scale of a page that receives its first row is the least power of two with which its rows' largest value is at most 127 (448)
+ * codes, and 2^-80 at least.  That of a page that holds rows is doubled as often as the new rows need it, and the codes of the rows it
+ * holds are rounded again.  Values are rounded to the nearest code, ties to the even one: a row is off by at most half a scale
+ * (e4m3: by 2^-4 of itself, or 2^-10 of a scale where that is more) after its append, and by less than one scale however often it
+ * has doubled since (e4m3: it loses bits only below 2^-6 of a scale).  NaN and infinities are stored as 0.
+ * What lies in the other slots of a page is left as it was. */
+int ig_append_pages(ig_ctx *ctx, const ig_desc *desc, const ig_pages *pages, const ig_rotary *rotary, int32_t group,
+                    int32_t n_rows, const void *q, const void *k_rows, const void *v_rows, int64_t row_stride,
+                    const int32_t *n_append, const int32_t *kv_len, const int32_t *pos, void *q_out, void *stream);
+
+/* Attention of n_q tokens per sequence that are in the pages already, as ig_cache_attention without mass: q, out, q_len, kv_len and
+ * group as there, and the same expectations of finite rows and logits.  Every product and sum is in float32; with IG_F16 the
+ * softmax weights, times their page's scale, are rounded to half precision where they multiply the codes of V, by at most 2^-11
+ * of themselves down to 2^-23 of the row's largest (calls of up to 32 query rows a pool: 2^-28), and by at most 2^-34 of that
+ * below; with IG_F32 queries and weights are taken as two halves each, which leaves 2^-22 of themselves. */
+int ig_page_attention(ig_ctx *ctx, const ig_desc *desc, const ig_pages *pages, int32_t group, int32_t n_q, const void *q,
+                      const int32_t *q_len, const int32_t *kv_len, void *out, void *stream);
+
+/* Size the workspace of ig_page_attention for up to n_q query tokens of `group` heads a pool head and desc->N_cap slots
+ * (allocates; synchronous).  The other calls here need none. */
+int ig_reserve_pages(ig_ctx *ctx, const ig_desc *desc, int32_t group, int32_t n_q);
+
+/* ig_gather_kv out of pages: row j < sel_cnt[b*H+h] of K_sel, V_sel (device [B*H, sel_stride, d] of desc->dtype, 16-byte aligned) is
+ * the value of slot sel_idx[b*H+h, j] (clamped into [0, N_cap)), a code times its scale, rounded once; rows from sel_cnt on are not
+ * written.  What ig_slab_build, ig_sparse_attention and the calls over whole pools need of such a cache. */
+int ig_gather_pages(ig_ctx *ctx, const ig_desc *desc, const ig_pages *pages, const int32_t *sel_idx, int32_t sel_stride,
+                    const int32_t *sel_cnt, void *K_sel, void *V_sel, void *stream);
 
 /* ---- measurement --------------------------------------------------------------------------- */
 

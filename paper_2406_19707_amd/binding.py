@@ -18,7 +18,8 @@ __all__ = [
     "IG_OK", "IG_EINVAL", "IG_ESHAPE", "IG_EDTYPE", "IG_ECAPACITY", "IG_EHIP", "IG_ENOCONV",
     "IG_ENOMEM", "IG_F32", "IG_F16", "IG_MEM_DEVICE", "IG_MEM_HOST_PINNED", "IG_POLICY_COUNTER", "IG_POLICY_FIFO", "IG_POLICY_LRU", "IG_K_PROJECT",
     "IG_K_FINALIZE", "IG_K_SCAN", "IG_K_SELECT", "IG_K_GATHER", "IG_K_ATTENTION", "IG_K_BUILD",
-    "IG_K_COPY", "IG_K_READ", "IG_K_LAYER", "IG_K_CACHE", "IG_K_EVICT", "IgDesc", "IgLayerIO", "IgBufferSet", "IgError", "Context", "lib", "lib_path", "ig_skew_offline",
+    "IG_K_COPY", "IG_K_READ", "IG_K_LAYER", "IG_K_CACHE", "IG_K_EVICT", "IG_CODE_I8", "IG_CODE_E4M3",
+    "IG_ROPE_PLAIN", "IG_ROPE_LINEAR", "IG_ROPE_NTK", "IG_ROPE_RAMP", "IG_ROPE_WAVELENGTH", "IgPages", "IgRotary", "ig_rotary_frequencies", "IgDesc", "IgLayerIO", "IgBufferSet", "IgError", "Context", "lib", "lib_path", "ig_skew_offline",
     "ig_partial_index", "ig_apply_skew", "ig_rope_rows", "ig_speculate_host", "ig_wq_bytes", "ig_slab_bytes", "EXPORTS",
 ]
 
@@ -26,6 +27,8 @@ IG_OK, IG_EINVAL, IG_ESHAPE, IG_EDTYPE, IG_ECAPACITY, IG_EHIP, IG_ENOCONV, IG_EN
 IG_F32, IG_F16 = 0, 1
 IG_MEM_DEVICE, IG_MEM_HOST_PINNED = 0, 1
 IG_POLICY_COUNTER, IG_POLICY_FIFO, IG_POLICY_LRU = 0, 1, 2
+IG_CODE_I8, IG_CODE_E4M3 = 0, 1
+IG_ROPE_PLAIN, IG_ROPE_LINEAR, IG_ROPE_NTK, IG_ROPE_RAMP, IG_ROPE_WAVELENGTH = range(5)
 (IG_K_PROJECT, IG_K_FINALIZE, IG_K_SCAN, IG_K_SELECT, IG_K_GATHER, IG_K_ATTENTION, IG_K_BUILD,
  IG_K_COPY, IG_K_READ, IG_K_LAYER, IG_K_CACHE, IG_K_EVICT) = range(12)
 
@@ -40,6 +43,7 @@ EXPORTS = [
     "ig_speculate_host", "ig_speculate_equalized", "ig_equalize_heads", "ig_gather_kv", "ig_sparse_attention", "ig_sparse_attention_static",
     "ig_sparse_attention_indexed", "ig_gather_attention", "ig_layer_step", "ig_decode_step_overlapped", "ig_set_wait_limit", "ig_profile_begin", "ig_profile_end", "ig_profile_read",
     "ig_cache_attention", "ig_tree_attention", "ig_reserve_cache", "ig_append_rows", "ig_pool_evict",
+    "ig_rotary_frequencies", "ig_rotate_rows", "ig_append_pages", "ig_page_attention", "ig_reserve_pages", "ig_gather_pages",
     "ig_copy_bytes", "ig_read_bytes",
 ]
 
@@ -66,6 +70,32 @@ class IgBufferSet(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("sel_idx", "sel_cnt", "K_sel", "V_sel")]
 
 
+class IgPages(ctypes.Structure):
+    """A cache in pages of 8-bit codes: K, V [n_pages, H, page_size, d], their scales [n_pages, H], the pages of each sequence
+    [B, table_stride].  The tensors are held as long as the structure."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "table_stride", "code")] + \
+               [(n, ctypes.c_void_p) for n in ("table", "K", "V", "K_scale", "V_scale")]
+
+    def __init__(self, table, K, V, K_scale, V_scale, code=IG_CODE_I8):
+        n_pages, H, page_size, d = K.shape
+        assert K.shape == V.shape and K_scale.shape == V_scale.shape == (n_pages, H), "shapes of the pages and their scales"
+        assert K.element_size() == V.element_size() == 1 and K_scale.element_size() == V_scale.element_size() == table.element_size() == 4, \
+            "codes of a byte, float32 scales and an int32 table"
+        super().__init__(n_pages, page_size, table.shape[1], code, *map(_ptr, (table, K, V, K_scale, V_scale)))
+        self.tensors = table, K, V, K_scale, V_scale
+
+
+class IgRotary(ctypes.Structure):
+    """A rotary embedding: freq is a device tensor of dims/2 doubles (ig_rotary_frequencies), held as long as the structure."""
+    _fields_ = [("dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float), ("freq", ctypes.c_void_p)]
+
+    def __init__(self, freq, dims=None, interleaved=False, magnitude=1.0):
+        dims = 2 * freq.numel() if dims is None else dims
+        assert freq.element_size() == 8 and freq.numel() >= dims // 2, "dims/2 doubles"
+        super().__init__(dims, int(interleaved), magnitude, _ptr(freq))
+        self.tensors = freq,
+
+
 class IgError(RuntimeError):
     def __init__(self, code, message):
         super().__init__(f"infinigen error {code}: {message}")
@@ -82,7 +112,8 @@ def lib_path() -> str:
 
 _lib = None
 _vp, _i32, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
-_dp = ctypes.POINTER(IgDesc)
+_i64 = ctypes.c_int64
+_dp, _pp, _rp = ctypes.POINTER(IgDesc), ctypes.POINTER(IgPages), ctypes.POINTER(IgRotary)
 
 
 def lib():
@@ -142,6 +173,13 @@ def lib():
             "ig_reserve_cache": (ctypes.c_int, [_vp, _dp, _i32, _i32]),
             "ig_append_rows": (ctypes.c_int, [_vp, _dp, _i32] + [_vp] * 13),
             "ig_pool_evict": (ctypes.c_int, [_vp, _dp, _i32] + [_vp] * 9),
+            "ig_rotary_frequencies": (ctypes.c_int, [_vp, ctypes.c_int, ctypes.c_double, ctypes.c_int] + [ctypes.c_double] * 3 +
+                                      [_i32, _vp, ctypes.POINTER(_f32)]),
+            "ig_rotate_rows": (ctypes.c_int, [_vp, ctypes.c_int, _i32, _i32, _i32, _rp, ctypes.c_int, _vp, _vp, _i64, _vp, _i64, _vp]),
+            "ig_append_pages": (ctypes.c_int, [_vp, _dp, _pp, _rp, _i32, _i32, _vp, _vp, _vp, _i64] + [_vp] * 5),
+            "ig_page_attention": (ctypes.c_int, [_vp, _dp, _pp, _i32, _i32] + [_vp] * 5),
+            "ig_reserve_pages": (ctypes.c_int, [_vp, _dp, _i32, _i32]),
+            "ig_gather_pages": (ctypes.c_int, [_vp, _dp, _pp, _vp, _i32] + [_vp] * 4),
             "ig_set_wait_limit": (ctypes.c_int, [_vp, ctypes.c_int64]),
             "ig_profile_begin": (ctypes.c_int, [_vp]),
             "ig_profile_end": (ctypes.c_int, [_vp]),
@@ -196,13 +234,17 @@ def _current_stream():
     return handle
 
 
+def _byref(s):
+    return None if s is None else ctypes.byref(s)
+
+
 def _through_ctypes(name, *args):
     """An entry point with its arguments marshalled here: the context's address, the descriptor where there is one,
     tensors / numpy arrays / addresses / None, numbers."""
     entry = getattr(lib(), name)
     # by the parameter's type and not the argument's: a number may come as a tensor or array of one whole number, whose value
     # and not whose address is meant
-    marshal = {_vp: _ptr, _dp: ctypes.byref}
+    marshal = {_vp: _ptr, _dp: ctypes.byref, _pp: _byref, _rp: _byref}
     types = entry.argtypes
     if len(args) != len(types):
         return entry(*args)                       # (refused there)
@@ -285,6 +327,16 @@ def ig_rope_rows(q, pos, theta=10000.0, ctx=None):
     if rc != IG_OK:
         raise IgError(rc, ctx.last_error() if ctx else "ig_rope_rows")
     return q
+
+
+def ig_rotary_frequencies(dims, theta=10000.0, kind=IG_ROPE_PLAIN, factor=1.0, low=1.0, high=1.0, original=0, ctx=None):
+    """Host call. Returns (freq float64 [dims/2], magnitude): what IgRotary takes, freq as a device tensor."""
+    freq, magnitude = np.zeros(max(int(dims) // 2, 1)), _f32(1.0)
+    rc = lib().ig_rotary_frequencies(ctx._h if ctx else None, dims, float(theta), kind, float(factor), float(low), float(high), original,
+                                     _ptr(freq), ctypes.byref(magnitude))
+    if rc != IG_OK:
+        raise IgError(rc, ctx.last_error() if ctx else "ig_rotary_frequencies")
+    return freq, magnitude.value
 
 
 def ig_speculate_host(desc, q_p, slab_host, sel_stride=None, want_scores=False, threads=0, ctx=None):
@@ -490,6 +542,24 @@ class Context:
     def ig_pool_evict(self, desc, keep, kv_len, mass, born, protect_from, idx_dev, slab, Kpool, Vpool, stream=None):
         self._ck(_entries.ig_pool_evict(self._address, desc, keep, kv_len, mass, born, protect_from, idx_dev, slab,
                                         Kpool, Vpool, _stream(stream)))
+
+    def ig_rotate_rows(self, dtype, n, heads, d, rotary, inverse, pos, x, x_stride, out, out_stride, stream=None):
+        self._ck(_entries.ig_rotate_rows(self._address, dtype, n, heads, d, rotary, inverse, pos, x, x_stride, out, out_stride,
+                                         _stream(stream)))
+
+    def ig_append_pages(self, desc, pages, rotary, group, n_rows, q, k_rows, v_rows, row_stride, n_append, kv_len, pos, q_out,
+                        stream=None):
+        self._ck(_entries.ig_append_pages(self._address, desc, pages, rotary, group, n_rows, q, k_rows, v_rows, row_stride, n_append,
+                                          kv_len, pos, q_out, _stream(stream)))
+
+    def ig_page_attention(self, desc, pages, group, n_q, q, q_len, kv_len, out, stream=None):
+        self._ck(_entries.ig_page_attention(self._address, desc, pages, group, n_q, q, q_len, kv_len, out, _stream(stream)))
+
+    def ig_reserve_pages(self, desc, group, n_q):
+        self._ck(lib().ig_reserve_pages(self._h, ctypes.byref(desc), group, n_q))
+
+    def ig_gather_pages(self, desc, pages, sel_idx, sel_stride, sel_cnt, K_sel, V_sel, stream=None):
+        self._ck(_entries.ig_gather_pages(self._address, desc, pages, sel_idx, sel_stride, sel_cnt, K_sel, V_sel, _stream(stream)))
 
     def ig_set_wait_limit(self, ticks: int):
         self._ck(lib().ig_set_wait_limit(self._h, int(ticks)))

@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libinfinigen_hip.so")
 CALL = os.path.join(HERE, "_ig_call" + sysconfig.get_config_var("EXT_SUFFIX"))    # for this Python alone
-SOURCES = ["ig_api.hip", "k_scan.hip", "k_project.hip", "k_kv.hip", "k_layer.hip", "k_equalize.hip", "k_index.hip", "k_skew.hip", "k_cache.hip", "k_evict.hip",
+SOURCES = ["ig_api.hip", "k_scan.hip", "k_project.hip", "k_kv.hip", "k_layer.hip", "k_equalize.hip", "k_index.hip", "k_skew.hip", "k_cache.hip", "k_evict.hip", "k_pages.hip", "k_page_attention.hip",
            "ig_host.cpp"]
 HIPCC = "/opt/rocm/bin/hipcc"
 # packed-fp32 instruction selection is switched off for every device compile

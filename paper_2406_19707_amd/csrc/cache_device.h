@@ -25,6 +25,9 @@ struct StreamArgs {
   long logits_ld;
 };
 
+// The slices of a call joined and its rows out; mass: the weights of one token's kept logits too, or NULL.
+int ig_launch_join(ig_ctx *ctx, const ig_desc *d, const StreamArgs &a, float *mass, hipStream_t stream);
+
 // A row's weights are exp2(c s - ref) / sum.  The reference is its largest c s so far, or somewhat less; a row
 // that has seen nothing has NOTHING_SEEN, against which every weight is zero, and a sum of zero.
 constexpr float NOTHING_SEEN = -1e30f;

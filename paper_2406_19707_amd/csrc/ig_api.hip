@@ -1068,6 +1068,158 @@ int ig_pool_evict(ig_ctx *ctx, const ig_desc *d, int32_t keep, const int32_t *kv
                          (hipStream_t)stream);
 }
 
+// ---- rotary embedding on the device; pages of 8-bit codes ----
+
+static int check_rotary(ig_ctx *ctx, const char *what, const ig_rotary *r, int d) {
+  if (r->dims < 2 || r->dims % 2 || r->dims > d) return ig_fail(ctx, IG_ESHAPE, "%s: %d rotated channels of %d", what, r->dims, d);
+  if (r->interleaved != 0 && r->interleaved != 1) return ig_fail(ctx, IG_EINVAL, "%s: interleaved must be 0 or 1", what);
+  if (!isfinite(r->magnitude)) return ig_fail(ctx, IG_EINVAL, "%s: magnitude must be finite", what);
+  if (!r->freq || (uintptr_t)r->freq % 8) return ig_fail(ctx, IG_EINVAL, "%s: freq must be an 8-byte aligned array", what);
+  return IG_OK;
+}
+// bytes from the first element to behind the last one of n tokens of `row` elements, `stride` apart
+static size_t strided_bytes(long n, long row, long stride, int size) { return ((size_t)(n - 1) * stride + row) * size; }
+
+int ig_rotate_rows(ig_ctx *ctx, int dtype, int32_t n, int32_t heads, int32_t d, const ig_rotary *rotary, int inverse, const int32_t *pos,
+                   const void *x, int64_t x_stride, void *out, int64_t out_stride, void *stream) {
+  const char *what = "ig_rotate_rows";
+  if (!ctx) return IG_EINVAL;
+  ctx->call_stream = (hipStream_t)stream;
+  if (dtype != IG_F32 && dtype != IG_F16) return ig_fail(ctx, IG_EDTYPE, "unknown dtype %d", dtype);
+  if (n < 1 || heads < 1 || d < 16 || d % 16 || d > 1024) return ig_fail(ctx, IG_ESHAPE, "%s: n = %d, heads = %d, d = %d", what, n, heads, d);
+  const int size = ig_elem_bytes(dtype);
+  const long row = (long)heads * d;
+  if (row > 16777216l) return ig_fail(ctx, IG_ESHAPE, "%s: a token's heads are too many", what);
+  if (ig_rotate_threads(n, heads, d) > 2147483647l) return ig_fail(ctx, IG_ESHAPE, "%s: too many rows for a launch", what);
+  if (!rotary || !pos || !x || !out) return ig_fail(ctx, IG_EINVAL, "%s: NULL argument", what);
+  int rc = check_rotary(ctx, what, rotary, d);
+  if (rc) return rc;
+  if (inverse != 0 && inverse != 1) return ig_fail(ctx, IG_EINVAL, "%s: inverse must be 0 or 1", what);
+  if ((rc = check_aligned(ctx, what, {x, out}))) return rc;
+  for (int64_t *s : {&x_stride, &out_stride}) {
+    if (*s == 0) *s = row;
+    if (*s < row || *s > 1ll << 40 || *s * size % 16) return ig_fail(ctx, IG_ESHAPE, "%s: a stride of %lld elements", what, (long long)*s);
+  }
+  const size_t x_bytes = strided_bytes(n, row, x_stride, size), out_bytes = strided_bytes(n, row, out_stride, size);
+  if (!(x == out && x_stride == out_stride) && overlap(x, x_bytes, out, out_bytes))
+    return ig_fail(ctx, IG_EINVAL, "%s: out is neither x nor apart from it", what);
+  if (overlap(out, out_bytes, pos, (size_t)n * sizeof(int32_t)) || overlap(out, out_bytes, rotary->freq, rotary->dims / 2 * sizeof(double)))
+    return ig_fail(ctx, IG_EINVAL, "%s: out must not overlap pos or freq", what);
+  if ((rc = set_device(ctx))) return rc;
+  return ig_launch_rotate(ctx, dtype, n, heads, d, rotary, inverse, pos, x, x_stride, out, out_stride, (hipStream_t)stream);
+}
+
+// the descriptor and pages of a call over pages
+static int check_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, const char *what, int group, int n, void *stream) {
+  int rc = check_cache(ctx, d, what, group, n, true, false, stream);
+  if (rc) return rc;
+  if (!p) return ig_fail(ctx, IG_EINVAL, "%s: pages are NULL", what);
+  if (p->code != IG_CODE_I8 && p->code != IG_CODE_E4M3) return ig_fail(ctx, IG_EDTYPE, "%s: unknown code %d", what, p->code);
+  if (p->page_size != 16 && p->page_size != 32 && p->page_size != 64 && p->page_size != 128)
+    return ig_fail(ctx, IG_ESHAPE, "%s: pages of %d slots", what, p->page_size);
+  if (p->n_pages < 1 || (double)p->n_pages * d->H > 2147483647.0)
+    return ig_fail(ctx, IG_ESHAPE, "%s: %d pages", what, p->n_pages);
+  if (p->table_stride < 1 || (int64_t)p->table_stride * p->page_size < d->N_cap)
+    return ig_fail(ctx, IG_ESHAPE, "%s: %d entries of %d slots do not hold N_cap = %d", what, p->table_stride, p->page_size, d->N_cap);
+  if (!p->table || !p->K || !p->V || !p->K_scale || !p->V_scale) return ig_fail(ctx, IG_EINVAL, "%s: NULL argument among the pages", what);
+  return check_aligned(ctx, what, {p->K, p->V});
+}
+struct Part {
+  const void *p;
+  size_t n;
+};
+static bool overlaps_any(const Part &a, std::initializer_list<Part> others) {
+  for (const Part &x : others)
+    if (x.p && overlap(a.p, a.n, x.p, x.n)) return true;
+  return false;
+}
+static size_t pool_bytes(const ig_desc *d, const ig_pages *p) { return (size_t)p->n_pages * d->H * p->page_size * d->d; }
+static size_t scale_bytes(const ig_desc *d, const ig_pages *p) { return (size_t)p->n_pages * d->H * sizeof(float); }
+static size_t table_bytes(const ig_desc *d, const ig_pages *p) { return (size_t)d->B * p->table_stride * sizeof(int32_t); }
+
+int ig_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *pages, const ig_rotary *rotary, int32_t group, int32_t n_rows, const void *q,
+                    const void *k_rows, const void *v_rows, int64_t row_stride, const int32_t *n_append, const int32_t *kv_len,
+                    const int32_t *pos, void *q_out, void *stream) {
+  const char *what = "ig_append_pages";
+  if (!q) group = 1;
+  int rc = check_pages(ctx, d, pages, what, group, n_rows, stream);
+  if (rc) return rc;
+  const int Hq = q ? d->H * group : 0, size = ig_elem_bytes(d->dtype);
+  if (ig_append_pages_threads(d, pages, Hq, n_rows) > 2147483647l) return ig_fail(ctx, IG_ESHAPE, "%s: too many rows for a launch", what);
+  if (!k_rows || !v_rows || (q && !q_out)) return ig_fail(ctx, IG_EINVAL, "%s: NULL argument", what);
+  if (rotary && (rc = check_rotary(ctx, what, rotary, d->d))) return rc;
+  if ((rc = check_aligned(ctx, what, {q, k_rows, v_rows, q_out}))) return rc;
+  const long most = (long)(Hq > d->H ? Hq : d->H) * d->d;
+  if (row_stride && (row_stride < most || row_stride > 1ll << 40 || row_stride * size % 16))
+    return ig_fail(ctx, IG_ESHAPE, "%s: a stride of %lld elements", what, (long long)row_stride);
+  const long n = (long)d->B * n_rows, q_row = (long)Hq * d->d, kv_row = (long)d->H * d->d;
+  const size_t lens = d->B * sizeof(int32_t), kv_bytes = strided_bytes(n, kv_row, row_stride ? row_stride : kv_row, size);
+  const Part in[] = {{k_rows, kv_bytes}, {v_rows, kv_bytes}, {q, q ? strided_bytes(n, q_row, row_stride ? row_stride : q_row, size) : 0}};
+  const Part small[] = {{n_append, lens}, {kv_len, lens}, {pos, lens}, {pages->table, table_bytes(d, pages)},
+                        {rotary ? rotary->freq : nullptr, rotary ? rotary->dims / 2 * sizeof(double) : 0}};
+  const Part out[] = {{pages->K, pool_bytes(d, pages)}, {pages->V, pool_bytes(d, pages)}, {pages->K_scale, scale_bytes(d, pages)},
+                      {pages->V_scale, scale_bytes(d, pages)}, {q ? q_out : nullptr, (size_t)n * q_row * size}};
+  for (int o = 0; o < 5; ++o) {
+    if (!out[o].p) continue;
+    for (int x = 0; x < 3; ++x)
+      if (!(o == 4 && x == 2 && q == q_out && (!row_stride || row_stride == q_row)) && overlaps_any(out[o], {in[x]}))
+        return ig_fail(ctx, IG_EINVAL, "%s: the rows must not overlap what is written", what);
+    for (const Part &x : small)
+      if (overlaps_any(out[o], {x})) return ig_fail(ctx, IG_EINVAL, "%s: lengths, positions, table and freq must not overlap what is written", what);
+    for (int x = 0; x < o; ++x)
+      if (overlaps_any(out[o], {out[x]})) return ig_fail(ctx, IG_EINVAL, "%s: pages, scales and q_out must not overlap", what);
+  }
+  if ((rc = set_device(ctx))) return rc;
+  return ig_launch_append_pages(ctx, d, pages, rotary, Hq, n_rows, q, k_rows, v_rows, row_stride, n_append, kv_len, pos, q_out, (hipStream_t)stream);
+}
+
+int ig_reserve_pages(ig_ctx *ctx, const ig_desc *d, int32_t group, int32_t n_q) {
+  int rc = check_cache(ctx, d, "ig_reserve_pages", group, n_q, true, false, nullptr);
+  if (rc) return rc;
+  if ((rc = set_device(ctx))) return rc;
+  return ig_ensure(ctx, (void **)&ctx->cache_ws, &ctx->cache_ws_bytes, ig_page_reserve_bytes(d, group, n_q));
+}
+
+int ig_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *pages, int32_t group, int32_t n_q, const void *q, const int32_t *q_len,
+                      const int32_t *kv_len, void *out, void *stream) {
+  const char *what = "ig_page_attention";
+  int rc = check_pages(ctx, d, pages, what, group, n_q, stream);
+  if (rc) return rc;
+  const PageCall c{group, n_q, q, q_len, kv_len, out};
+  const PagePlan plan = ig_page_plan(d, c);
+  if (plan.threads > IG_MOST_THREADS) return ig_fail(ctx, IG_ESHAPE, "%s: B * H is too large for a launch", what);
+  if (!q || !out) return ig_fail(ctx, IG_EINVAL, "%s: NULL argument", what);
+  if ((rc = check_aligned(ctx, what, {q, out}))) return rc;
+  const size_t q_bytes = (size_t)d->B * n_q * d->H * group * d->d * ig_elem_bytes(d->dtype), lens = d->B * sizeof(int32_t);
+  if (overlaps_any({out, q_bytes}, {{q, q_bytes}, {pages->K, pool_bytes(d, pages)}, {pages->V, pool_bytes(d, pages)},
+                                    {pages->K_scale, scale_bytes(d, pages)}, {pages->V_scale, scale_bytes(d, pages)},
+                                    {pages->table, table_bytes(d, pages)}, {q_len, lens}, {kv_len, lens}}))
+    return ig_fail(ctx, IG_EINVAL, "%s: out must not overlap the inputs", what);
+  if ((rc = set_device(ctx))) return rc;
+  if ((rc = ig_ensure(ctx, (void **)&ctx->cache_ws, &ctx->cache_ws_bytes, plan.bytes))) return rc;
+  return ig_launch_page_attention(ctx, d, pages, c, plan, ctx->cache_ws, (hipStream_t)stream);
+}
+
+int ig_gather_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *pages, const int32_t *sel_idx, int32_t sel_stride, const int32_t *sel_cnt,
+                    void *K_sel, void *V_sel, void *stream) {
+  const char *what = "ig_gather_pages";
+  int rc = check_pages(ctx, d, pages, what, 1, 1, stream);
+  if (rc) return rc;
+  if ((rc = check_sel(ctx, sel_idx, sel_stride, sel_cnt))) return rc;
+  if (ig_gather_pages_threads(d, sel_stride) > IG_MOST_THREADS) return ig_fail(ctx, IG_ESHAPE, "%s: the lists are too large for a launch", what);
+  if (!K_sel || !V_sel) return ig_fail(ctx, IG_EINVAL, "%s: NULL argument", what);
+  if ((rc = check_aligned(ctx, what, {K_sel, V_sel}))) return rc;
+  const size_t lists = (size_t)d->B * d->H * sel_stride, bytes = lists * d->d * ig_elem_bytes(d->dtype);
+  for (const void *to : {K_sel, V_sel})
+    if (overlaps_any({to, bytes}, {{pages->K, pool_bytes(d, pages)}, {pages->V, pool_bytes(d, pages)}, {pages->K_scale, scale_bytes(d, pages)},
+                                   {pages->V_scale, scale_bytes(d, pages)}, {pages->table, table_bytes(d, pages)},
+                                   {sel_idx, lists * sizeof(int32_t)}, {sel_cnt, (size_t)d->B * d->H * sizeof(int32_t)},
+                                   {to == K_sel ? V_sel : K_sel, bytes}}))
+      return ig_fail(ctx, IG_EINVAL, "%s: K_sel and V_sel must not overlap the inputs or each other", what);
+  if ((rc = set_device(ctx))) return rc;
+  return ig_launch_gather_pages(ctx, d, pages, sel_idx, sel_stride, sel_cnt, K_sel, V_sel, (hipStream_t)stream);
+}
+
 int ig_set_wait_limit(ig_ctx *ctx, int64_t ticks) {
   if (!ctx) return IG_EINVAL;
   ctx->spin_limit = ticks == 0 ? IG_WAIT_LIMIT_DEFAULT : (long)ticks;

@@ -58,6 +58,24 @@ Outcome take(PyObject *o, const ig_desc **out) {
   PyBuffer_Release(&b);
   return whole ? TAKEN : UNKNOWN;
 }
+// a structure of pointers and numbers, by what it holds (the caller keeps it, and the tensors in it, for the length of the call)
+template <typename T> Outcome take_struct(PyObject *o, const T **out) {
+  if (o == Py_None) {
+    *out = nullptr;
+    return TAKEN;
+  }
+  Py_buffer b;
+  if (THPVariable_Check(o) || PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) {
+    PyErr_Clear();
+    return UNKNOWN;
+  }
+  *out = static_cast<const T *>(b.buf);
+  const bool whole = b.len == (Py_ssize_t)sizeof(T) && PyObject_HasAttrString(o, "_fields_");
+  PyBuffer_Release(&b);
+  return whole ? TAKEN : UNKNOWN;
+}
+Outcome take(PyObject *o, const ig_pages **out) { return take_struct<ig_pages>(o, out); }
+Outcome take(PyObject *o, const ig_rotary **out) { return take_struct<ig_rotary>(o, out); }
 template <typename T> Outcome take_const(PyObject *o, const T **out) {
   T *p = nullptr;
   const Outcome got = take<T>(o, &p);
@@ -73,6 +91,11 @@ Outcome take(PyObject *o, const ig_buffer_set **out) { return take_const<ig_buff
 Outcome take(PyObject *o, int *out) {
   if (!PyLong_CheckExact(o)) return UNKNOWN;
   *out = (int)PyLong_AsUnsignedLongMask(o);
+  return PyErr_Occurred() ? RAISED : TAKEN;
+}
+Outcome take(PyObject *o, int64_t *out) {
+  if (!PyLong_CheckExact(o)) return UNKNOWN;
+  *out = (int64_t)PyLong_AsUnsignedLongLongMask(o);
   return PyErr_Occurred() ? RAISED : TAKEN;
 }
 Outcome take(PyObject *o, double *out) {
@@ -129,7 +152,8 @@ template <typename... A> PyObject *run(const char *name, int (*f)(A...), PyObjec
   X(ig_project_indexed) X(ig_speculate_indexed) X(ig_speculate_equalized) X(ig_equalize_heads)              \
   X(ig_gather_kv) X(ig_sparse_attention) X(ig_sparse_attention_static) X(ig_sparse_attention_indexed)       \
   X(ig_gather_attention) X(ig_layer_step) X(ig_decode_step_overlapped) X(ig_skew_device)                    \
-  X(ig_partial_index_device) X(ig_cache_attention) X(ig_tree_attention) X(ig_append_rows) X(ig_pool_evict)
+  X(ig_partial_index_device) X(ig_cache_attention) X(ig_tree_attention) X(ig_append_rows) X(ig_pool_evict)  \
+  X(ig_rotate_rows) X(ig_append_pages) X(ig_page_attention) X(ig_gather_pages)
 
 #define WRAPPER(NAME) \
   PyObject *call_##NAME(PyObject *, PyObject *const *args, Py_ssize_t n) { return run(#NAME, NAME, args, n); }

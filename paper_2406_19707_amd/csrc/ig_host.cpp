@@ -1,6 +1,7 @@
 // Host-side, offline parts of the library: weight skewing and partial weight index generation.
 // Plain C++ (no GPU calls); float32 data, double arithmetic.
 #include <math.h>
+#include <cmath>
 #include <stdint.h>
 #include <string.h>
 
@@ -181,6 +182,37 @@ extern "C" int ig_rope_rows(ig_ctx *ctx, int n, int H, int d, const int32_t *pos
         row[c + half] = (float)(b * cs + a * sn);
       }
     }
+  return IG_OK;
+}
+
+extern "C" int ig_rotary_frequencies(ig_ctx *ctx, int dims, double theta, int kind, double factor, double low, double high, int32_t original,
+                                     double *freq, float *magnitude) {
+  const char *what = "ig_rotary_frequencies";
+  if (dims < 2 || dims % 2) return ig_fail(ctx, IG_ESHAPE, "%s: dims = %d must be even and positive", what, dims);
+  if (!freq) return ig_fail(ctx, IG_EINVAL, "%s: NULL argument", what);
+  if (!(theta > 1.0) || !std::isfinite(theta)) return ig_fail(ctx, IG_EINVAL, "%s: theta must be above 1", what);
+  if (kind < IG_ROPE_PLAIN || kind > IG_ROPE_WAVELENGTH) return ig_fail(ctx, IG_EINVAL, "%s: unknown kind %d", what, kind);
+  if (kind != IG_ROPE_PLAIN && (!(factor >= 1.0) || !std::isfinite(factor)))
+    return ig_fail(ctx, IG_EINVAL, "%s: factor must be at least 1", what);
+  if (kind == IG_ROPE_NTK && dims < 4) return ig_fail(ctx, IG_ESHAPE, "%s: IG_ROPE_NTK needs more than one pair", what);
+  if (kind >= IG_ROPE_RAMP && (!(low > 0.0) || !(high > low) || !std::isfinite(high) || original < 1))
+    return ig_fail(ctx, IG_EINVAL, "%s: needs 0 < low < high and original >= 1", what);
+  if (magnitude) *magnitude = kind == IG_ROPE_RAMP ? (float)(0.1 * log(factor) + 1.0) : 1.f;
+  if (kind == IG_ROPE_NTK) theta *= pow(factor, (double)dims / (double)(dims - 2));
+  const double circle = 6.28318530717958647693;
+  // the pair, not a whole number, that turns n times over `original` positions: original theta^(-2c/dims) = 2 pi n
+  auto pair_of = [&](double n) { return dims * log(original / (circle * n)) / (2.0 * log(theta)); };
+  const double first = kind == IG_ROPE_RAMP ? fmax(floor(pair_of(high)), 0.0) : 0.0;
+  const double last = kind == IG_ROPE_RAMP ? fmin(ceil(pair_of(low)), (double)(dims - 1)) : 0.0;
+  for (int c = 0; c < dims / 2; ++c) {
+    const double f = pow(theta, -2.0 * (double)c / (double)dims);
+    double kept = 1.0;                                   // the share that is not divided by factor
+    if (kind == IG_ROPE_LINEAR) kept = 0.0;
+    // (the ends can meet: then a step)
+    if (kind == IG_ROPE_RAMP) kept = 1.0 - fmin(fmax((c - first) / fmax(last - first, 0.001), 0.0), 1.0);
+    if (kind == IG_ROPE_WAVELENGTH) kept = fmin(fmax((original * f / circle - low) / (high - low), 0.0), 1.0);
+    freq[c] = f * kept + (kept < 1.0 ? f / factor * (1.0 - kept) : 0.0);
+  }
   return IG_OK;
 }
 

@@ -316,6 +316,33 @@ int ig_launch_append_rows(ig_ctx *ctx, const ig_desc *d, int n_rows, const void 
                           const int32_t *path, const int32_t *n_append, const int32_t *kv_len, const int32_t *pos,
                           const int32_t *idx, void *slab, void *Kpool, void *Vpool, float *mass, int32_t *born,
                           hipStream_t s);
+// rotation, pages of 8-bit codes (k_pages.hip)
+long ig_rotate_threads(int n, int heads, int d);
+int ig_launch_rotate(ig_ctx *ctx, int dtype, int n, int heads, int d, const ig_rotary *rotary, int inverse, const int32_t *pos, const void *x,
+                     long x_stride, void *out, long out_stride, hipStream_t s);
+long ig_append_pages_threads(const ig_desc *d, const ig_pages *p, int Hq, int n_rows);     // Hq = 0: no queries
+int ig_launch_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, const ig_rotary *rotary, int Hq, int n_rows, const void *q,
+                           const void *k, const void *v, long row_stride, const int32_t *n_append, const int32_t *kv_len, const int32_t *pos,
+                           void *q_out, hipStream_t s);
+long ig_gather_pages_threads(const ig_desc *d, int sel_stride);
+int ig_launch_gather_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, const int32_t *sel_idx, int sel_stride, const int32_t *sel_cnt,
+                           void *K_sel, void *V_sel, hipStream_t s);
+// attention over pages (k_page_attention.hip)
+struct PageCall {
+  int group, n_q;
+  const void *q;
+  const int32_t *q_len, *kv_len;
+  void *out;
+};
+struct PagePlan {
+  int rb, nrb, slices;                          // query rows of a workgroup, row blocks and slices of a pool head
+  bool prompt;
+  long threads;                                 // of the largest launch
+  size_t part_ml_at, part_at, bytes;            // parts of the workspace
+};
+PagePlan ig_page_plan(const ig_desc *d, const PageCall &c);
+size_t ig_page_reserve_bytes(const ig_desc *d, int group, int n_q);
+int ig_launch_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *pages, const PageCall &c, const PagePlan &p, char *ws, hipStream_t s);
 int ig_launch_copy(ig_ctx *ctx, const void *src, void *dst, size_t bytes, hipStream_t s);
 int ig_launch_read(ig_ctx *ctx, const void *src, size_t bytes, hipStream_t s);
 

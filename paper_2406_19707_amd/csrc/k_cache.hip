@@ -984,6 +984,32 @@ CachePlan ig_cache_plan(const ig_desc *d, const CacheCall &c) {
   return p;
 }
 
+int ig_launch_join(ig_ctx *ctx, const ig_desc *d, const StreamArgs &a, float *mass, hipStream_t stream) {
+  const bool logits = mass != nullptr;
+  const dim3 block(256);
+  const int chunks = logits && d->N ? div_up(d->N, 1024) : 1;
+  // four elements a thread where that leaves workgroups for two a compute unit (a chunk of 317 x 4 rows, 32 pools: 38 us
+  // with one, 15 with four), one where the trip through memory is what takes the time (13 rows, 32 pools: 4.2 us with
+  // four, 3.2 with one; a call for one token over 777 slots 11.0 and 10.3)
+  const int E = !logits && (long)d->B * d->H * div_up(a.R, 1024 / d->d) >= 512 ? 4 : 1;
+  const int rows = a.slices > 1 ? div_up(a.R, 256 * E / d->d) : 1;
+  const FastDiv by_chunks = ig_fast_div(chunks > rows ? chunks : rows), by_threads = ig_fast_div(d->d / E);
+  const dim3 jgrid((unsigned)((long)by_chunks.d * d->B * d->H));
+#define JOIN_AS(T, E, LOGITS)                                                                        \
+  {                                                                                                  \
+    auto k = attend_join<T, E, LOGITS>;                                                              \
+    IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, mass, (int)d->d, by_chunks, by_threads);  \
+  }
+#define JOIN(T)                                                                                      \
+  {                                                                                                  \
+    if (logits) JOIN_AS(T, 1, true)                                                                  \
+    else if (E == 4) JOIN_AS(T, 4, false)                                                            \
+    else JOIN_AS(T, 1, false)                                                                        \
+  }
+  if (d->dtype == IG_F16) JOIN(half_t) else JOIN(float)
+  return IG_OK;
+}
+
 int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const CachePlan &p, char *ws, hipStream_t stream) {
   const bool tree = c.k_tree != nullptr, logits = keeps_logits(c, p);
   const long BH = (long)d->B * d->H;
@@ -1058,28 +1084,8 @@ int ig_launch_cache(ig_ctx *ctx, const ig_desc *d, const CacheCall &c, const Cac
   } else {
     BY_DIM(float, STREAM_ROWS)
   }
-  if (p.slices > 1 || logits) {
-    const int chunks = logits && d->N ? div_up(d->N, 1024) : 1;
-    // four elements a thread where that leaves workgroups for two a compute unit (a chunk of 317 x 4 rows, 32 pools: 38 us
-    // with one, 15 with four), one where the trip through memory is what takes the time (13 rows, 32 pools: 4.2 us with
-    // four, 3.2 with one; a call for one token over 777 slots 11.0 and 10.3)
-    const int E = !logits && BH * div_up(a.R, 1024 / d->d) >= 512 ? 4 : 1;
-    const int rows = p.slices > 1 ? div_up(a.R, 256 * E / d->d) : 1;
-    const FastDiv by_chunks = ig_fast_div(chunks > rows ? chunks : rows), by_threads = ig_fast_div(d->d / E);
-    const dim3 jgrid((unsigned)(by_chunks.d * BH));
-#define JOIN_AS(T, E, LOGITS)                                                                        \
-  {                                                                                                  \
-    auto k = attend_join<T, E, LOGITS>;                                                              \
-    IG_LAUNCH(ctx, IG_K_CACHE, k, jgrid, block, stream, a, c.mass, (int)d->d, by_chunks, by_threads);\
-  }
-#define JOIN(T)                                                                                      \
-  {                                                                                                  \
-    if (logits) JOIN_AS(T, 1, true)                                                                  \
-    else if (E == 4) JOIN_AS(T, 4, false)                                                            \
-    else JOIN_AS(T, 1, false)                                                                        \
-  }
-    if (d->dtype == IG_F16) JOIN(half_t) else JOIN(float)
-  }
+  if (p.slices > 1 || logits)
+    if (int rc = ig_launch_join(ctx, d, a, logits ? c.mass : nullptr, stream)) return rc;
   if (!c.mass || logits || d->N == 0) return IG_OK;
   if (d->dtype == IG_F16) {
     // keys in pairs of blocks as the rows above: a prompt's first keys are seen by all of its rows, its last by few

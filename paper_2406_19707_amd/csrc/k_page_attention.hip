@@ -1,0 +1,367 @@
+// Attention over pages of 8-bit codes with a scale for each page and head: softmax(q K^T) V of a prompt, a chunk of one or a
+// single token, with K = 2^ek codes and V = 2^ev codes.
+#include <type_traits>
+
+#include "cache_device.h"
+#include "page_device.h"
+
+namespace {
+
+// ---- codes as operands -----------------------------------------------------------------------------------------------
+// Every code is a half exactly, so products with codes are those of half precision: eight codes as an operand.
+// An int8 code with its sign bit flipped is c + 128, and 0x6400 with that as its low byte the half 1024 + c + 128.
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+template <bool E4M3> __device__ __forceinline__ uint2 halves_of(unsigned codes) {
+  if constexpr (E4M3) {
+    return make_uint2(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, 1.f, false)),
+                      __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, 1.f, true)));
+  } else {
+    const unsigned u = codes ^ 0x80808080u, x = __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u), y = __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u);
+    const half2v off = {(half_t)1152.f, (half_t)1152.f};
+    return make_uint2(__builtin_bit_cast(unsigned, __builtin_bit_cast(half2v, x) - off), __builtin_bit_cast(unsigned, __builtin_bit_cast(half2v, y) - off));
+  }
+}
+template <bool E4M3> __device__ __forceinline__ half8 operand_of(unsigned lo, unsigned hi) {
+  const uint2 a = halves_of<E4M3>(lo), b = halves_of<E4M3>(hi);
+  return __builtin_bit_cast(half8, make_uint4(a.x, a.y, b.x, b.y));
+}
+// the words of four rows as the words of four columns: byte r of word c is byte c of row r
+__device__ __forceinline__ void transpose4(const unsigned (&r)[4], unsigned (&c)[4]) {
+  const unsigned a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), b = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u);
+  const unsigned x = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u), y = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+  c[0] = __builtin_amdgcn_perm(b, a, 0x05040100u), c[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  c[2] = __builtin_amdgcn_perm(y, x, 0x05040100u), c[3] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+}
+
+// a float as two halves: x - hi - lo is at most 2^-22 |x|, or 2^-25
+struct Halves {
+  half_t hi, lo;
+};
+__device__ __forceinline__ Halves split(float x) {
+  const half_t hi = (half_t)x;
+  return Halves{hi, (half_t)(x - (float)hi)};
+}
+
+// ---- few query rows, many cached rows ----------------------------------------------------------------------------------
+// As over a pool of rows (attend_stream): S^T = K Q^T and O^T = V^T P^T on 16x16x32 products, a query row a column, tiles of 32
+// slots dealt to the four waves of a workgroup, each with its own running reference, sums and outputs, nothing of K or V
+// through LDS.  Lane (i, g) = (lane % 16, lane / 16):
+//  - row i of the 16-row block m of S^T is the tile's slot 8 (i/4) + 4 m + i%4; a lane holds channels g d/4 .. of it, so that a
+//    wave reads whole rows, and the queries in the same order;
+//  - it supplies the weights of slots 8g .. 8g+7 and holds d/16 channels of V's rows there, whose bytes are transposed four
+//    by four.  Those eight slots lie in one page: its scales are the lane's.
+// K's scale goes into the factor of the logits.  V's scale 2^ev goes into the exponent of the weights, which are
+// exp2(l + ev - ref) with ref the largest l + ev (or LIFT less): so no page's scale takes them out of half precision's range, and
+// sums take them times 2^-ev.  Float32 queries and weights are two halves each, and their products two.
+template <int D, int NT, bool E4M3, bool F32>
+__global__ __launch_bounds__(256) void page_stream(StreamArgs a, PageRefs p) {
+  typedef typename std::conditional<F32, float, half_t>::type T;
+  constexpr int TT = 32, CJ = D / 16, RB = 16 * NT, KS = D / 32, PARTS = F32 ? 2 : 1;
+  constexpr int KW = D / 16, VB = CJ, VW = (VB + 3) / 4;  // words of a lane's part of a K row; bytes and words of a V row
+  constexpr float LIFT = 14.f;
+  constexpr int LDB = D + 4;
+  __shared__ __attribute__((aligned(16))) float boxes[4][RB * LDB];
+  __shared__ float box_m[4][RB], box_l[4][RB];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = lane & 15, g = lane >> 4;
+  int work = xcd_order(blockIdx.x, a.per_xcd);
+  if (work >= a.total) return;
+  const int h = a.by_pair.div(work);
+  work -= h * (int)a.by_pair.d;
+  const int number = a.by_units.div(work), rb = a.nrb - 1 - a.by_units.mod(work);
+  const Span span = span_of<false>(a, number);
+  if (span.b < 0) return;
+  const int b = span.b, kv = span.kv, nq = span.nq;
+
+  const int first_row = rb * RB, last_row = min(min(a.R, nq * (int)a.by_group.d), first_row + RB) - 1;
+  const bool rows_here = last_row >= first_row;
+  const int lim_min = rows_here ? row_limit<false>(a, first_row, kv, nq) : 0x7fffffff;
+  const int cached = rows_here ? row_limit<false>(a, last_row, kv, nq) : 0, tiles = (cached + TT - 1) / TT;
+  const int per = (tiles + span.slices - 1) / span.slices;
+  const int t_begin = min(tiles, span.slice * per), t_end = min(tiles, t_begin + per);
+
+  const int32_t *table = p.table + (long)b * p.stride;
+  const unsigned in_page = (1u << p.shift) - 1;
+  const char *Kh = p.K + ((unsigned long)h << p.shift) * D, *Vh = p.V + ((unsigned long)h << p.shift) * D;
+  // (slots past the last one that a row sees are read from that one)
+  const int last = cached - 1;
+  auto page_at = [&](int tile) __attribute__((always_inline)) { return page_read(p, table[min(tile * TT + 8 * g, last) >> p.shift]); };
+  unsigned k[2][KW], v[8][VW];
+  float ks = 1.f, vs = 1.f;
+  auto load_k = [&](int tile, unsigned page) __attribute__((always_inline)) {
+    const unsigned k_page = (unsigned)__shfl((int)page, (i >> 2) * 16, 64);
+    const char *base = Kh + (unsigned long)k_page * p.page_bytes + g * (D / 4);
+#pragma unroll
+    for (int m = 0; m < 2; ++m) load_words<KW>(base + (min(tile * TT + 8 * (i >> 2) + 4 * m + (i & 3), last) & in_page) * D, k[m]);
+    ks = p.K_scale[(unsigned long)page * p.H + h];
+  };
+  auto load_v = [&](int tile, unsigned page) __attribute__((always_inline)) {
+    const char *base = Vh + (unsigned long)page * p.page_bytes + VB * i;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const char *from = base + (min(tile * TT + 8 * g + u, last) & in_page) * D;
+      if constexpr (VB == 2) v[u][0] = *reinterpret_cast<const unsigned short *>(from);
+      else load_words<VW>(from, v[u]);
+    }
+    vs = p.V_scale[(unsigned long)page * p.H + h];
+  };
+
+  int tile = t_begin + w;
+  unsigned page = 0, page_next = 0;
+  if (tile < t_end) {
+    page = page_at(tile);
+    page_next = page_at(tile + 4);
+  }
+  int lim[NT];
+  float q_scale[NT];
+  half8 qf[NT][PARTS][KS];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int row = rb * RB + n * 16 + i, iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
+    lim[n] = row <= last_row ? row_limit<false>(a, row, kv, nq) : 0x7fffffff;
+    const T *src = static_cast<const T *>(a.q) + (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * (int)a.by_group.d + gq) * D + g * (D / 4);
+    q_scale[n] = 1.f;
+    if constexpr (!F32) {
+#pragma unroll
+      for (int c = 0; c < KS; ++c) qf[n][0][c] = __builtin_bit_cast(half8, flip_sign<half_t>(reinterpret_cast<const uint4 *>(src)[c], a.flip));
+    } else {
+      // a row's largest value comes to 2^13 .. 2^14, so that what the two halves leave is 2^-38 of it at most
+      float x[KS * 8], top = 0.f;
+#pragma unroll
+      for (int c = 0; c < KS * 2; ++c) {
+        const floatx4 f = __builtin_bit_cast(floatx4, flip_sign<float>(reinterpret_cast<const uint4 *>(src)[c], a.flip));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[c * 4 + e] = f[e], top = fmaxf(top, fabsf(f[e]));
+      }
+      const int e = min(max((int)(__float_as_uint(column_max(top)) >> 23), 20), 254) - 127;
+      const float by = exp2_int(13 - e);
+      q_scale[n] = exp2_int(e - 13);
+#pragma unroll
+      for (int c = 0; c < KS * 8; ++c) {
+        const Halves s = split(x[c] * by);
+        qf[n][0][c / 8][c % 8] = s.hi, qf[n][PARTS - 1][c / 8][c % 8] = s.lo;
+      }
+    }
+  }
+  if (tile < t_end) {
+    load_k(tile, page);
+    load_v(tile, page);
+  }
+
+  floatx4 acc[NT][CJ];
+  float m_run[NT], l_run[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    m_run[n] = NOTHING_SEEN;
+    l_run[n] = 0.f;
+#pragma unroll
+    for (int j = 0; j < CJ; ++j) acc[n][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  auto turn = [&](auto more_tiles) __attribute__((always_inline)) {
+    constexpr bool more = decltype(more_tiles)::value;
+    floatx4 s[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) s[n][m] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < KS; ++c)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const half8 kf = operand_of<E4M3>(k[m][2 * c], k[m][2 * c + 1]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int x = 0; x < PARTS; ++x) s[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[n][x][c], s[n][m], 0, 0, 0);
+      }
+    const int ke = scale_exponent(ks), ve = scale_exponent(vs);
+    if constexpr (more) {
+      page = page_next;
+      page_next = page_at(tile + 8);
+      load_k(tile + 4, page);
+    }
+    const float k_by = exp2_int(ke) * a.c, lift_v = (float)ve, v_back = exp2_int(-ve);
+    const int t0 = tile * TT + 8 * g;
+    if ((tile + 1) * TT > lim_min) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (t0 + 4 * m + r >= lim[n]) s[n][m][r] = -INFINITY;
+    }
+    half8 wf[NT][PARTS];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float by = k_by * q_scale[n];
+      float top = s[n][0][0];
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, s[n][m][r]);
+      top = column_max(fmaf(top, by, lift_v));
+      const float ref = fmaxf(m_run[n], lifted(top, LIFT));
+      if (__any(ref > m_run[n])) {
+        const float shrink = exp2_fast(m_run[n] - ref);
+        l_run[n] *= shrink;
+#pragma unroll
+        for (int j = 0; j < CJ; ++j) acc[n][j] *= shrink;
+        m_run[n] = ref;
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float x = exp2_fast(fmaf(s[n][m][r], by, lift_v - ref));
+          sum += x;
+          if constexpr (F32) {
+            const Halves y = split(x);
+            wf[n][0][4 * m + r] = y.hi, wf[n][PARTS - 1][4 * m + r] = y.lo;
+          } else {
+            wf[n][0][4 * m + r] = (half_t)x;
+          }
+        }
+      l_run[n] = fmaf(sum, v_back, l_run[n]);
+    }
+#pragma unroll
+    for (int x = 0; x < VW; ++x) {
+      unsigned lo[4], hi[4];
+      {
+        const unsigned r0[4] = {v[0][x], v[1][x], v[2][x], v[3][x]}, r1[4] = {v[4][x], v[5][x], v[6][x], v[7][x]};
+        transpose4(r0, lo);
+        transpose4(r1, hi);
+      }
+#pragma unroll
+      for (int j = 0; j < (CJ < 4 ? CJ : 4); ++j) {
+        const half8 vt = operand_of<E4M3>(lo[j], hi[j]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int y = 0; y < PARTS; ++y) acc[n][4 * x + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, wf[n][y], acc[n][4 * x + j], 0, 0, 0);
+      }
+    }
+    if constexpr (more) load_v(tile + 4, page);
+  };
+  for (; tile + 4 < t_end; tile += 4) turn(std::true_type());
+  if (tile < t_end) turn(std::false_type());
+
+  // the four waves' states joined, and rows out: finished ones to `out`, the states of a slice to the workspace
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    l_run[n] = column_sum(l_run[n]);
+    if (g == 0) {
+      box_m[w][n * 16 + i] = m_run[n];
+      box_l[w][n * 16 + i] = l_run[n];
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float o[CJ];
+#pragma unroll
+      for (int j = 0; j < CJ; ++j) o[j] = acc[n][j][r];
+      store_words<CJ>(boxes[w] + (n * 16 + i) * LDB + (4 * g + r) * CJ, o);
+    }
+  }
+  __syncthreads();
+  for (int u = threadIdx.x; u < RB * (D / 4); u += 256) {
+    const int at = u / (D / 4), e = u % (D / 4) * 4, row = rb * RB + at;
+    const int iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
+    if (row >= a.R || iq >= nq) continue;
+    const float m = fmaxf(fmaxf(box_m[0][at], box_m[1][at]), fmaxf(box_m[2][at], box_m[3][at]));
+    float l = 0.f;
+    floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float by = exp2_fast(box_m[x][at] - m);
+      l = fmaf(box_l[x][at], by, l);
+      o += *reinterpret_cast<const floatx4 *>(boxes[x] + at * LDB + e) * by;
+    }
+    if (a.slices == 1) {
+      const float inv = inverse_of(l);
+      T y[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) y[x] = (T)(o[x] * inv);
+      store_words<(int)sizeof(T)>(static_cast<T *>(a.out) + (((long)b * a.n_q + iq) * a.Hq + h * (int)a.by_group.d + gq) * D + e, y);
+    } else {
+      const long to = ((long)h * a.B * a.slices + number) * a.R + row;
+      *reinterpret_cast<floatx4 *>(a.part + to * D + e) = o;
+      if (e == 0) a.part_ml[to] = make_float2(m, l);
+    }
+  }
+}
+
+int div_up(long n, long d) { return (int)((n + d - 1) / d); }
+
+int row_block(const ig_desc *d, long R) { return R <= 16 || d->d > 128 || d->dtype == IG_F32 ? 16 : 32; }
+
+// Slices: as over a pool of rows, with the same units of time.
+constexpr long ROUNDS = 4, WORKGROUPS = 512;
+int slices_of(const ig_desc *d, long nrb) {
+  const long groups = d->B * (long)d->H * nrb, turns = div_up(d->N, 128);
+  long best = 1, best_cost = -1;
+  for (long s = 1; s <= MOST_SLICES && s <= turns && (s == 1 || groups * s <= ROUNDS * WORKGROUPS); ++s) {
+    const long cost = div_up(groups * s, WORKGROUPS) * (div_up(turns, s) + 2) + (s > 1 ? 3 * div_up(s, 8) : 0);
+    if (best_cost < 0 || cost < best_cost) best = s, best_cost = cost;
+  }
+  return (int)best;
+}
+
+}  // namespace
+
+PagePlan ig_page_plan(const ig_desc *d, const PageCall &c) {
+  PagePlan p = {};
+  const long R = (long)c.n_q * c.group, BH = (long)d->B * d->H;
+  p.rb = row_block(d, R);
+  p.nrb = div_up(R, p.rb);
+  p.slices = slices_of(d, p.nrb);
+  p.threads = (BH * p.slices * p.nrb + 8) * 256;
+  const size_t ml = p.slices > 1 ? BH * p.slices * R * sizeof(float2) : 0;
+  p.part_at = (ml + 255) / 256 * 256;
+  p.bytes = p.part_at + (p.slices > 1 ? BH * p.slices * R * d->d * sizeof(float) : 0);
+  return p;
+}
+
+// A bound for any number of tokens and slots up to these: states of at most MOST_SLICES slices of every row, and of at most
+// ROUNDS rounds of workgroups.
+size_t ig_page_reserve_bytes(const ig_desc *d, int group, int n_q) {
+  const long all = (long)MOST_SLICES * d->B * d->H * n_q * group, rounds = ROUNDS * WORKGROUPS * 32;
+  return (size_t)(all < rounds ? all : rounds) * (sizeof(float2) + d->d * sizeof(float)) + 2 * 256;
+}
+
+int ig_launch_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *pages, const PageCall &c, const PagePlan &p, char *ws, hipStream_t stream) {
+  const long BH = (long)d->B * d->H;
+  const PageRefs refs = ig_page_refs(d, pages);
+  StreamArgs a = {};
+  a.q = c.q, a.out = c.out, a.q_len = c.q_len, a.kv_len = c.kv_len;
+  a.n_q = c.n_q, a.R = c.n_q * c.group, a.Hq = d->H * c.group, a.N = d->N, a.N_cap = d->N_cap;
+  a.nrb = p.nrb, a.slices = p.slices, a.B = d->B, a.H = d->H, a.turn_shift = 1;
+  a.by_slices = ig_fast_div(p.slices), a.by_H = ig_fast_div(d->H), a.by_group = ig_fast_div(c.group);
+  a.flip = d->scale < 0.f ? 1 : (d->scale == 0.f ? 2 : 0);
+  a.c = (d->scale == 0.f ? 1.f : fabsf(d->scale)) * 1.44269504088896340736f;
+  a.part_ml = reinterpret_cast<float2 *>(ws);
+  a.part = reinterpret_cast<float *>(ws + p.part_at);
+  a.by_units = ig_fast_div(p.nrb), a.by_pair = ig_fast_div(d->B * p.slices * p.nrb);
+  a.total = (int)(BH * p.slices * p.nrb), a.per_xcd = div_up(a.total, 8);
+  const dim3 grid(a.per_xcd * 8), block(256);
+#define STREAM(D, NT, E4M3, F32)                                                                     \
+  {                                                                                                  \
+    auto k = page_stream<D, NT, E4M3, F32>;                                                          \
+    IG_LAUNCH(ctx, IG_K_CACHE, k, grid, block, stream, a, refs);                                     \
+  }
+#define STREAM_ROWS(D, E4M3)                                                                         \
+  {                                                                                                  \
+    if (d->dtype == IG_F32) STREAM(D, 1, E4M3, true)                                                 \
+    else if (p.rb == 16) STREAM(D, 1, E4M3, false)                                                   \
+    else if constexpr (D <= 128) STREAM(D, 2, E4M3, false)                                           \
+  }
+#define BY_DIM(DO, E4M3)                                                                             \
+  switch (d->d) {                                                                                    \
+    case 32: DO(32, E4M3) break;                                                                     \
+    case 64: DO(64, E4M3) break;                                                                     \
+    case 128: DO(128, E4M3) break;                                                                   \
+    default: DO(256, E4M3) break;                                                                    \
+  }
+  if (pages->code == IG_CODE_I8) BY_DIM(STREAM_ROWS, false) else BY_DIM(STREAM_ROWS, true)
+  return p.slices > 1 ? ig_launch_join(ctx, d, a, nullptr, stream) : IG_OK;
+}
