@@ -6,75 +6,76 @@ namespace {
 int div_up(long n, long d) { return (int)((n + d - 1) / d); }
 
 // ---- rotation ------------------------------------------------------------------------------------------------------
-// A thread takes one unit of a token, works out its eight turns once, and takes HEADS heads of it.
-constexpr int ROTATE_HEADS = 8;
+// A thread takes one unit of a token, works out its eight turns once, and takes `per` heads of it, the next head's values asked
+// for ahead.
 struct RotateArgs {
   const void *x;
   void *out;
   const int32_t *pos;
   long x_stride, out_stride;
-  int n, heads, d, chunks;            // chunks of ROTATE_HEADS heads
-  long total;                         // units of all tokens, times chunks
-  FastDiv by_units, by_chunks;
+  int heads, per, d;
+  int total;                          // units of all tokens, times their parts of `per` heads
+  FastDiv by_units, by_parts;
   RotaryRefs r;
 };
-template <typename T>
-__device__ __forceinline__ void rotate_heads(const T *x, T *out, int d, int h0, int heads, int s, int pos, const RotaryRefs &r) {
+template <typename T, int KIND>
+__device__ __forceinline__ void rotate_heads(const T *x, T *out, int d, int h0, int h1, int s, int pos, const RotaryRefs &r) {
+  Unit<T, KIND> u;
+  u.load(x + (long)h0 * d, s, r.dims);
   float2 turn[8];
-  turns_of(s, pos, r, turn);
-  for (int h = h0; h < min(h0 + ROTATE_HEADS, heads); ++h) {
-    Unit<T> u;
-    u.load(x + (long)h * d, s, r.dims, r.kind);
+  if (KIND != TURN_NONE && 16 * s < r.dims) turns_of(s, pos, r, turn);
+  for (int h = h0; h < h1; ++h) {
     float v[16];
     u.get(v);
-    rotate_unit(v, s, r.dims, r.kind, turn);
-    Unit<T>::store(out + (long)h * d, s, r.dims, r.kind, v);
+    if (h + 1 < h1) u.load(x + (long)(h + 1) * d, s, r.dims);
+    rotate_unit<KIND>(v, s, r.dims, turn);
+    Unit<T, KIND>::store(out + (long)h * d, s, r.dims, v);
   }
 }
-template <typename T> __global__ __launch_bounds__(256) void rotate_rows(RotateArgs a) {
+template <typename T, int KIND> __global__ __launch_bounds__(256) void rotate_rows(RotateArgs a) {
   const int u = blockIdx.x * 256 + threadIdx.x;
   if (u >= a.total) return;
-  const int at = a.by_units.div(u), s = u - at * (int)a.by_units.d, i = a.by_chunks.div(at), chunk = at - i * a.chunks;
-  rotate_heads<T>(static_cast<const T *>(a.x) + i * a.x_stride, static_cast<T *>(a.out) + i * a.out_stride, a.d, chunk * ROTATE_HEADS, a.heads, s,
+  const int at = a.by_units.div(u), s = u - at * (int)a.by_units.d, i = a.by_parts.div(at), h = (at - i * (int)a.by_parts.d) * a.per;
+  rotate_heads<T, KIND>(static_cast<const T *>(a.x) + i * a.x_stride, static_cast<T *>(a.out) + i * a.out_stride, a.d, h, min(h + a.per, a.heads), s,
                   a.pos[i], a.r);
 }
 
 // ---- append --------------------------------------------------------------------------------------------------------
-// A workgroup takes the new rows of one page of a sequence, head after head of APPEND_HEADS, K and V together: two
-// units of 16 channels a thread, their turns worked out once for all heads.  The largest value of a head's rows gives the scale.
-constexpr int APPEND_HEADS = 8, APPEND_UNITS = 2;
+// A workgroup takes the new rows of one page of a sequence, of K or of V, head after head of `per`: two units of 16
+// channels a thread, their turns worked out once for all heads, the next head's values asked for ahead.  The largest value
+// of a head's rows gives the scale.
+constexpr int APPEND_UNITS = 2;
 struct AppendArgs {
   PageRefs p;
   const void *q, *k, *v;
   void *q_out;
   const int32_t *n_append, *kv_len, *pos;
   long q_stride, kv_stride;
-  int B, H, Hq, N, N_cap, n_rows;
-  int pages, chunks, q_chunks;        // pages a sequence's rows touch at most, chunks of heads
-  int kv_blocks;                      // workgroups of the pages; those behind them rotate queries
-  long q_total;
-  FastDiv by_pages, by_chunks, by_rows, by_q_chunks, by_q_units;
+  int H, Hq, d, unit_shift, N, N_cap, n_rows;           // a row has 1 << unit_shift units
+  int per, q_per;                     // heads of a workgroup, and of a thread that rotates queries
+  int kv_blocks, q_total;             // workgroups of the pages; threads of those behind them, which rotate queries
+  FastDiv by_pages, by_parts, by_rows, by_q_parts;      // pages that a sequence's rows touch at most, parts of `per` heads, ..
   RotaryRefs r;
 };
 // the value to be stored: 0 for one that is not finite
 __device__ __forceinline__ float finite_or_zero(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? 0.f : x; }
 
-template <typename T, int D, bool E4M3> __global__ void append_pages(AppendArgs a) {
-  constexpr int UNITS = D / 16;
-  __shared__ float tops[2][2][16];
+template <typename T, bool E4M3, int KIND> __global__ __launch_bounds__(1024) void append_pages(AppendArgs a) {
+  __shared__ float tops[2][16];
   const int tid = threadIdx.x, team = blockDim.x;
   if ((int)blockIdx.x >= a.kv_blocks) {
     const int u = (blockIdx.x - a.kv_blocks) * team + tid;
     if (u >= a.q_total) return;
-    const int at = u / UNITS, s = u % UNITS, i = a.by_q_chunks.div(at), chunk = at - i * a.q_chunks;
+    const int at = u >> a.unit_shift, s = u & ((1 << a.unit_shift) - 1), i = a.by_q_parts.div(at), h = (at - i * (int)a.by_q_parts.d) * a.q_per;
     const int b = a.by_rows.div(i), j = i - b * a.n_rows;
     if (j >= (a.n_append ? min(max(a.n_append[b], 0), a.n_rows) : a.n_rows)) return;
     const int first = a.pos ? a.pos[b] : (a.kv_len ? min(max(a.kv_len[b], 0), a.N_cap) : a.N);
-    rotate_heads<T>(static_cast<const T *>(a.q) + i * a.q_stride, static_cast<T *>(a.q_out) + (long)i * a.Hq * D, D, chunk * ROTATE_HEADS, a.Hq, s,
+    rotate_heads<T, KIND>(static_cast<const T *>(a.q) + i * a.q_stride, static_cast<T *>(a.q_out) + (long)i * a.Hq * a.d, a.d, h, min(h + a.q_per, a.Hq), s,
                     first + j, a.r);
     return;
   }
-  const int at = a.by_pages.div(blockIdx.x), p = blockIdx.x - at * a.pages, b = a.by_chunks.div(at), chunk = at - b * a.chunks;
+  const int kv = blockIdx.x & 1, work = blockIdx.x >> 1;
+  const int at = a.by_pages.div(work), p = work - at * (int)a.by_pages.d, b = a.by_parts.div(at), h0 = (at - b * (int)a.by_parts.d) * a.per;
   const int start = a.kv_len ? min(max(a.kv_len[b], 0), a.N_cap) : a.N;
   const int n = min(a.n_append ? min(max(a.n_append[b], 0), a.n_rows) : a.n_rows, a.N_cap - start);
   const int number = (start >> a.p.shift) + p, slot0 = number << a.p.shift;
@@ -82,98 +83,92 @@ template <typename T, int D, bool E4M3> __global__ void append_pages(AppendArgs 
   if (r0 >= r1) return;
   const int entry = a.p.table[(long)b * a.p.stride + number];
   if ((unsigned)entry >= a.p.n_pages) return;
-  const int held = r0 - slot0, total = (r1 - r0) * UNITS, first_pos = (a.pos ? a.pos[b] : start) + (r0 - start);
+  const int held = r0 - slot0, total = (r1 - r0) << a.unit_shift, dims = kv ? 0 : a.r.dims;
+  const int h1 = min(h0 + a.per, a.H);
+  const T *rows = static_cast<const T *>(kv ? a.v : a.k) + ((long)b * a.n_rows + (r0 - start)) * a.kv_stride;
+  float *scales = (kv ? a.p.V_scale : a.p.K_scale) + (long)entry * a.H;
 
   int row[APPEND_UNITS], unit[APPEND_UNITS];
-  float2 turn[APPEND_UNITS][8];
   bool mine[APPEND_UNITS];
+  Unit<T, KIND> in[APPEND_UNITS];
+  float scale = 0.f;
+  // (a thread without a unit reads the first row and stores nothing)
+  auto ask = [&](int h) __attribute__((always_inline)) {
+    if (held) scale = scales[h];
+#pragma unroll
+    for (int k = 0; k < APPEND_UNITS; ++k) in[k].load(rows + row[k] * a.kv_stride + (long)h * a.d, unit[k], dims);
+  };
 #pragma unroll
   for (int k = 0; k < APPEND_UNITS; ++k) {
     const int u = tid + k * team;
     mine[k] = u < total;
-    row[k] = mine[k] ? u / UNITS : 0, unit[k] = u % UNITS;
-    turns_of(unit[k], first_pos + row[k], a.r, turn[k]);
+    row[k] = mine[k] ? u >> a.unit_shift : 0, unit[k] = u & ((1 << a.unit_shift) - 1);
   }
-  const int h_end = min((chunk + 1) * APPEND_HEADS, a.H);
-  for (int h = chunk * APPEND_HEADS; h < h_end; ++h) {
-    float x[2][APPEND_UNITS][16];                          // of K, of V
-    float top[2] = {0.f, 0.f};
+  ask(h0);
+  float2 turn[APPEND_UNITS][8];
+  if (KIND != TURN_NONE && dims) {
+    const int first_pos = (a.pos ? a.pos[b] : start) + (r0 - start);
+#pragma unroll
+    for (int k = 0; k < APPEND_UNITS; ++k)
+      if (16 * unit[k] < dims) turns_of(unit[k], first_pos + row[k], a.r, turn[k]);
+  }
+  for (int h = h0; h < h1; ++h) {
+    float x[APPEND_UNITS][16], top = 0.f;
+    int before = held ? scale_exponent(scale) : SCALE_LEAST;
+#pragma unroll
+    for (int k = 0; k < APPEND_UNITS; ++k) in[k].get(x[k]);
+    if (h + 1 < h1) ask(h + 1);
 #pragma unroll
     for (int k = 0; k < APPEND_UNITS; ++k) {
-      // (a thread without a unit reads the first row and stores nothing)
-      const long src = ((long)b * a.n_rows + (r0 - start) + row[k]) * a.kv_stride + (long)h * D;
-      Unit<T> ku, vu;
-      ku.load(static_cast<const T *>(a.k) + src, unit[k], a.r.dims, a.r.kind);
-      vu.load(static_cast<const T *>(a.v) + src, unit[k], 0, TURN_NONE);
-      ku.get(x[0][k]);
-      vu.get(x[1][k]);
-      rotate_unit(x[0][k], unit[k], a.r.dims, a.r.kind, turn[k]);
+      rotate_unit<KIND>(x[k], unit[k], dims, turn[k]);
 #pragma unroll
-      for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          x[kv][k][e] = finite_or_zero(x[kv][k][e]);
-          if (mine[k]) top[kv] = fmaxf(top[kv], fabsf(x[kv][k][e]));
-        }
+      for (int e = 0; e < 16; ++e) {
+        x[k][e] = finite_or_zero(x[k][e]);
+        if (mine[k]) top = fmaxf(top, fabsf(x[k][e]));
+      }
     }
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      top[kv] = wave_max(top[kv]);
-      if (team > 64 && tid % 64 == 0) tops[h & 1][kv][tid / 64] = top[kv];
-    }
-    const long scale_at = (long)entry * a.H + h;
-    float *scales[2] = {a.p.K_scale + scale_at, a.p.V_scale + scale_at};
-    int before[2] = {SCALE_LEAST, SCALE_LEAST};
-    if (held)
-      for (int kv = 0; kv < 2; ++kv) before[kv] = scale_exponent(*scales[kv]);
+    top = wave_max(top);
     if (team > 64) {
-      // (the scales are there before any thread may store a new one)
-      asm volatile("" : "+v"(before[0]), "+v"(before[1]));
+      if (tid % 64 == 0) tops[h & 1][tid / 64] = top;
+      // (the scale is there before any thread may store a new one)
+      asm volatile("" : "+v"(before));
       __syncthreads();
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv)
-        for (int w = 0; w < team / 64; ++w) top[kv] = fmaxf(top[kv], tops[h & 1][kv][w]);
+      for (int w = 0; w < team / 64; ++w) top = fmaxf(top, tops[h & 1][w]);
     }
+    const int e2 = max(before, exponent_for<E4M3>(top));
+    char *page = (kv ? a.p.V : a.p.K) + (unsigned long)(unsigned)entry * a.p.page_bytes + ((unsigned long)h << a.p.shift) * a.d;
+    if (held && e2 > before) {
+      const float by = exp2_int(max(before - e2, -126));
+      for (int u = tid; u < held << a.unit_shift; u += team) {
+        uint4 *c = reinterpret_cast<uint4 *>(page) + u;
+        const uint4 v = *c;
+        unsigned w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      const int e2 = max(before[kv], exponent_for<E4M3>(top[kv]));
-      char *page = (kv ? a.p.V : a.p.K) + (unsigned long)(unsigned)entry * a.p.page_bytes + ((long)h << a.p.shift) * D;
-      if (held && e2 > before[kv]) {
-        const float by = exp2_int(max(before[kv] - e2, -126));
-        for (int u = tid; u < held * (D / 16); u += team) {
-          uint4 *c = reinterpret_cast<uint4 *>(page) + u;
-          uint4 v = *c;
-          unsigned w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const floatx4 f = decode4<E4M3>(w[i]) * by;
-            w[i] = encode4<E4M3>(f[0], f[1], f[2], f[3]);
-          }
-          *c = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int i = 0; i < 4; ++i) {
+          const floatx4 f = decode4<E4M3>(w[i]) * by;
+          w[i] = encode4<E4M3>(f[0], f[1], f[2], f[3]);
         }
+        *c = make_uint4(w[0], w[1], w[2], w[3]);
       }
-      const float inv = exp2_int(-e2);
-#pragma unroll
-      for (int k = 0; k < APPEND_UNITS; ++k) {
-        if (!mine[k]) continue;
-        char *to = page + (long)(held + row[k]) * D;
-        float *f = x[kv][k];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) f[e] *= inv;
-        unsigned c[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = encode4<E4M3>(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-        if (kv == 0 && a.r.kind == TURN_ANY) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) to[any_channel(8 * unit[k] + e % 8, e / 8, a.r.dims)] = (char)(c[e / 4] >> e % 4 * 8);
-        } else {
-          const Runs at = runs_of(unit[k], a.r.dims, kv ? TURN_NONE : a.r.kind);
-          *reinterpret_cast<uint2 *>(to + at.first) = make_uint2(c[0], c[1]);
-          *reinterpret_cast<uint2 *>(to + at.second) = make_uint2(c[2], c[3]);
-        }
-      }
-      if (tid == 0 && (!held || e2 > before[kv])) *scales[kv] = exp2_int(e2);
     }
+    const float inv = exp2_int(-e2);
+#pragma unroll
+    for (int k = 0; k < APPEND_UNITS; ++k) {
+      if (!mine[k]) continue;
+      char *to = page + (long)(held + row[k]) * a.d;
+      unsigned c[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = encode4<E4M3>(x[k][4 * i] * inv, x[k][4 * i + 1] * inv, x[k][4 * i + 2] * inv, x[k][4 * i + 3] * inv);
+      if (Unit<T, KIND>::one_by_one(dims)) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) to[any_channel(8 * unit[k] + e % 8, e / 8, dims)] = (char)(c[e / 4] >> e % 4 * 8);
+      } else {
+        const Runs runs = runs_of<KIND>(unit[k], dims);
+        *reinterpret_cast<uint2 *>(to + runs.first) = make_uint2(c[0], c[1]);
+        *reinterpret_cast<uint2 *>(to + runs.second) = make_uint2(c[2], c[3]);
+      }
+    }
+    if (tid == 0 && (!held || e2 > before)) scales[h] = exp2_int(e2);
   }
 }
 
@@ -213,7 +208,13 @@ template <typename T, int D, bool E4M3> __global__ __launch_bounds__(256) void g
   }
 }
 
-int head_chunks(int heads, int per) { return (heads + per - 1) / per; }
+// Heads that are taken one after the other, so that turns are worked out once for them: one where that is what fills the GPU
+// with waves, up to eight where there are enough.
+int heads_each(int heads, double threads) {
+  int per = 1;
+  while (per < 8 && per < heads && threads / (2 * per) >= 65536.0) per *= 2;
+  return per;
+}
 // Pages that n_rows new rows of a sequence touch at most, and threads of a workgroup: a page's new rows in two units each.
 int append_page_count(const ig_pages *p, int n_rows) { return (n_rows + p->page_size - 2) / p->page_size + 1; }
 int append_team(const ig_desc *d, const ig_pages *p, int n_rows) {
@@ -223,25 +224,37 @@ int append_team(const ig_desc *d, const ig_pages *p, int n_rows) {
   return team;
 }
 
+int rotate_each(long n, int heads, int d) { return heads_each(heads, (double)n * heads * (d / 16)); }
+int append_each(const ig_desc *d, const ig_pages *p, int n_rows) {
+  return heads_each(d->H, 2.0 * d->B * append_page_count(p, n_rows) * d->H * append_team(d, p, n_rows));
+}
+
 }  // namespace
 
-long ig_rotate_threads(int n, int heads, int d) { return ((long)n * head_chunks(heads, ROTATE_HEADS) * (d / 16) + 255) / 256 * 256; }
+long ig_rotate_threads(int n, int heads, int d) { return (long)n * div_up(heads, rotate_each(n, heads, d)) * (d / 16) + 255; }
 
 int ig_launch_rotate(ig_ctx *ctx, int dtype, int n, int heads, int d, const ig_rotary *rotary, int inverse, const int32_t *pos, const void *x,
                      long x_stride, void *out, long out_stride, hipStream_t s) {
   RotateArgs a = {};
-  a.x = x, a.out = out, a.pos = pos, a.x_stride = x_stride, a.out_stride = out_stride, a.n = n, a.heads = heads, a.d = d;
-  a.chunks = head_chunks(heads, ROTATE_HEADS), a.by_units = ig_fast_div(d / 16), a.by_chunks = ig_fast_div(a.chunks);
-  a.total = (long)n * a.chunks * (d / 16);
+  a.x = x, a.out = out, a.pos = pos, a.x_stride = x_stride, a.out_stride = out_stride, a.heads = heads, a.d = d;
+  a.per = rotate_each(n, heads, d);
+  const int parts = div_up(heads, a.per);
+  a.by_units = ig_fast_div(d / 16), a.by_parts = ig_fast_div(parts);
+  a.total = n * parts * (d / 16);
   a.r = ig_rotary_refs(rotary, inverse);
   const dim3 grid((unsigned)div_up(a.total, 256)), block(256);
-  if (dtype == IG_F16) {
-    auto k = rotate_rows<half_t>;
-    IG_LAUNCH(ctx, IG_K_BUILD, k, grid, block, s, a);
-  } else {
-    auto k = rotate_rows<float>;
-    IG_LAUNCH(ctx, IG_K_BUILD, k, grid, block, s, a);
+#define ROTATE(T, KIND)                                                                              \
+  {                                                                                                  \
+    auto k = rotate_rows<T, KIND>;                                                                   \
+    IG_LAUNCH(ctx, IG_K_BUILD, k, grid, block, s, a);                                                \
   }
+#define ROTATE_KIND(T)                                                                               \
+  {                                                                                                  \
+    if (a.r.kind == TURN_HALVES) ROTATE(T, TURN_HALVES)                                              \
+    else if (a.r.kind == TURN_ADJACENT) ROTATE(T, TURN_ADJACENT)                                     \
+    else ROTATE(T, TURN_ANY)                                                                         \
+  }
+  if (dtype == IG_F16) ROTATE_KIND(half_t) else ROTATE_KIND(float)
   return IG_OK;
 }
 
@@ -262,8 +275,8 @@ int ig_launch_rotate(ig_ctx *ctx, int dtype, int n, int heads, int d, const ig_r
 
 long ig_append_pages_threads(const ig_desc *d, const ig_pages *p, int Hq, int n_rows) {
   const int team = append_team(d, p, n_rows);
-  const long kv = (long)d->B * append_page_count(p, n_rows) * head_chunks(d->H, APPEND_HEADS) * team;
-  return kv + ((long)d->B * n_rows * head_chunks(Hq, ROTATE_HEADS) * (d->d / 16) + team - 1) / team * team;
+  const long kv = 2l * d->B * append_page_count(p, n_rows) * div_up(d->H, append_each(d, p, n_rows)) * team, n = (long)d->B * n_rows;
+  return kv + (Hq ? n * div_up(Hq, rotate_each(n, Hq, d->d)) * (d->d / 16) + team : 0);
 }
 
 int ig_launch_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, const ig_rotary *rotary, int Hq, int n_rows, const void *q,
@@ -273,21 +286,33 @@ int ig_launch_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, con
   a.p = ig_page_refs(d, p);
   a.q = q, a.k = k, a.v = v, a.q_out = q_out, a.n_append = n_append, a.kv_len = kv_len, a.pos = pos;
   a.q_stride = row_stride ? row_stride : (long)Hq * d->d, a.kv_stride = row_stride ? row_stride : (long)d->H * d->d;
-  a.B = d->B, a.H = d->H, a.Hq = Hq, a.N = d->N, a.N_cap = d->N_cap, a.n_rows = n_rows;
-  a.pages = append_page_count(p, n_rows), a.chunks = head_chunks(d->H, APPEND_HEADS), a.q_chunks = head_chunks(Hq, ROTATE_HEADS);
-  a.kv_blocks = d->B * a.pages * a.chunks;
-  a.q_total = q ? (long)d->B * n_rows * a.q_chunks * (d->d / 16) : 0;
-  a.by_pages = ig_fast_div(a.pages), a.by_chunks = ig_fast_div(a.chunks), a.by_rows = ig_fast_div(n_rows);
-  a.by_q_chunks = ig_fast_div(a.q_chunks > 0 ? a.q_chunks : 1), a.by_q_units = ig_fast_div(d->d / 16);
+  a.H = d->H, a.Hq = Hq, a.d = d->d, a.unit_shift = __builtin_ctz(d->d / 16), a.N = d->N, a.N_cap = d->N_cap, a.n_rows = n_rows;
+  const int n = d->B * n_rows, pages = append_page_count(p, n_rows);
+  a.per = append_each(d, p, n_rows), a.q_per = Hq ? rotate_each(n, Hq, d->d) : 1;
+  const int parts = div_up(d->H, a.per), q_parts = Hq ? div_up(Hq, a.q_per) : 1;
+  a.kv_blocks = 2 * d->B * pages * parts;
+  a.q_total = q ? n * q_parts * (d->d / 16) : 0;
+  a.by_pages = ig_fast_div(pages), a.by_parts = ig_fast_div(parts), a.by_rows = ig_fast_div(n_rows), a.by_q_parts = ig_fast_div(q_parts);
   a.r = ig_rotary_refs(rotary, 0);
   const int team = append_team(d, p, n_rows);
   const dim3 grid((unsigned)(a.kv_blocks + div_up(a.q_total, team))), block(team);
-#define APPEND(T, D, E4M3)                                                                           \
+#define APPEND(T, E4M3, KIND)                                                                        \
   {                                                                                                  \
-    auto kernel = append_pages<T, D, E4M3>;                                                          \
+    auto kernel = append_pages<T, E4M3, KIND>;                                                       \
     IG_LAUNCH(ctx, IG_K_BUILD, kernel, grid, block, s, a);                                           \
   }
-  BY_TYPE(APPEND)
+#define APPEND_KIND(T, E4M3)                                                                         \
+  {                                                                                                  \
+    if (a.r.kind == TURN_NONE) APPEND(T, E4M3, TURN_NONE)                                            \
+    else if (a.r.kind == TURN_HALVES) APPEND(T, E4M3, TURN_HALVES)                                   \
+    else if (a.r.kind == TURN_ADJACENT) APPEND(T, E4M3, TURN_ADJACENT)                               \
+    else APPEND(T, E4M3, TURN_ANY)                                                                   \
+  }
+#define APPEND_CODE(T)                                                                               \
+  {                                                                                                  \
+    if (p->code == IG_CODE_I8) APPEND_KIND(T, false) else APPEND_KIND(T, true)                       \
+  }
+  if (d->dtype == IG_F16) APPEND_CODE(half_t) else APPEND_CODE(float)
   return IG_OK;
 }
 

@@ -71,8 +71,8 @@ static inline RotaryRefs ig_rotary_refs(const ig_rotary *r, int inverse) {
 struct Runs {
   int first, second;
 };
-__device__ __forceinline__ Runs runs_of(int s, int dims, int kind) {
-  const bool halves = kind == TURN_HALVES && 16 * s < dims;
+template <int KIND> __device__ __forceinline__ Runs runs_of(int s, int dims) {
+  const bool halves = KIND == TURN_HALVES && 16 * s < dims;
   return Runs{halves ? 8 * s : 16 * s, halves ? 8 * s + dims / 2 : 16 * s + 8};
 }
 // TURN_ANY: channel x (0: a, 1: b) of pair c
@@ -95,13 +95,14 @@ __device__ __forceinline__ float2 turn_of(int pos, double freq, const RotaryRefs
   const float cs = q & 1 ? s : c, sn = q & 1 ? c : s;
   return make_float2((q == 1 || q == 2 ? -cs : cs) * r.magnitude, (q >= 2 ? -sn : sn) * r.magnitude * r.sign);
 }
-// the eight pairs of unit s (a pair past the last one: no turn, and no factor)
+// the eight pairs of unit s (a pair past the last one: any)
 __device__ __forceinline__ void turns_of(int s, int pos, const RotaryRefs &r, float2 (&turn)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const int c = 8 * s + e;
-    turn[e] = make_float2(1.f, 0.f);
-    if (2 * c < r.dims) turn[e] = turn_of(pos, r.freq[c], r);
+    turn[e] = turn_of(pos, r.freq[min(c, r.dims / 2 - 1)], r);
+    // (one after the other: all at once they take more registers than there are)
+    asm volatile("" : "+v"(turn[e].x), "+v"(turn[e].y));
   }
 }
 // eight values of a row
@@ -142,16 +143,17 @@ template <> struct Run8<float> {
   }
 };
 
-// a unit's values: x[0 .. 7] the first run, x[8 .. 15] the second (TURN_ANY: the pairs' a, the pairs' b)
-template <typename T> struct Unit {
+// a unit's values: x[0 .. 7] the first run, x[8 .. 15] the second (channels one by one: the pairs' a, the pairs' b)
+template <typename T, int KIND> struct Unit {
   Run8<T> lo, hi;
-  __device__ __forceinline__ void load(const T *row, int s, int dims, int kind) {
-    if (kind == TURN_ANY) {
+  static __device__ __forceinline__ bool one_by_one(int dims) { return KIND == TURN_ANY && dims > 0; }
+  __device__ __forceinline__ void load(const T *row, int s, int dims) {
+    if (one_by_one(dims)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) lo.set(e, row[any_channel(8 * s + e, 0, dims)]), hi.set(e, row[any_channel(8 * s + e, 1, dims)]);
       return;
     }
-    const Runs c = runs_of(s, dims, kind);
+    const Runs c = runs_of<KIND>(s, dims);
     lo.load(row + c.first);
     hi.load(row + c.second);
   }
@@ -159,28 +161,25 @@ template <typename T> struct Unit {
     lo.get(x);
     hi.get(x + 8);
   }
-  static __device__ __forceinline__ void store(T *row, int s, int dims, int kind, const float (&x)[16]) {
-    if (kind == TURN_ANY) {
+  static __device__ __forceinline__ void store(T *row, int s, int dims, const float (&x)[16]) {
+    if (one_by_one(dims)) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) row[any_channel(8 * s + e, 0, dims)] = (T)x[e], row[any_channel(8 * s + e, 1, dims)] = (T)x[8 + e];
       return;
     }
-    const Runs c = runs_of(s, dims, kind);
+    const Runs c = runs_of<KIND>(s, dims);
     Run8<T>::store(row + c.first, x);
     Run8<T>::store(row + c.second, x + 8);
   }
 };
 // (channels that stay are not multiplied: an infinity there would make a NaN of its neighbour)
-__device__ __forceinline__ void rotate_unit(float (&x)[16], int s, int dims, int kind, const float2 (&turn)[8]) {
+template <int KIND> __device__ __forceinline__ void rotate_unit(float (&x)[16], int s, int dims, const float2 (&turn)[8]) {
+  if (KIND == TURN_NONE || 16 * s >= dims) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const bool turns = 2 * (8 * s + e) < dims;
-    if (kind == TURN_ADJACENT) {
-      const float a = x[2 * e], b = x[2 * e + 1];
-      if (turns) x[2 * e] = fmaf(a, turn[e].x, -b * turn[e].y), x[2 * e + 1] = fmaf(b, turn[e].x, a * turn[e].y);
-    } else {
-      const float a = x[e], b = x[8 + e];
-      if (turns) x[e] = fmaf(a, turn[e].x, -b * turn[e].y), x[8 + e] = fmaf(b, turn[e].x, a * turn[e].y);
-    }
+    constexpr int A = KIND == TURN_ADJACENT ? 2 : 1, B = KIND == TURN_ADJACENT ? 1 : 8;
+    const float a = x[A * e], b = x[A * e + B], y = fmaf(a, turn[e].x, -b * turn[e].y), z = fmaf(b, turn[e].x, a * turn[e].y);
+    const bool turns = KIND == TURN_HALVES || 2 * (8 * s + e) < dims;
+    x[A * e] = turns ? y : a, x[A * e + B] = turns ? z : b;
   }
 }
