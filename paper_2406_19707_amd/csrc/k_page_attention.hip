@@ -54,7 +54,7 @@ __device__ __forceinline__ Halves split(float x) {
 // exp2(l + ev - ref) with ref the largest l + ev (or LIFT less): so no page's scale takes them out of half precision's range, and
 // sums take them times 2^-ev.  Float32 queries and weights are two halves each, and their products two.
 template <int D, int NT, bool E4M3, bool F32>
-__global__ __launch_bounds__(256) void page_stream(StreamArgs a, PageRefs p) {
+__global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs a, PageRefs p) {
   typedef typename std::conditional<F32, float, half_t>::type T;
   constexpr int TT = 32, CJ = D / 16, RB = 16 * NT, KS = D / 32, PARTS = F32 ? 2 : 1;
   constexpr int KW = D / 16, VB = CJ, VW = (VB + 3) / 4;  // words of a lane's part of a K row; bytes and words of a V row
@@ -291,17 +291,305 @@ __global__ __launch_bounds__(256) void page_stream(StreamArgs a, PageRefs p) {
   }
 }
 
+// ---- many query rows, half precision -----------------------------------------------------------------------------------
+// As over a pool of rows (attend_prompt): 32x32x16 products, a wave takes 32 query rows, a workgroup 32 NW that share the tiles of
+// 64 slots; the 32-slot half blocks are a pipeline of logits, weights and outputs.  A tile's codes come to registers a turn ahead
+// and are written to LDS as halves, once for all waves; so every turn has, beside its products, the codes of one tile of K and
+// one of V to convert (16 codes: 20 vector instructions from int8, 8 from e4m3).
+// A lane's load covers at most 16 consecutive slots, i.e. one page for the whole wave.  Lane l looks after the 16 slots
+// l % 4 of a tile: their entry of the table (asked for three turns ahead), and their scales.
+constexpr float RISE = 6.f, PROMPT_LIFT = 9.f;
+constexpr int PROMPT_KEYS = 64;
+
+template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void page_prompt(StreamArgs a, PageRefs p) {
+  constexpr int KS = D / 16, OB = D / 32, TK = PROMPT_KEYS, ROWS = NW * 32;
+  constexpr int LB = TK * D / (NW * 64) < 16 ? 8 : 16;            // bytes of a lane's load
+  constexpr int PIECES = D / LB, LR = 64 / PIECES, LOADS = TK / (LR * NW);      // loads of a row; rows of a wave's load; loads of a wave
+  static_assert(LOADS >= 1 && LR <= 16, "a wave's load stays in a page");
+  constexpr int LW = LB / 4;
+  __shared__ __attribute__((aligned(16))) half_t tiles[2][2][TK * D];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i = lane & 31, hb = lane >> 5;
+  int work = xcd_order(blockIdx.x, a.per_xcd);
+  if (work >= a.total) return;
+  const int h = a.by_pair.div(work);
+  work -= h * (int)a.by_pair.d;
+  const int number = a.by_units.div(work), unit = a.by_units.mod(work);
+  const Span span = span_of<false>(a, number);
+  if (span.b < 0) return;
+  const int b = span.b, slice = span.slice, G = (int)a.by_group.d, kv = span.kv, nq = span.nq;
+  const int32_t *table = p.table + (long)b * p.stride;
+  const unsigned in_page = (1u << p.shift) - 1;
+  const unsigned long head = ((unsigned long)h << p.shift) * D;
+
+  // where this lane's loads go: rows from_row, from_row + LR, .. of a tile, as halves from channel (lane % PIECES) LB on
+  const int from_row = w * LR * LOADS + lane / PIECES, from_byte = lane % PIECES * LB;
+  // (addresses of other pieces and columns are the first one's and a constant)
+  const unsigned k_first = row_offset<D>(lane, 0), v_first = column_offset<D>(lane, 0, 0);
+
+  for (int turn = 0; turn < (a.paired ? 2 : 1); ++turn) {
+    const int rb = turn ? unit : a.nrb - 1 - unit;        // (a prompt's last rows see most: first)
+    if (turn) {
+      if (2 * unit >= a.nrb - 1) break;
+      __syncthreads();                                    // the other waves are done with the tiles
+    }
+    const int row = rb * ROWS + w * 32 + i, iq = a.by_group.div(row), gq = row - iq * G;
+    const bool live = row < a.R && iq < nq;
+    const int lim = live ? row_limit<false>(a, row, kv, nq) : 0x7fffffff;
+    const long row_at = (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * G + gq) * D;
+    const int first_row = rb * ROWS + w * 32, lim_min = row_limit<false>(a, first_row, kv, nq);
+    const int last_row = min(min(a.R, nq * G), (rb + 1) * ROWS) - 1;
+    const int most = last_row < rb * ROWS ? 0 : row_limit<false>(a, last_row, kv, nq);
+    const int tiles_all = (most + TK - 1) / TK;
+    const int per = (tiles_all + span.slices - 1) / span.slices;
+    const int t_begin = min(tiles_all, slice * per), t_end = min(tiles_all, t_begin + per);
+
+    half8 qf[KS];
+    {
+      const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const half_t *>(a.q) + row_at);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(half8, flip_sign<half_t>(src[2 * s + hb], a.flip));
+    }
+    // (slots past the last one that a row sees are read from that one; tiles past the last: the last)
+    const int last = most - 1;
+    auto entry_of = [&](int tile) __attribute__((always_inline)) {
+      return page_read(p, table[min(tile * TK + 16 * (lane & 3), last) >> p.shift]);
+    };
+    auto load_codes = [&](const char *pool, int tile, unsigned entries, unsigned (&to)[LOADS][LW]) __attribute__((always_inline)) {
+      tile = min(tile, t_end - 1);
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x) {
+        const int r0 = (w * LOADS + x) * LR;              // (rows r0 .. r0 + LR - 1: one page)
+        const unsigned page = (unsigned)__builtin_amdgcn_readlane((int)entries, r0 / 16);
+        const char *base = pool + (unsigned long)page * p.page_bytes + head;
+        load_words<LW>(base + (unsigned)((min(tile * TK + from_row + x * LR, last) & in_page) * D + from_byte), to[x]);
+      }
+    };
+    auto store_halves = [&](const unsigned (&from)[LOADS][LW], half_t *to) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x) {
+        const int r = from_row + x * LR;
+        char *at = reinterpret_cast<char *>(to) + r * D * 2;
+#pragma unroll
+        for (int y = 0; y < LW / 2; ++y)
+          *reinterpret_cast<half8 *>(at + ((from_byte / 8 + y) ^ piece_swap<D>(r)) * 16) = operand_of<E4M3>(from[x][2 * y], from[x][2 * y + 1]);
+      }
+    };
+
+    floatx16 acc[OB];
+#pragma unroll
+    for (int o = 0; o < OB; ++o)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[o][e] = 0.f;
+    float ref = NOTHING_SEEN, sum_all = 0.f;
+    floatx16 sA = {}, sB = {};
+    half8 pA[2], pB[2];
+    // scales of a tile, of the lane's 16 slots
+    struct Scales {
+      float k, v;
+    };
+
+    // now: logits in, weights out (half `now_half` of tile `now_tile`); next: the logits of rows `next_row` .. of tile K; out: acc +=
+    // the weights `old` times rows `old_row` .. of tile V
+    auto half_step = [&](auto has_now, auto has_next, auto has_old, const floatx16 &now, int now_tile, auto now_half, const Scales &scales,
+                         half8 (&weights)[2], floatx16 &next, const half_t *K, int next_row, const half8 (&old)[2],
+                         const half_t *V, int old_row) __attribute__((always_inline)) {
+      constexpr bool NOW = decltype(has_now)::value, NEXT = decltype(has_next)::value, OLD = decltype(has_old)::value;
+      constexpr int HALF = decltype(now_half)::value;
+      // (operands are read LEAD products ahead: all at once they take more registers than there are)
+      constexpr int LEAD = 3;
+      half8 kf[KS];
+      uint4 vt[2 * OB];
+      const unsigned k_at = opaque(k_first), v_at = opaque(v_first);
+      auto read = [&](int x) __attribute__((always_inline)) {
+        if constexpr (NEXT) {
+#pragma unroll
+          for (int k = x * KS / 8; k < (x + 1) * KS / 8; ++k) kf[k] = row_piece(K + next_row * D, k_at ^ k << 5);
+        }
+        if constexpr (OLD) {
+#pragma unroll
+          for (int y = x * 2 * OB / 8; y < (x + 1) * 2 * OB / 8; ++y) {
+            const half_t *rows = V + (old_row + y / OB * 16) * D;
+            const uint2 lo = column_rows<D>(rows, v_at ^ y % OB << 6, 0), hi = column_rows<D>(rows, v_at ^ (y % OB << 6 | 1 << 5), 1);
+            vt[y] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+          }
+        }
+      };
+#pragma unroll
+      for (int x = 0; x < LEAD; ++x) read(x);
+      floatx16 s;
+      float shrink = 1.f, by[2], off[2], back[2], sums[4] = {0.f, 0.f, 0.f, 0.f};
+      bool rises = false;
+      if constexpr (NOW) {
+        s = now;
+        const int t0 = now_tile * TK + HALF * 32;
+        if (t0 + 32 > lim_min) {
+          const int mine = t0 + (int)opaque(hb * 4);
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (mine + ((e / 4) * 8 + e % 4) >= lim) s[e] = -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int ke = scale_exponent(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(scales.k), HALF * 2 + x)));
+          const int ve = scale_exponent(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(scales.v), HALF * 2 + x)));
+          by[x] = exp2_int(ke) * a.c, off[x] = (float)ve, back[x] = exp2_int(-ve);
+          float m = s[8 * x];
+#pragma unroll
+          for (int e = 8 * x + 1; e < 8 * x + 8; ++e) m = __builtin_elementwise_maximum(m, s[e]);
+          top = fmaxf(top, fmaf(m, by[x], off[x]));
+        }
+        top = lifted(both_max(top), PROMPT_LIFT);
+        const float to = top > ref + RISE ? top : ref;
+        rises = __any(to != ref);
+        shrink = exp2_fast(ref - to);
+        ref = to;
+        sum_all *= shrink;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) off[x] -= ref;
+      }
+      if constexpr (NEXT) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) next[e] = 0.f;
+      }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        if (x + LEAD < 8) read(x + LEAD);
+        if constexpr (NEXT) {
+#pragma unroll
+          for (int k = x * KS / 8; k < (x + 1) * KS / 8; ++k)
+            next = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[k], qf[k], next, 0, 0, 0);
+        }
+        if constexpr (OLD) {
+#pragma unroll
+          for (int y = x * 2 * OB / 8; y < (x + 1) * 2 * OB / 8; ++y) {
+            acc[y % OB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vt[y]), old[y / OB], acc[y % OB], 0, 0, 0);
+          }
+        }
+        if constexpr (NOW) {
+#pragma unroll
+          for (int e = 2 * x; e < 2 * x + 2; ++e) {
+            const float y = exp2_fast(fmaf(s[e], by[e / 8], off[e / 8]));
+            sums[e / 8 * 2 + e % 2] += y;
+            weights[e / 8][e % 8] = (half_t)y;
+          }
+        }
+      }
+      if constexpr (NOW) {
+        sum_all = fmaf(sums[0] + sums[1], back[0], fmaf(sums[2] + sums[3], back[1], sum_all));
+        keep_here(weights[0]);
+        keep_here(weights[1]);
+        keep_here(sum_all);                               // (not put off: the weights' registers are needed)
+      }
+      if (NOW && rises) {
+#pragma unroll
+        for (int o = 0; o < OB; ++o) acc[o] *= shrink;
+      }
+    };
+    typedef std::true_type Y;
+    typedef std::false_type N;
+    typedef std::integral_constant<int, 0> H0;
+    typedef std::integral_constant<int, 1> H1;
+    if (t_end > t_begin) {
+      const int turns = t_end - t_begin;
+      unsigned k_codes[LOADS][LW], v_codes[LOADS][LW];
+      // entries of the tile that K is asked for next, and of the one after it; scales of this turn's tile, the last one's and the next
+      unsigned e0 = entry_of(t_begin), e1 = entry_of(t_begin + 1), e2 = entry_of(t_begin + 2);
+      auto scales_of = [&](unsigned entry) __attribute__((always_inline)) {
+        const unsigned long at = (unsigned long)entry * p.H + h;
+        return Scales{p.K_scale[at], p.V_scale[at]};
+      };
+      Scales now = scales_of(e0), before = now, ahead;
+      load_codes(p.K, t_begin, e0, k_codes);
+      store_halves(k_codes, tiles[0][0]);
+      load_codes(p.K, t_begin + 1, e1, k_codes);
+      load_codes(p.V, t_begin, e0, v_codes);
+      ahead = scales_of(e1);
+      // Turn r: tile r of K is in slot r % 2, of V comes to slot r % 2; the codes of K r + 1 and V r are in registers.
+      auto begin_turn = [&](int r, half_t *k_next, half_t *v_now) __attribute__((always_inline)) {
+        __syncthreads();                                  // tile r of K and r - 1 of V are there, the other slots are free
+        store_halves(k_codes, k_next);
+        store_halves(v_codes, v_now);
+        load_codes(p.K, t_begin + r + 2, e2, k_codes);
+        load_codes(p.V, t_begin + r + 1, e1, v_codes);
+        e1 = e2;
+        e2 = entry_of(t_begin + r + 3);
+      };
+      auto end_turn = [&]() __attribute__((always_inline)) {
+        before = now, now = ahead;
+        ahead = scales_of(e1);
+      };
+      auto turn_of = [&](int r, auto slot) __attribute__((always_inline)) {
+        constexpr int S = decltype(slot)::value;
+        begin_turn(r, tiles[1 - S][0], tiles[S][1]);
+        const half_t *K = tiles[S][0], *V = tiles[1 - S][1];
+        half_step(Y(), Y(), Y(), sB, t_begin + r - 1, H1(), before, pB, sA, K, 0, pA, V, 0);
+        half_step(Y(), Y(), Y(), sA, t_begin + r, H0(), now, pA, sB, K, 32, pB, V, 32);
+        end_turn();
+      };
+      begin_turn(0, tiles[1][0], tiles[0][1]);
+      half_step(N(), Y(), N(), sB, 0, H0(), now, pB, sA, tiles[0][0], 0, pA, tiles[0][1], 0);
+      half_step(Y(), Y(), N(), sA, t_begin, H0(), now, pA, sB, tiles[0][0], 32, pB, tiles[0][1], 0);
+      end_turn();
+      int r = 1;
+      // (tested at its end: tested at its beginning the compiler keeps outputs and logits twice, 75 registers more)
+      if (r + 1 < turns) do {
+        turn_of(r, H1());
+        turn_of(r + 1, H0());
+        r += 2;
+      } while (r + 1 < turns);
+      if (r < turns) turn_of(r, H1());
+      __syncthreads();
+      const half_t *V = tiles[(turns - 1) % 2][1];
+      half_step(Y(), N(), Y(), sB, t_end - 1, H1(), before, pB, sA, V, 0, pA, V, 0);
+      half_step(N(), N(), Y(), sA, 0, H0(), now, pA, sB, V, 0, pB, V, 32);
+    }
+
+    if (!live) continue;
+    const float sum = both_sum(sum_all);
+    const float inv = inverse_of(sum);
+    if (a.slices == 1) {
+      half_t *to = static_cast<half_t *>(a.out) + row_at;
+#pragma unroll
+      for (int o = 0; o < OB; ++o)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          half_t v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = (half_t)(acc[o][x * 4 + e] * inv);
+          store_words<2>(to + o * 32 + x * 8 + hb * 4, v);
+        }
+    } else {
+      const long at = ((long)h * a.B * a.slices + number) * a.R + row;
+#pragma unroll
+      for (int o = 0; o < OB; ++o)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          *reinterpret_cast<floatx4 *>(a.part + at * D + o * 32 + x * 8 + hb * 4) =
+              floatx4{acc[o][x * 4], acc[o][x * 4 + 1], acc[o][x * 4 + 2], acc[o][x * 4 + 3]};
+      if (hb == 0) a.part_ml[at] = make_float2(ref, sum);
+    }
+  }
+}
+
 int div_up(long n, long d) { return (int)((n + d - 1) / d); }
 
+// Query rows of a workgroup: page_stream's 16 or 32, page_prompt's 128 or 256 (as over a pool of rows, by the same rules).
 int row_block(const ig_desc *d, long R) { return R <= 16 || d->d > 128 || d->dtype == IG_F32 ? 16 : 32; }
+bool many_rows(const ig_desc *d, long R) { return d->dtype == IG_F16 && R > (d->d > 128 ? 16 : 32); }
+int prompt_rows(const ig_desc *d, const PageCall &c) {
+  return d->d >= 64 && d->d <= 128 && (long)c.n_q * c.group > 128 && 2 * (long)c.n_q <= d->N ? 256 : 128;
+}
 
 // Slices: as over a pool of rows, with the same units of time.
-constexpr long ROUNDS = 4, WORKGROUPS = 512;
-int slices_of(const ig_desc *d, long nrb) {
-  const long groups = d->B * (long)d->H * nrb, turns = div_up(d->N, 128);
+constexpr long ROUNDS = 4;
+long workgroups_of(int rb) { return rb == 256 ? 256 : 512; }
+int slices_of(const ig_desc *d, const PagePlan &p) {
+  const long groups = d->B * (long)d->H * p.nrb, turns = div_up(d->N, p.prompt ? 64 : 128), at_once = workgroups_of(p.rb);
   long best = 1, best_cost = -1;
-  for (long s = 1; s <= MOST_SLICES && s <= turns && (s == 1 || groups * s <= ROUNDS * WORKGROUPS); ++s) {
-    const long cost = div_up(groups * s, WORKGROUPS) * (div_up(turns, s) + 2) + (s > 1 ? 3 * div_up(s, 8) : 0);
+  for (long s = 1; s <= MOST_SLICES && s <= turns && (s == 1 || groups * s <= ROUNDS * at_once); ++s) {
+    const long cost = div_up(groups * s, at_once) * (div_up(turns, s) + 2) + (s > 1 ? 3 * div_up(s, 8) : 0);
     if (best_cost < 0 || cost < best_cost) best = s, best_cost = cost;
   }
   return (int)best;
@@ -312,10 +600,11 @@ int slices_of(const ig_desc *d, long nrb) {
 PagePlan ig_page_plan(const ig_desc *d, const PageCall &c) {
   PagePlan p = {};
   const long R = (long)c.n_q * c.group, BH = (long)d->B * d->H;
-  p.rb = row_block(d, R);
+  p.prompt = many_rows(d, R);
+  p.rb = p.prompt ? prompt_rows(d, c) : row_block(d, R);
   p.nrb = div_up(R, p.rb);
-  p.slices = slices_of(d, p.nrb);
-  p.threads = (BH * p.slices * p.nrb + 8) * 256;
+  p.slices = slices_of(d, p);
+  p.threads = (BH * p.slices * p.nrb + 8) * (p.rb == 256 ? 512 : 256);
   const size_t ml = p.slices > 1 ? BH * p.slices * R * sizeof(float2) : 0;
   p.part_at = (ml + 255) / 256 * 256;
   p.bytes = p.part_at + (p.slices > 1 ? BH * p.slices * R * d->d * sizeof(float) : 0);
@@ -325,7 +614,7 @@ PagePlan ig_page_plan(const ig_desc *d, const PageCall &c) {
 // A bound for any number of tokens and slots up to these: states of at most MOST_SLICES slices of every row, and of at most
 // ROUNDS rounds of workgroups.
 size_t ig_page_reserve_bytes(const ig_desc *d, int group, int n_q) {
-  const long all = (long)MOST_SLICES * d->B * d->H * n_q * group, rounds = ROUNDS * WORKGROUPS * 32;
+  const long all = (long)MOST_SLICES * d->B * d->H * n_q * group, rounds = ROUNDS * (d->dtype == IG_F16 ? 256 * workgroups_of(256) : 16 * workgroups_of(16));
   return (size_t)(all < rounds ? all : rounds) * (sizeof(float2) + d->d * sizeof(float)) + 2 * 256;
 }
 
@@ -335,19 +624,35 @@ int ig_launch_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *page
   StreamArgs a = {};
   a.q = c.q, a.out = c.out, a.q_len = c.q_len, a.kv_len = c.kv_len;
   a.n_q = c.n_q, a.R = c.n_q * c.group, a.Hq = d->H * c.group, a.N = d->N, a.N_cap = d->N_cap;
-  a.nrb = p.nrb, a.slices = p.slices, a.B = d->B, a.H = d->H, a.turn_shift = 1;
+  a.nrb = p.nrb, a.slices = p.slices, a.B = d->B, a.H = d->H, a.turn_shift = !p.prompt;
   a.by_slices = ig_fast_div(p.slices), a.by_H = ig_fast_div(d->H), a.by_group = ig_fast_div(c.group);
   a.flip = d->scale < 0.f ? 1 : (d->scale == 0.f ? 2 : 0);
   a.c = (d->scale == 0.f ? 1.f : fabsf(d->scale)) * 1.44269504088896340736f;
   a.part_ml = reinterpret_cast<float2 *>(ws);
   a.part = reinterpret_cast<float *>(ws + p.part_at);
-  a.by_units = ig_fast_div(p.nrb), a.by_pair = ig_fast_div(d->B * p.slices * p.nrb);
-  a.total = (int)(BH * p.slices * p.nrb), a.per_xcd = div_up(a.total, 8);
+  // a causal call with workgroups to spare: each takes a late and an early row block, so that all take equally long
+  a.paired = p.prompt && p.slices == 1 && BH * p.nrb >= 1024 && 2 * c.n_q > d->N;
+  const int units = a.paired ? (p.nrb + 1) / 2 : p.nrb;
+  a.by_units = ig_fast_div(units), a.by_pair = ig_fast_div(d->B * p.slices * units);
+  a.total = (int)(BH * p.slices * units), a.per_xcd = div_up(a.total, 8);
   const dim3 grid(a.per_xcd * 8), block(256);
 #define STREAM(D, NT, E4M3, F32)                                                                     \
   {                                                                                                  \
     auto k = page_stream<D, NT, E4M3, F32>;                                                          \
     IG_LAUNCH(ctx, IG_K_CACHE, k, grid, block, stream, a, refs);                                     \
+  }
+#define PROMPT_WAVES(D, NW, E4M3)                                                                     \
+  {                                                                                                  \
+    auto k = page_prompt<D, NW, E4M3>;                                                               \
+    IG_LAUNCH(ctx, IG_K_CACHE, k, grid, dim3(NW * 64), stream, a, refs);                             \
+  }
+#define PROMPT(D, E4M3)                                                                              \
+  {                                                                                                  \
+    if constexpr (D == 64 || D == 128) {                                                             \
+      if (p.rb == 256) PROMPT_WAVES(D, 8, E4M3)                                                      \
+      else PROMPT_WAVES(D, 4, E4M3)                                                                  \
+    } else                                                                                           \
+      PROMPT_WAVES(D, 4, E4M3)                                                                       \
   }
 #define STREAM_ROWS(D, E4M3)                                                                         \
   {                                                                                                  \
@@ -362,6 +667,10 @@ int ig_launch_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *page
     case 128: DO(128, E4M3) break;                                                                   \
     default: DO(256, E4M3) break;                                                                    \
   }
-  if (pages->code == IG_CODE_I8) BY_DIM(STREAM_ROWS, false) else BY_DIM(STREAM_ROWS, true)
+  if (p.prompt) {
+    if (pages->code == IG_CODE_I8) BY_DIM(PROMPT, false) else BY_DIM(PROMPT, true)
+  } else {
+    if (pages->code == IG_CODE_I8) BY_DIM(STREAM_ROWS, false) else BY_DIM(STREAM_ROWS, true)
+  }
   return p.slices > 1 ? ig_launch_join(ctx, d, a, nullptr, stream) : IG_OK;
 }
