@@ -365,14 +365,14 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
         load_words<LW>(base + (unsigned)((min(tile * TK + from_row + x * LR, last) & in_page) * D + from_byte), to[x]);
       }
     };
-    auto store_halves = [&](const unsigned (&from)[LOADS][LW], half_t *to) __attribute__((always_inline)) {
+    // part `x` of eight of a tile's codes to LDS as halves
+    constexpr int RUNS = LOADS * LW / 2;                  // runs of eight codes that a lane holds
+    auto store_halves = [&](int x, const unsigned (&from)[LOADS][LW], half_t *to) __attribute__((always_inline)) {
 #pragma unroll
-      for (int x = 0; x < LOADS; ++x) {
-        const int r = from_row + x * LR;
-        char *at = reinterpret_cast<char *>(to) + r * D * 2;
-#pragma unroll
-        for (int y = 0; y < LW / 2; ++y)
-          *reinterpret_cast<half8 *>(at + ((from_byte / 8 + y) ^ piece_swap<D>(r)) * 16) = operand_of<E4M3>(from[x][2 * y], from[x][2 * y + 1]);
+      for (int u = x * RUNS / 8; u < (x + 1) * RUNS / 8; ++u) {
+        const int l = u / (LW / 2), y = u % (LW / 2), r = from_row + l * LR;
+        *reinterpret_cast<half8 *>(reinterpret_cast<char *>(to) + r * D * 2 + ((from_byte / 8 + y) ^ piece_swap<D>(r)) * 16) =
+            operand_of<E4M3>(from[l][2 * y], from[l][2 * y + 1]);
       }
     };
 
@@ -384,16 +384,16 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
     float ref = NOTHING_SEEN, sum_all = 0.f;
     floatx16 sA = {}, sB = {};
     half8 pA[2], pB[2];
-    // scales of a tile, of the lane's 16 slots
+    // of the lane's 16 slots of a tile: the factor of logits, the exponent of V's scale and 1 / that scale
     struct Scales {
-      float k, v;
+      float k, v, back;
     };
 
     // now: logits in, weights out (half `now_half` of tile `now_tile`); next: the logits of rows `next_row` .. of tile K; out: acc +=
     // the weights `old` times rows `old_row` .. of tile V
     auto half_step = [&](auto has_now, auto has_next, auto has_old, const floatx16 &now, int now_tile, auto now_half, const Scales &scales,
                          half8 (&weights)[2], floatx16 &next, const half_t *K, int next_row, const half8 (&old)[2],
-                         const half_t *V, int old_row) __attribute__((always_inline)) {
+                         const half_t *V, int old_row, auto store) __attribute__((always_inline)) {
       constexpr bool NOW = decltype(has_now)::value, NEXT = decltype(has_next)::value, OLD = decltype(has_old)::value;
       constexpr int HALF = decltype(now_half)::value;
       // (operands are read LEAD products ahead: all at once they take more registers than there are)
@@ -432,9 +432,8 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
         float top = -INFINITY;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const int ke = scale_exponent(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(scales.k), HALF * 2 + x)));
-          const int ve = scale_exponent(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(scales.v), HALF * 2 + x)));
-          by[x] = exp2_int(ke) * a.c, off[x] = (float)ve, back[x] = exp2_int(-ve);
+          auto of = [&](float y) __attribute__((always_inline)) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y), HALF * 2 + x)); };
+          by[x] = of(scales.k), off[x] = of(scales.v), back[x] = of(scales.back);
           float m = s[8 * x];
 #pragma unroll
           for (int e = 8 * x + 1; e < 8 * x + 8; ++e) m = __builtin_elementwise_maximum(m, s[e]);
@@ -456,6 +455,7 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
         if (x + LEAD < 8) read(x + LEAD);
+        store(x);
         if constexpr (NEXT) {
 #pragma unroll
           for (int k = x * KS / 8; k < (x + 1) * KS / 8; ++k)
@@ -498,40 +498,48 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
       unsigned e0 = entry_of(t_begin), e1 = entry_of(t_begin + 1), e2 = entry_of(t_begin + 2);
       auto scales_of = [&](unsigned entry) __attribute__((always_inline)) {
         const unsigned long at = (unsigned long)entry * p.H + h;
-        return Scales{p.K_scale[at], p.V_scale[at]};
+        return make_float2(p.K_scale[at], p.V_scale[at]);
       };
-      Scales now = scales_of(e0), before = now, ahead;
+      auto ready = [&](float2 s) __attribute__((always_inline)) {
+        const int ke = scale_exponent(s.x), ve = scale_exponent(s.y);
+        return Scales{exp2_int(ke) * a.c, (float)ve, exp2_int(-ve)};
+      };
+      Scales now = ready(scales_of(e0)), before = now;
+      float2 ahead;
       load_codes(p.K, t_begin, e0, k_codes);
-      store_halves(k_codes, tiles[0][0]);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) store_halves(x, k_codes, tiles[0][0]);
       load_codes(p.K, t_begin + 1, e1, k_codes);
       load_codes(p.V, t_begin, e0, v_codes);
       ahead = scales_of(e1);
-      // Turn r: tile r of K is in slot r % 2, of V comes to slot r % 2; the codes of K r + 1 and V r are in registers.
-      auto begin_turn = [&](int r, half_t *k_next, half_t *v_now) __attribute__((always_inline)) {
-        __syncthreads();                                  // tile r of K and r - 1 of V are there, the other slots are free
-        store_halves(k_codes, k_next);
-        store_halves(v_codes, v_now);
-        load_codes(p.K, t_begin + r + 2, e2, k_codes);
+      // Turn r: tile r of K is in slot r % 2, r - 1 of V in the other one; the codes of K r + 1 and V r are in registers and go to the
+      // free slots among the products, K's in the first half, V's in the second.
+      auto to_slot = [&](const unsigned (&codes)[LOADS][LW], half_t *to) __attribute__((always_inline)) {
+        return [&codes, to, &store_halves](int x) __attribute__((always_inline)) { store_halves(x, codes, to); };
+      };
+      auto nothing = [](int) __attribute__((always_inline)) {};
+      auto middle = [&](int r) __attribute__((always_inline)) { load_codes(p.K, t_begin + r + 2, e2, k_codes); };
+      auto end_turn = [&](int r) __attribute__((always_inline)) {
         load_codes(p.V, t_begin + r + 1, e1, v_codes);
         e1 = e2;
         e2 = entry_of(t_begin + r + 3);
-      };
-      auto end_turn = [&]() __attribute__((always_inline)) {
-        before = now, now = ahead;
+        before = now, now = ready(ahead);
         ahead = scales_of(e1);
+        __syncthreads();                                  // the next turn's tiles are there, and the other slots are free
       };
       auto turn_of = [&](int r, auto slot) __attribute__((always_inline)) {
         constexpr int S = decltype(slot)::value;
-        begin_turn(r, tiles[1 - S][0], tiles[S][1]);
         const half_t *K = tiles[S][0], *V = tiles[1 - S][1];
-        half_step(Y(), Y(), Y(), sB, t_begin + r - 1, H1(), before, pB, sA, K, 0, pA, V, 0);
-        half_step(Y(), Y(), Y(), sA, t_begin + r, H0(), now, pA, sB, K, 32, pB, V, 32);
-        end_turn();
+        half_step(Y(), Y(), Y(), sB, t_begin + r - 1, H1(), before, pB, sA, K, 0, pA, V, 0, to_slot(k_codes, tiles[1 - S][0]));
+        middle(r);
+        half_step(Y(), Y(), Y(), sA, t_begin + r, H0(), now, pA, sB, K, 32, pB, V, 32, to_slot(v_codes, tiles[S][1]));
+        end_turn(r);
       };
-      begin_turn(0, tiles[1][0], tiles[0][1]);
-      half_step(N(), Y(), N(), sB, 0, H0(), now, pB, sA, tiles[0][0], 0, pA, tiles[0][1], 0);
-      half_step(Y(), Y(), N(), sA, t_begin, H0(), now, pA, sB, tiles[0][0], 32, pB, tiles[0][1], 0);
-      end_turn();
+      __syncthreads();
+      half_step(N(), Y(), N(), sB, 0, H0(), now, pB, sA, tiles[0][0], 0, pA, tiles[0][1], 0, to_slot(k_codes, tiles[1][0]));
+      middle(0);
+      half_step(Y(), Y(), N(), sA, t_begin, H0(), now, pA, sB, tiles[0][0], 32, pB, tiles[0][1], 0, to_slot(v_codes, tiles[0][1]));
+      end_turn(0);
       int r = 1;
       // (tested at its end: tested at its beginning the compiler keeps outputs and logits twice, 75 registers more)
       if (r + 1 < turns) do {
@@ -540,10 +548,9 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
         r += 2;
       } while (r + 1 < turns);
       if (r < turns) turn_of(r, H1());
-      __syncthreads();
       const half_t *V = tiles[(turns - 1) % 2][1];
-      half_step(Y(), N(), Y(), sB, t_end - 1, H1(), before, pB, sA, V, 0, pA, V, 0);
-      half_step(N(), N(), Y(), sA, 0, H0(), now, pA, sB, V, 0, pB, V, 32);
+      half_step(Y(), N(), Y(), sB, t_end - 1, H1(), before, pB, sA, V, 0, pA, V, 0, nothing);
+      half_step(N(), N(), Y(), sA, 0, H0(), now, pA, sB, V, 0, pB, V, 32, nothing);
     }
 
     if (!live) continue;
