@@ -46,8 +46,8 @@ __device__ __forceinline__ Halves split(float x) {
 // As over a pool of rows (attend_stream): S^T = K Q^T and O^T = V^T P^T on 16x16x32 products, a query row a column, tiles of 32
 // slots dealt to the four waves of a workgroup, each with its own running reference, sums and outputs, nothing of K or V
 // through LDS.  Lane (i, g) = (lane % 16, lane / 16):
-//  - row i of the 16-row block m of S^T is the tile's slot 8 (i/4) + 4 m + i%4; a lane holds channels g d/4 .. of it, so that a
-//    wave reads whole rows, and the queries in the same order;
+//  - row i of the 16-row block m of S^T is the tile's slot 8 (i/4) + 4 m + i%4; a lane holds 16 bytes of every 64 of it (d = 32:
+//    8 of 32), so that a load is whole sectors of 16 rows, and the queries in the same order;
 //  - it supplies the weights of slots 8g .. 8g+7 and holds d/16 channels of V's rows there, whose bytes are transposed four
 //    by four.  Those eight slots lie in one page: its scales are the lane's.
 // K's scale goes into the factor of the logits.  V's scale 2^ev goes into the exponent of the weights, which are
@@ -57,7 +57,8 @@ template <int D, int NT, bool E4M3, bool F32>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs a, PageRefs p) {
   typedef typename std::conditional<F32, float, half_t>::type T;
   constexpr int TT = 32, CJ = D / 16, RB = 16 * NT, KS = D / 32, PARTS = F32 ? 2 : 1;
-  constexpr int KW = D / 16, VB = CJ, VW = (VB + 3) / 4;  // words of a lane's part of a K row; bytes and words of a V row
+  constexpr int KB = D < 64 ? 8 : 16, KW = D / 16;        // bytes of a load of K; words of a lane's part of a row
+  constexpr int VB = CJ, VW = (VB + 3) / 4;               // bytes and words of a lane's part of a V row
   constexpr float LIFT = 14.f;
   constexpr int LDB = D + 4;
   __shared__ __attribute__((aligned(16))) float boxes[4][RB * LDB];
@@ -90,9 +91,13 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
   float ks = 1.f, vs = 1.f;
   auto load_k = [&](int tile, unsigned page) __attribute__((always_inline)) {
     const unsigned k_page = (unsigned)__shfl((int)page, (i >> 2) * 16, 64);
-    const char *base = Kh + (unsigned long)k_page * p.page_bytes + g * (D / 4);
+    const char *base = Kh + (unsigned long)k_page * p.page_bytes + g * KB;
 #pragma unroll
-    for (int m = 0; m < 2; ++m) load_words<KW>(base + (min(tile * TT + 8 * (i >> 2) + 4 * m + (i & 3), last) & in_page) * D, k[m]);
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int c = 0; c < D / (4 * KB); ++c)
+        load_words<KB / 4>(base + (min(tile * TT + 8 * (i >> 2) + 4 * m + (i & 3), last) & in_page) * D + c * 4 * KB,
+                           reinterpret_cast<unsigned (&)[KB / 4]>(k[m][c * (KB / 4)]));
     ks = p.K_scale[(unsigned long)page * p.H + h];
   };
   auto load_v = [&](int tile, unsigned page) __attribute__((always_inline)) {
@@ -119,17 +124,19 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
   for (int n = 0; n < NT; ++n) {
     const int row = rb * RB + n * 16 + i, iq = a.by_group.div(row), gq = row - iq * (int)a.by_group.d;
     lim[n] = row <= last_row ? row_limit<false>(a, row, kv, nq) : 0x7fffffff;
-    const T *src = static_cast<const T *>(a.q) + (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * (int)a.by_group.d + gq) * D + g * (D / 4);
+    const T *src = static_cast<const T *>(a.q) + (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * (int)a.by_group.d + gq) * D;
+    // (the eight channels of product c of this lane)
+    auto channel = [&](int c) { return KB == 8 ? 8 * g : c / 2 * 64 + g * 16 + c % 2 * 8; };
     q_scale[n] = 1.f;
     if constexpr (!F32) {
 #pragma unroll
-      for (int c = 0; c < KS; ++c) qf[n][0][c] = __builtin_bit_cast(half8, flip_sign<half_t>(reinterpret_cast<const uint4 *>(src)[c], a.flip));
+      for (int c = 0; c < KS; ++c) qf[n][0][c] = __builtin_bit_cast(half8, flip_sign<half_t>(*reinterpret_cast<const uint4 *>(src + channel(c)), a.flip));
     } else {
       // a row's largest value comes to 2^13 .. 2^14, so that what the two halves leave is 2^-38 of it at most
       float x[KS * 8], top = 0.f;
 #pragma unroll
       for (int c = 0; c < KS * 2; ++c) {
-        const floatx4 f = __builtin_bit_cast(floatx4, flip_sign<float>(reinterpret_cast<const uint4 *>(src)[c], a.flip));
+        const floatx4 f = __builtin_bit_cast(floatx4, flip_sign<float>(reinterpret_cast<const uint4 *>(src + channel(c / 2))[c % 2], a.flip));
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[c * 4 + e] = f[e], top = fmaxf(top, fabsf(f[e]));
       }
