@@ -87,8 +87,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
   // (slots past the last one that a row sees are read from that one)
   const int last = cached - 1;
   auto page_at = [&](int tile) __attribute__((always_inline)) { return page_read(p, table[min(tile * TT + 8 * g, last) >> p.shift]); };
-  unsigned k[2][KW], v[8][VW];
-  float ks = 1.f, vs = 1.f;
+  unsigned k[2][KW], v[2][8][VW];                         // (of V this tile's and the next one's)
+  float ks = 1.f, vs[2] = {1.f, 1.f};
   auto load_k = [&](int tile, unsigned page) __attribute__((always_inline)) {
     const unsigned k_page = (unsigned)__shfl((int)page, (i >> 2) * 16, 64);
     const char *base = Kh + (unsigned long)k_page * p.page_bytes + g * KB;
@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
                            reinterpret_cast<unsigned (&)[KB / 4]>(k[m][c * (KB / 4)]));
     ks = p.K_scale[(unsigned long)page * p.H + h];
   };
-  auto load_v = [&](int tile, unsigned page) __attribute__((always_inline)) {
+  auto load_v = [&](int tile, unsigned page, unsigned (&v)[8][VW], float &vs) __attribute__((always_inline)) {
     const char *base = Vh + (unsigned long)page * p.page_bytes + VB * i;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
   }
   if (tile < t_end) {
     load_k(tile, page);
-    load_v(tile, page);
+    load_v(tile, page, v[0], vs[0]);
   }
 
   floatx4 acc[NT][CJ];
@@ -164,8 +164,9 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
 #pragma unroll
     for (int j = 0; j < CJ; ++j) acc[n][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  auto turn = [&](auto more_tiles) __attribute__((always_inline)) {
+  auto turn = [&](auto more_tiles, auto buffer) __attribute__((always_inline)) {
     constexpr bool more = decltype(more_tiles)::value;
+    constexpr int NOW = decltype(buffer)::value;
     floatx4 s[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -181,11 +182,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
 #pragma unroll
           for (int x = 0; x < PARTS; ++x) s[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[n][x][c], s[n][m], 0, 0, 0);
       }
-    const int ke = scale_exponent(ks), ve = scale_exponent(vs);
+    const int ke = scale_exponent(ks), ve = scale_exponent(vs[NOW]);
     if constexpr (more) {
       page = page_next;
       page_next = page_at(tile + 8);
       load_k(tile + 4, page);
+      load_v(tile + 4, page, v[1 - NOW], vs[1 - NOW]);
     }
     const float k_by = exp2_int(ke) * a.c, lift_v = (float)ve, v_back = exp2_int(-ve);
     const int t0 = tile * TT + 8 * g;
@@ -236,7 +238,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
     for (int x = 0; x < VW; ++x) {
       unsigned lo[4], hi[4];
       {
-        const unsigned r0[4] = {v[0][x], v[1][x], v[2][x], v[3][x]}, r1[4] = {v[4][x], v[5][x], v[6][x], v[7][x]};
+        const unsigned r0[4] = {v[NOW][0][x], v[NOW][1][x], v[NOW][2][x], v[NOW][3][x]};
+        const unsigned r1[4] = {v[NOW][4][x], v[NOW][5][x], v[NOW][6][x], v[NOW][7][x]};
         transpose4(r0, lo);
         transpose4(r1, hi);
       }
@@ -249,10 +252,22 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
           for (int y = 0; y < PARTS; ++y) acc[n][4 * x + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vt, wf[n][y], acc[n][4 * x + j], 0, 0, 0);
       }
     }
-    if constexpr (more) load_v(tile + 4, page);
   };
-  for (; tile + 4 < t_end; tile += 4) turn(std::true_type());
-  if (tile < t_end) turn(std::false_type());
+  typedef std::integral_constant<int, 0> B0;
+  typedef std::integral_constant<int, 1> B1;
+  for (; tile + 8 < t_end; tile += 8) {
+    turn(std::true_type(), B0());
+    tile += 4;
+    turn(std::true_type(), B1());
+    tile -= 4;
+  }
+  if (tile + 4 < t_end) {
+    turn(std::true_type(), B0());
+    tile += 4;
+    turn(std::false_type(), B1());
+  } else if (tile < t_end) {
+    turn(std::false_type(), B0());
+  }
 
   // the four waves' states joined, and rows out: finished ones to `out`, the states of a slice to the workspace
 #pragma unroll
@@ -596,14 +611,24 @@ int prompt_rows(const ig_desc *d, const PageCall &c) {
   return d->d >= 64 && d->d <= 128 && (long)c.n_q * c.group > 128 && 2 * (long)c.n_q <= d->N ? 256 : 128;
 }
 
-// Slices: as over a pool of rows, with the same units of time.
+// Slices that the slots of a pool head are cut into: the number for which the last workgroups end first.  page_prompt: as over a
+// pool of rows.  page_stream, in turns of 128 slots: the fullest compute unit has n workgroups, which take turns two at a time, and
+// 4/5 of a turn each where memory is what holds them up; four turns to start, and for a join two and three for every eight
+// slices.  (8 x 32 heads of 2048: 31 us with 1 slice, 35 with 2, 38 with 4; 32 of 777: 8.5 with 7, 10.3 with 1; 4 x 8 of 8192:
+// 18 with 8, 22 with 4; 16 x 8 ragged of 32768: 131 with 4, 159 with 3, 177 with 2.)
+// Never more than four rounds of workgroups, so that the states they leave are bounded (ig_page_reserve_bytes).
 constexpr long ROUNDS = 4;
 long workgroups_of(int rb) { return rb == 256 ? 256 : 512; }
 int slices_of(const ig_desc *d, const PagePlan &p) {
   const long groups = d->B * (long)d->H * p.nrb, turns = div_up(d->N, p.prompt ? 64 : 128), at_once = workgroups_of(p.rb);
   long best = 1, best_cost = -1;
   for (long s = 1; s <= MOST_SLICES && s <= turns && (s == 1 || groups * s <= ROUNDS * at_once); ++s) {
-    const long cost = div_up(groups * s, at_once) * (div_up(turns, s) + 2) + (s > 1 ? 3 * div_up(s, 8) : 0);
+    const long per = div_up(turns, s), join = s > 1 ? 3 * div_up(s, 8) : 0;
+    long cost = div_up(groups * s, at_once) * (per + 2) + join;
+    if (!p.prompt) {
+      const long n = div_up(groups * s, 256), two = 5 * div_up(n, 2) * per, bound = 4 * n * per;
+      cost = (two > bound ? two : bound) + 5 * (4 + join + (s > 1 ? 2 : 0));
+    }
     if (best_cost < 0 || cost < best_cost) best = s, best_cost = cost;
   }
   return (int)best;
