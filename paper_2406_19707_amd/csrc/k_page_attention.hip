@@ -33,6 +33,24 @@ __device__ __forceinline__ void transpose4(const unsigned (&r)[4], unsigned (&c)
   c[2] = __builtin_amdgcn_perm(y, x, 0x05040100u), c[3] = __builtin_amdgcn_perm(y, x, 0x07060302u);
 }
 
+// W words as load_words loads them, past the caches where they are read ONCE.  (V's: its loads are whole rows.  16 x 32 heads of 4096
+// 95 -> 86 us, 16 x 8 ragged of 32768 131 -> 121, float32 16 x 32 of 4096 99 -> 90, d = 256 100 -> 91, d = 64 as before.  K's too: 87
+// and 127, as a load is half of its rows' lines.)
+template <int W, bool ONCE> __device__ __forceinline__ void load_codes_of(const char *from, unsigned (&to)[W]) {
+  if constexpr (!ONCE) {
+    load_words<W>(from, to);
+  } else {
+    typedef unsigned vec __attribute__((ext_vector_type(W < 4 ? W : 4)));
+    constexpr int PER = W < 4 ? W : 4;
+#pragma unroll
+    for (int i = 0; i < W / PER; ++i) {
+      const vec x = __builtin_nontemporal_load(reinterpret_cast<const vec *>(from) + i);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) to[i * PER + e] = x[e];
+    }
+  }
+}
+
 // a float as two halves: x - hi - lo is at most 2^-22 |x|, or 2^-25
 struct Halves {
   half_t hi, lo;
@@ -53,7 +71,7 @@ __device__ __forceinline__ Halves split(float x) {
 // K's scale goes into the factor of the logits.  V's scale 2^ev goes into the exponent of the weights, which are
 // exp2(l + ev - ref) with ref the largest l + ev (or LIFT less): so no page's scale takes them out of half precision's range, and
 // sums take them times 2^-ev.  Float32 queries and weights are two halves each, and their products two.
-template <int D, int NT, bool E4M3, bool F32>
+template <int D, int NT, bool E4M3, bool F32, bool ONCE>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs a, PageRefs p) {
   typedef typename std::conditional<F32, float, half_t>::type T;
   constexpr int TT = 32, CJ = D / 16, RB = 16 * NT, KS = D / 32, PARTS = F32 ? 2 : 1;
@@ -106,7 +124,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
     for (int u = 0; u < 8; ++u) {
       const char *from = base + (min(tile * TT + 8 * g + u, last) & in_page) * D;
       if constexpr (VB == 2) v[u][0] = *reinterpret_cast<const unsigned short *>(from);
-      else load_words<VW>(from, v[u]);
+      else load_codes_of<VW, ONCE>(from, v[u]);
     }
     vs = p.V_scale[(unsigned long)page * p.H + h];
   };
@@ -675,9 +693,9 @@ int ig_launch_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *page
   a.by_units = ig_fast_div(units), a.by_pair = ig_fast_div(d->B * p.slices * units);
   a.total = (int)(BH * p.slices * units), a.per_xcd = div_up(a.total, 8);
   const dim3 grid(a.per_xcd * 8), block(256);
-#define STREAM(D, NT, E4M3, F32)                                                                     \
+#define STREAM(D, NT, E4M3, F32, ONCE)                                                               \
   {                                                                                                  \
-    auto k = page_stream<D, NT, E4M3, F32>;                                                          \
+    auto k = page_stream<D, NT, E4M3, F32, ONCE>;                                                         \
     IG_LAUNCH(ctx, IG_K_CACHE, k, grid, block, stream, a, refs);                                     \
   }
 #define PROMPT_WAVES(D, NW, E4M3)                                                                     \
@@ -695,9 +713,10 @@ int ig_launch_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *page
   }
 #define STREAM_ROWS(D, E4M3)                                                                         \
   {                                                                                                  \
-    if (d->dtype == IG_F32) STREAM(D, 1, E4M3, true)                                                 \
-    else if (p.rb == 16) STREAM(D, 1, E4M3, false)                                                   \
-    else if constexpr (D <= 128) STREAM(D, 2, E4M3, false)                                           \
+    if (d->dtype == IG_F32 && p.nrb == 1) STREAM(D, 1, E4M3, true, true)                             \
+    else if (d->dtype == IG_F32) STREAM(D, 1, E4M3, true, false)                                     \
+    else if (p.rb == 16) STREAM(D, 1, E4M3, false, true)                                             \
+    else if constexpr (D <= 128) STREAM(D, 2, E4M3, false, true)                                     \
   }
 #define BY_DIM(DO, E4M3)                                                                             \
   switch (d->d) {                                                                                    \
