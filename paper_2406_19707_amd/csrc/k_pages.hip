@@ -173,7 +173,9 @@ template <typename T, bool E4M3, int KIND> __global__ __launch_bounds__(1024) vo
 }
 
 // ---- rows read back ------------------------------------------------------------------------------------------------
-// A thread takes 16 channels of a listed row, of K and of V.
+// A thread takes the channels of one 16-byte store, of GATHER_ROWS listed rows of K and of V, all entries and then all codes
+// asked for together.  Stores are past the caches: whole lines of rows that somebody else reads.
+constexpr int GATHER_ROWS = 2;
 struct GatherArgs {
   PageRefs p;
   const int32_t *sel_idx, *sel_cnt;
@@ -182,29 +184,42 @@ struct GatherArgs {
   FastDiv by_chunks, by_H;
 };
 template <typename T, int D, bool E4M3> __global__ __launch_bounds__(256) void gather_pages(GatherArgs a) {
-  constexpr int UNITS = D / 16, ROWS = 256 / UNITS;
+  constexpr int CH = 16 / (int)sizeof(T), UNITS = D / CH, STEP = 256 / UNITS, U = GATHER_ROWS;
+  typedef unsigned codes_t __attribute__((ext_vector_type(CH / 4)));
+  typedef T vec __attribute__((ext_vector_type(CH)));
   const int bh = a.by_chunks.div(blockIdx.x), chunk = blockIdx.x - bh * (int)a.by_chunks.d, b = a.by_H.div(bh), h = bh - b * a.H;
-  const int j = chunk * ROWS + threadIdx.x / UNITS, s = threadIdx.x % UNITS;
-  if (j >= min(a.sel_cnt[bh], a.sel_stride)) return;
-  const int slot = min(max(a.sel_idx[(long)bh * a.sel_stride + j], 0), a.N_cap - 1);
-  const unsigned page = page_read(a.p, a.p.table[(long)b * a.p.stride + (slot >> a.p.shift)]);
-  const unsigned long from = (unsigned long)page * a.p.page_bytes + (((unsigned long)h << a.p.shift) + (slot & ((1 << a.p.shift) - 1))) * D + s * 16;
-  const uint4 codes[2] = {*reinterpret_cast<const uint4 *>(a.p.K + from), *reinterpret_cast<const uint4 *>(a.p.V + from)};
-  const float scales[2] = {a.p.K_scale[(long)page * a.H + h], a.p.V_scale[(long)page * a.H + h]};
+  const int n = min(a.sel_cnt[bh], a.sel_stride), j0 = chunk * STEP * U + threadIdx.x / UNITS, s = threadIdx.x % UNITS;
+  if (j0 >= n) return;
+  int slot[U];
+  unsigned page[U];
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    const float by = exp2_int(scale_exponent(scales[kv]));
-    const unsigned w[4] = {codes[kv].x, codes[kv].y, codes[kv].z, codes[kv].w};
-    float x[16];
+  for (int u = 0; u < U; ++u) slot[u] = min(max(a.sel_idx[(long)bh * a.sel_stride + min(j0 + u * STEP, n - 1)], 0), a.N_cap - 1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const floatx4 f = decode4<E4M3>(w[i]) * by;
+  for (int u = 0; u < U; ++u) page[u] = page_read(a.p, a.p.table[(long)b * a.p.stride + (slot[u] >> a.p.shift)]);
+  codes_t codes[U][2];
+  float scale[U][2];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * i + e] = f[e];
+  for (int u = 0; u < U; ++u) {
+    const unsigned long from = (unsigned long)page[u] * a.p.page_bytes + (((unsigned long)h << a.p.shift) + (slot[u] & ((1 << a.p.shift) - 1))) * D + s * CH;
+    codes[u][0] = *reinterpret_cast<const codes_t *>(a.p.K + from), codes[u][1] = *reinterpret_cast<const codes_t *>(a.p.V + from);
+    scale[u][0] = a.p.K_scale[(long)page[u] * a.H + h], scale[u][1] = a.p.V_scale[(long)page[u] * a.H + h];
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (j0 + u * STEP >= n) break;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const float by = exp2_int(scale_exponent(scale[u][kv]));
+      vec x;
+#pragma unroll
+      for (int i = 0; i < CH / 4; ++i) {
+        const floatx4 f = decode4<E4M3>(codes[u][kv][i]) * by;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * i + e] = (T)f[e];
+      }
+      T *to = static_cast<T *>(kv ? a.V_sel : a.K_sel) + ((long)bh * a.sel_stride + j0 + u * STEP) * D + s * CH;
+      __builtin_nontemporal_store(x, reinterpret_cast<vec *>(to));
     }
-    T *to = static_cast<T *>(kv ? a.V_sel : a.K_sel) + ((long)bh * a.sel_stride + j) * D + s * 16;
-    Run8<T>::store(to, x);
-    Run8<T>::store(to + 8, x + 8);
   }
 }
 
@@ -316,16 +331,17 @@ int ig_launch_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, con
   return IG_OK;
 }
 
-long ig_gather_pages_threads(const ig_desc *d, int sel_stride) {
-  return (long)d->B * d->H * div_up((long)sel_stride * (d->d / 16), 256) * 256;
+static int gather_chunks(const ig_desc *d, int sel_stride) {
+  return div_up((long)sel_stride * d->d * ig_elem_bytes(d->dtype), 256 * 16 * GATHER_ROWS);
 }
+long ig_gather_pages_threads(const ig_desc *d, int sel_stride) { return (long)d->B * d->H * gather_chunks(d, sel_stride) * 256; }
 
 int ig_launch_gather_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, const int32_t *sel_idx, int sel_stride, const int32_t *sel_cnt,
                            void *K_sel, void *V_sel, hipStream_t s) {
   GatherArgs a = {};
   a.p = ig_page_refs(d, p);
   a.sel_idx = sel_idx, a.sel_cnt = sel_cnt, a.K_sel = K_sel, a.V_sel = V_sel, a.H = d->H, a.N_cap = d->N_cap, a.sel_stride = sel_stride;
-  const int chunks = div_up((long)sel_stride * (d->d / 16), 256);
+  const int chunks = gather_chunks(d, sel_stride);
   a.by_chunks = ig_fast_div(chunks), a.by_H = ig_fast_div(d->H);
   const dim3 grid((unsigned)((long)d->B * d->H * chunks)), block(256);
 #define GATHER(T, D, E4M3)                                                                           \
