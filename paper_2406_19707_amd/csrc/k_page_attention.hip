@@ -341,8 +341,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
 constexpr float RISE = 6.f, PROMPT_LIFT = 9.f;
 constexpr int PROMPT_KEYS = 64;
 
-template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 128 ? 2 : 1) void page_prompt(StreamArgs a, PageRefs p) {
-  constexpr int KS = D / 16, OB = D / 32, TK = PROMPT_KEYS, ROWS = NW * 32;
+template <int D, int NW, int RB, bool E4M3> __global__ __launch_bounds__(NW * 64, D * RB <= 128 ? 2 : 1) void page_prompt(StreamArgs a, PageRefs p) {
+  constexpr int KS = D / 16, OB = D / 32, TK = PROMPT_KEYS, ROWS = RB * NW * 32;
   constexpr int LB = TK * D / (NW * 64) < 16 ? 8 : 16;            // bytes of a lane's load
   constexpr int PIECES = D / LB, LR = 64 / PIECES, LOADS = TK / (LR * NW);      // loads of a row; rows of a wave's load; loads of a wave
   static_assert(LOADS >= 1 && LR <= 16, "a wave's load stays in a page");
@@ -373,23 +373,27 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
       if (2 * unit >= a.nrb - 1) break;
       __syncthreads();                                    // the other waves are done with the tiles
     }
-    const int row = rb * ROWS + w * 32 + i, iq = a.by_group.div(row), gq = row - iq * G;
-    const bool live = row < a.R && iq < nq;
-    const int lim = live ? row_limit<false>(a, row, kv, nq) : 0x7fffffff;
-    const long row_at = (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * G + gq) * D;
-    const int first_row = rb * ROWS + w * 32, lim_min = row_limit<false>(a, first_row, kv, nq);
+    int lim[RB], lim_min[RB];
+    long row_at[RB];
+    bool live[RB];
+    half8 qf[RB][KS];
+#pragma unroll
+    for (int c = 0; c < RB; ++c) {
+      const int first_row = rb * ROWS + (c * NW + w) * 32, row = first_row + i, iq = a.by_group.div(row), gq = row - iq * G;
+      live[c] = row < a.R && iq < nq;
+      lim[c] = live[c] ? row_limit<false>(a, row, kv, nq) : 0x7fffffff;
+      lim_min[c] = row_limit<false>(a, first_row, kv, nq);
+      row_at[c] = (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * G + gq) * D;
+      const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const half_t *>(a.q) + row_at[c]);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) qf[c][s] = __builtin_bit_cast(half8, flip_sign<half_t>(src[2 * s + hb], a.flip));
+    }
     const int last_row = min(min(a.R, nq * G), (rb + 1) * ROWS) - 1;
     const int most = last_row < rb * ROWS ? 0 : row_limit<false>(a, last_row, kv, nq);
     const int tiles_all = (most + TK - 1) / TK;
     const int per = (tiles_all + span.slices - 1) / span.slices;
     const int t_begin = min(tiles_all, slice * per), t_end = min(tiles_all, t_begin + per);
 
-    half8 qf[KS];
-    {
-      const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const half_t *>(a.q) + row_at);
-#pragma unroll
-      for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(half8, flip_sign<half_t>(src[2 * s + hb], a.flip));
-    }
     // (slots past the last one that a row sees are read from that one; tiles past the last: the last)
     const int last = most - 1;
     auto entry_of = [&](int tile) __attribute__((always_inline)) {
@@ -416,14 +420,15 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
       }
     };
 
-    floatx16 acc[OB];
+    floatx16 acc[RB][OB], sA[RB], sB[RB];
+    float ref[RB], sum_all[RB];
+    half8 pA[RB][2], pB[RB][2];
 #pragma unroll
-    for (int o = 0; o < OB; ++o)
+    for (int c = 0; c < RB; ++c) {
+      ref[c] = NOTHING_SEEN, sum_all[c] = 0.f, sA[c] = floatx16{}, sB[c] = floatx16{};
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[o][e] = 0.f;
-    float ref = NOTHING_SEEN, sum_all = 0.f;
-    floatx16 sA = {}, sB = {};
-    half8 pA[2], pB[2];
+      for (int o = 0; o < OB; ++o) acc[c][o] = floatx16{};
+    }
     // of the lane's 16 slots of a tile: the factor of logits, the exponent of V's scale and 1 / that scale
     struct Scales {
       float k, v, back;
@@ -431,8 +436,8 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
 
     // now: logits in, weights out (half `now_half` of tile `now_tile`); next: the logits of rows `next_row` .. of tile K; out: acc +=
     // the weights `old` times rows `old_row` .. of tile V
-    auto half_step = [&](auto has_now, auto has_next, auto has_old, const floatx16 &now, int now_tile, auto now_half, const Scales &scales,
-                         half8 (&weights)[2], floatx16 &next, const half_t *K, int next_row, const half8 (&old)[2],
+    auto half_step = [&](auto has_now, auto has_next, auto has_old, const floatx16 (&now)[RB], int now_tile, auto now_half, const Scales &scales,
+                         half8 (&weights)[RB][2], floatx16 (&next)[RB], const half_t *K, int next_row, const half8 (&old)[RB][2],
                          const half_t *V, int old_row, auto store) __attribute__((always_inline)) {
       constexpr bool NOW = decltype(has_now)::value, NEXT = decltype(has_next)::value, OLD = decltype(has_old)::value;
       constexpr int HALF = decltype(now_half)::value;
@@ -457,40 +462,50 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
       };
 #pragma unroll
       for (int x = 0; x < LEAD; ++x) read(x);
-      floatx16 s;
-      float shrink = 1.f, by[2], off[2], back[2], sums[4] = {0.f, 0.f, 0.f, 0.f};
-      bool rises = false;
+      floatx16 s[RB];
+      float shrink[RB], by[2], off[RB][2], back[2], sums[RB][4] = {};
+      bool rises[RB];
       if constexpr (NOW) {
-        s = now;
-        const int t0 = now_tile * TK + HALF * 32;
-        if (t0 + 32 > lim_min) {
-          const int mine = t0 + (int)opaque(hb * 4);
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (mine + ((e / 4) * 8 + e % 4) >= lim) s[e] = -INFINITY;
-        }
-        float top = -INFINITY;
+        float exponent[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           auto of = [&](float y) __attribute__((always_inline)) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y), HALF * 2 + x)); };
-          by[x] = of(scales.k), off[x] = of(scales.v), back[x] = of(scales.back);
-          float m = s[8 * x];
-#pragma unroll
-          for (int e = 8 * x + 1; e < 8 * x + 8; ++e) m = __builtin_elementwise_maximum(m, s[e]);
-          top = fmaxf(top, fmaf(m, by[x], off[x]));
+          by[x] = of(scales.k), exponent[x] = of(scales.v), back[x] = of(scales.back);
         }
-        top = lifted(both_max(top), PROMPT_LIFT);
-        const float to = top > ref + RISE ? top : ref;
-        rises = __any(to != ref);
-        shrink = exp2_fast(ref - to);
-        ref = to;
-        sum_all *= shrink;
 #pragma unroll
-        for (int x = 0; x < 2; ++x) off[x] -= ref;
+        for (int c = 0; c < RB; ++c) {
+          s[c] = now[c];
+          const int t0 = now_tile * TK + HALF * 32;
+          if (t0 + 32 > lim_min[c]) {
+            const int mine = t0 + (int)opaque(hb * 4);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (mine + ((e / 4) * 8 + e % 4) >= lim[c]) s[c][e] = -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < RB; ++c) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float m = s[c][8 * x];
+#pragma unroll
+            for (int e = 8 * x + 1; e < 8 * x + 8; ++e) m = __builtin_elementwise_maximum(m, s[c][e]);
+            top = fmaxf(top, fmaf(m, by[x], exponent[x]));
+          }
+          top = lifted(both_max(top), PROMPT_LIFT);
+          const float to = top > ref[c] + RISE ? top : ref[c];
+          rises[c] = __any(to != ref[c]);
+          shrink[c] = exp2_fast(ref[c] - to);
+          ref[c] = to;
+          sum_all[c] *= shrink[c];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) off[c][x] = exponent[x] - to;
+        }
       }
       if constexpr (NEXT) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) next[e] = 0.f;
+        for (int c = 0; c < RB; ++c) next[c] = floatx16{};
       }
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
@@ -499,32 +514,41 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
         if constexpr (NEXT) {
 #pragma unroll
           for (int k = x * KS / 8; k < (x + 1) * KS / 8; ++k)
-            next = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[k], qf[k], next, 0, 0, 0);
+#pragma unroll
+            for (int c = 0; c < RB; ++c) next[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf[k], qf[c][k], next[c], 0, 0, 0);
         }
         if constexpr (OLD) {
 #pragma unroll
-          for (int y = x * 2 * OB / 8; y < (x + 1) * 2 * OB / 8; ++y) {
-            acc[y % OB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vt[y]), old[y / OB], acc[y % OB], 0, 0, 0);
-          }
+          for (int y = x * 2 * OB / 8; y < (x + 1) * 2 * OB / 8; ++y)
+#pragma unroll
+            for (int c = 0; c < RB; ++c)
+              acc[c][y % OB] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, vt[y]), old[c][y / OB], acc[c][y % OB], 0, 0, 0);
         }
         if constexpr (NOW) {
 #pragma unroll
-          for (int e = 2 * x; e < 2 * x + 2; ++e) {
-            const float y = exp2_fast(fmaf(s[e], by[e / 8], off[e / 8]));
-            sums[e / 8 * 2 + e % 2] += y;
-            weights[e / 8][e % 8] = (half_t)y;
-          }
+          for (int c = 0; c < RB; ++c)
+#pragma unroll
+            for (int e = 2 * x; e < 2 * x + 2; ++e) {
+              const float y = exp2_fast(fmaf(s[c][e], by[e / 8], off[c][e / 8]));
+              sums[c][e / 8 * 2 + e % 2] += y;
+              weights[c][e / 8][e % 8] = (half_t)y;
+            }
         }
       }
       if constexpr (NOW) {
-        sum_all = fmaf(sums[0] + sums[1], back[0], fmaf(sums[2] + sums[3], back[1], sum_all));
-        keep_here(weights[0]);
-        keep_here(weights[1]);
-        keep_here(sum_all);                               // (not put off: the weights' registers are needed)
-      }
-      if (NOW && rises) {
 #pragma unroll
-        for (int o = 0; o < OB; ++o) acc[o] *= shrink;
+        for (int c = 0; c < RB; ++c) {
+          sum_all[c] = fmaf(sums[c][0] + sums[c][1], back[0], fmaf(sums[c][2] + sums[c][3], back[1], sum_all[c]));
+          keep_here(weights[c][0]);
+          keep_here(weights[c][1]);
+          keep_here(sum_all[c]);                          // (not put off: the weights' registers are needed)
+        }
+#pragma unroll
+        for (int c = 0; c < RB; ++c)
+          if (rises[c]) {
+#pragma unroll
+            for (int o = 0; o < OB; ++o) acc[c][o] *= shrink[c];
+          }
       }
     };
     typedef std::true_type Y;
@@ -593,29 +617,32 @@ template <int D, int NW, bool E4M3> __global__ __launch_bounds__(NW * 64, D <= 1
       half_step(N(), N(), Y(), sA, 0, H0(), now, pA, sB, V, 0, pB, V, 32, nothing);
     }
 
-    if (!live) continue;
-    const float sum = both_sum(sum_all);
-    const float inv = inverse_of(sum);
-    if (a.slices == 1) {
-      half_t *to = static_cast<half_t *>(a.out) + row_at;
 #pragma unroll
-      for (int o = 0; o < OB; ++o)
+    for (int c = 0; c < RB; ++c) {
+      const float sum = both_sum(sum_all[c]);
+      if (!live[c]) continue;
+      const float inv = inverse_of(sum);
+      if (a.slices == 1) {
+        half_t *to = static_cast<half_t *>(a.out) + row_at[c];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          half_t v[4];
+        for (int o = 0; o < OB; ++o)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = (half_t)(acc[o][x * 4 + e] * inv);
-          store_words<2>(to + o * 32 + x * 8 + hb * 4, v);
-        }
-    } else {
-      const long at = ((long)h * a.B * a.slices + number) * a.R + row;
+          for (int x = 0; x < 4; ++x) {
+            half_t v[4];
 #pragma unroll
-      for (int o = 0; o < OB; ++o)
+            for (int e = 0; e < 4; ++e) v[e] = (half_t)(acc[c][o][x * 4 + e] * inv);
+            store_words<2>(to + o * 32 + x * 8 + hb * 4, v);
+          }
+      } else {
+        const long at = ((long)h * a.B * a.slices + number) * a.R + rb * ROWS + (c * NW + w) * 32 + i;
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          *reinterpret_cast<floatx4 *>(a.part + at * D + o * 32 + x * 8 + hb * 4) =
-              floatx4{acc[o][x * 4], acc[o][x * 4 + 1], acc[o][x * 4 + 2], acc[o][x * 4 + 3]};
-      if (hb == 0) a.part_ml[at] = make_float2(ref, sum);
+        for (int o = 0; o < OB; ++o)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            *reinterpret_cast<floatx4 *>(a.part + at * D + o * 32 + x * 8 + hb * 4) =
+                floatx4{acc[c][o][x * 4], acc[c][o][x * 4 + 1], acc[c][o][x * 4 + 2], acc[c][o][x * 4 + 3]};
+        if (hb == 0) a.part_ml[at] = make_float2(ref[c], sum);
+      }
     }
   }
 }
@@ -626,8 +653,11 @@ int div_up(long n, long d) { return (int)((n + d - 1) / d); }
 int row_block(const ig_desc *d, long R) { return R <= 16 || d->d > 128 || d->dtype == IG_F32 ? 16 : 32; }
 bool many_rows(const ig_desc *d, long R) { return d->dtype == IG_F16 && R > (d->d > 128 ? 16 : 32); }
 int prompt_rows(const ig_desc *d, const PageCall &c) {
-  return d->d >= 64 && d->d <= 128 && (long)c.n_q * c.group > 128 && 2 * (long)c.n_q <= d->N ? 256 : 128;
+  const long R = (long)c.n_q * c.group;
+  if (d->d == 128) return R > 128 && 2 * (long)c.n_q <= d->N ? 256 : 128;
+  return d->d == 64 && d->B * (long)d->H * div_up(R, 256) >= 512 ? 256 : 128;
 }
+int page_waves(const ig_desc *d, int rb) { return rb == 256 && d->d == 128 ? 8 : 4; }
 
 // Slices that the slots of a pool head are cut into: the number for which the last workgroups end first.  page_prompt: as over a
 // pool of rows.  page_stream, in turns of 128 slots: the fullest compute unit has n workgroups, which take turns two at a time, and
@@ -661,7 +691,7 @@ PagePlan ig_page_plan(const ig_desc *d, const PageCall &c) {
   p.rb = p.prompt ? prompt_rows(d, c) : row_block(d, R);
   p.nrb = div_up(R, p.rb);
   p.slices = slices_of(d, p);
-  p.threads = (BH * p.slices * p.nrb + 8) * (p.rb == 256 ? 512 : 256);
+  p.threads = (BH * p.slices * p.nrb + 8) * 64 * page_waves(d, p.rb);
   const size_t ml = p.slices > 1 ? BH * p.slices * R * sizeof(float2) : 0;
   p.part_at = (ml + 255) / 256 * 256;
   p.bytes = p.part_at + (p.slices > 1 ? BH * p.slices * R * d->d * sizeof(float) : 0);
@@ -698,18 +728,16 @@ int ig_launch_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *page
     auto k = page_stream<D, NT, E4M3, F32, ONCE>;                                                         \
     IG_LAUNCH(ctx, IG_K_CACHE, k, grid, block, stream, a, refs);                                     \
   }
-#define PROMPT_WAVES(D, NW, E4M3)                                                                     \
+#define PROMPT_WAVES(D, NW, RB, E4M3)                                                                 \
   {                                                                                                  \
-    auto k = page_prompt<D, NW, E4M3>;                                                               \
+    auto k = page_prompt<D, NW, RB, E4M3>;                                                           \
     IG_LAUNCH(ctx, IG_K_CACHE, k, grid, dim3(NW * 64), stream, a, refs);                             \
   }
 #define PROMPT(D, E4M3)                                                                              \
   {                                                                                                  \
-    if constexpr (D == 64 || D == 128) {                                                             \
-      if (p.rb == 256) PROMPT_WAVES(D, 8, E4M3)                                                      \
-      else PROMPT_WAVES(D, 4, E4M3)                                                                  \
-    } else                                                                                           \
-      PROMPT_WAVES(D, 4, E4M3)                                                                       \
+    if (p.rb == 128) PROMPT_WAVES(D, 4, 1, E4M3)                                                     \
+    else if constexpr (D == 64) PROMPT_WAVES(D, 4, 2, E4M3)                                          \
+    else if constexpr (D == 128) PROMPT_WAVES(D, 8, 1, E4M3)                                         \
   }
 #define STREAM_ROWS(D, E4M3)                                                                         \
   {                                                                                                  \
