@@ -1141,11 +1141,11 @@ int ig_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *pages, const 
                     const void *k_rows, const void *v_rows, int64_t row_stride, const int32_t *n_append, const int32_t *kv_len,
                     const int32_t *pos, void *q_out, void *stream) {
   const char *what = "ig_append_pages";
-  if (!q) group = 1;
+  if (!q) group = 1, q_out = nullptr;
   int rc = check_pages(ctx, d, pages, what, group, n_rows, stream);
   if (rc) return rc;
   const int Hq = q ? d->H * group : 0, size = ig_elem_bytes(d->dtype);
-  if (ig_append_pages_threads(d, pages, Hq, n_rows) > 2147483647l) return ig_fail(ctx, IG_ESHAPE, "%s: too many rows for a launch", what);
+  // (2^26 rows, of queries too, are a launch of at most 2^29 threads)
   if (!k_rows || !v_rows || (q && !q_out)) return ig_fail(ctx, IG_EINVAL, "%s: NULL argument", what);
   if (rotary && (rc = check_rotary(ctx, what, rotary, d->d))) return rc;
   if ((rc = check_aligned(ctx, what, {q, k_rows, v_rows, q_out}))) return rc;

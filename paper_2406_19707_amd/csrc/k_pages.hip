@@ -288,12 +288,6 @@ int ig_launch_rotate(ig_ctx *ctx, int dtype, int n, int heads, int d, const ig_r
     else BY_DIM(float, true, DO)                                                                     \
   }
 
-long ig_append_pages_threads(const ig_desc *d, const ig_pages *p, int Hq, int n_rows) {
-  const int team = append_team(d, p, n_rows);
-  const long kv = 2l * d->B * append_page_count(p, n_rows) * div_up(d->H, append_each(d, p, n_rows)) * team, n = (long)d->B * n_rows;
-  return kv + (Hq ? n * div_up(Hq, rotate_each(n, Hq, d->d)) * (d->d / 16) + team : 0);
-}
-
 int ig_launch_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, const ig_rotary *rotary, int Hq, int n_rows, const void *q,
                            const void *k, const void *v, long row_stride, const int32_t *n_append, const int32_t *kv_len, const int32_t *pos,
                            void *q_out, hipStream_t s) {

@@ -143,3 +143,93 @@ def test_no_slots(ctx):
         ctx.ig_page_attention(desc(2, 2, 64, 0, 16, "f16"), pages.struct(), 1, n_q, q, i32([n_q, 0]), None, out)
         torch.cuda.synchronize()
         assert (out[0] == 0).all() and (out[1] == SENTINEL).all()
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+@pytest.mark.parametrize("d,n_q,N", [(32, 150, 160), (64, 290, 300), (64, 300, 400), (128, 150, 160)])
+def test_many_workgroups(ctx, code, d, n_q, N):
+    """Prompts of many heads: row blocks in pairs, two row blocks a wave; the last rows see all, the first none or few."""
+    kv = [N, N, 1, N - 70, n_q - 9, N, 64, N]
+    run_attention(ctx, "f16", code, d, B=8, H=64, group=1, n_q=n_q, N=N, N_cap=N, page=16, kv=kv, seed=d)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_long_rows(ctx, d):
+    """A chunk over many tiles: references that rise again and again, rows with one large logit."""
+    B, H, n_q, N = 1, 2, 200, 5000
+    pages = Pages(B, H, d, N, 64, "i8", 1).fill([N], 2, spread=1)
+    # keys grow along the sequence, so that every tile raises the largest logit
+    for c in range(-(-N // 64)):
+        pages.K_scale[int(pages.table[0, c])] = 2.0 ** (-9 + c // 16)
+    q = rows((B, n_q, H, d), "f16", 3)
+    out = torch.full_like(q, SENTINEL)
+    ctx.ig_page_attention(desc(B, H, d, N, N, "f16", 0.5), pages.struct(), 1, n_q, q, None, None, out)
+    torch.cuda.synchronize()
+    check_attention(pages, q, [N], [n_q], 1, 0.5, "f16", out, out)
+
+
+@pytest.mark.parametrize("n_q", [1, 40])
+def test_what_lies_behind_the_last_slot(ctx, n_q):
+    """Junk codes (e4m3: NaN) and scales behind a sequence's slots, in its last page and in entries past it, do not count."""
+    B, H, d, N, page = 2, 2, 64, 70, 32
+    for dtype in ("f16", "f32"):
+        pages = Pages(B, H, d, 128, page, "e4m3", 1).fill([N, 33], 2)
+        q = rows((B, n_q, H, d), dtype, 3)
+        out, other = torch.full_like(q, SENTINEL), torch.full_like(q, SENTINEL)
+        ds = desc(B, H, d, N, 128, dtype, 0.125)
+        ctx.ig_page_attention(ds, pages.struct(), 1, n_q, q, None, i32([N, 33]), out)
+        for b, n in enumerate((N, 33)):
+            at = int(pages.table[b, n // page])
+            pages.K[at, :, n % page:], pages.V[at, :, n % page:] = 0x11, 0x22
+            rest = pages.table[b, n // page + 1:].long()
+            pages.K[rest], pages.V[rest], pages.K_scale[rest], pages.V_scale[rest] = 0x33, 0x44, 1.0, 1.0
+        ctx.ig_page_attention(ds, pages.struct(), 1, n_q, q, None, i32([N, 33]), other)
+        torch.cuda.synchronize()
+        assert torch.isfinite(out).all() and torch.equal(out, other)
+
+
+def test_shared_pages(ctx):
+    """Two sequences with the same first pages, and the same page twice in one."""
+    B, H, d, page, N = 2, 2, 128, 16, 64
+    pages = Pages(B, H, d, N, page, "i8", 1).fill([N, N], 2)
+    pages.table[1, :2] = pages.table[0, :2]
+    pages.table[0, 3] = pages.table[0, 2]
+    for n_q in (1, 50):
+        q = rows((B, n_q, H, d), "f16", 3)
+        out = torch.full_like(q, SENTINEL)
+        ctx.ig_page_attention(desc(B, H, d, N, N, "f16", 0.1), pages.struct(), 1, n_q, q, None, None, out)
+        torch.cuda.synchronize()
+        check_attention(pages, q, [N, N], [n_q, n_q], 1, float(torch.tensor(0.1)), "f16", out, out)
+
+
+def test_pages_far_into_the_pool(ctx):
+    """Codes past 2^32 bytes, and scales past 2^16 pages."""
+    H, d, page, n = 8, 128, 128, 40000                         # 5.2 GB of K
+    K = torch.zeros((n, H, page, d), dtype=torch.uint8, device="cuda")
+    V = torch.zeros_like(K)
+    scales = [torch.ones((n, H), device="cuda") for _ in "KV"]
+    small = Pages(1, H, d, 256, page, "i8", 1).fill([256], 2)
+    far = [n - 1, 33333]
+    for x, y, s, t in ((K, small.K, scales[0], small.K_scale), (V, small.V, scales[1], small.V_scale)):
+        for c, at in enumerate(far):
+            x[at], s[at] = y[int(small.table[0, c])], t[int(small.table[0, c])]
+    table = i32([far])
+    for n_q in (1, 40):
+        q = rows((1, n_q, H, d), "f16", 3)
+        out, other = torch.zeros_like(q), torch.zeros_like(q)
+        ds = desc(1, H, d, 256, 256, "f16", 0.1)
+        ctx.ig_page_attention(ds, small.struct(), 1, n_q, q, None, None, out)
+        ctx.ig_page_attention(ds, ig.IgPages(table, K, V, *scales, ig.IG_CODE_I8), 1, n_q, q, None, None, other)
+        torch.cuda.synchronize()
+        assert torch.equal(out, other)
+    # appended to and read back there
+    k = rows((1, 3, H, d), "f16", 5)
+    idx, cnt = i32([[200, 201, 202]] * H), i32([3] * H)
+    got = []
+    for p in (small.struct(), ig.IgPages(table, K, V, *scales, ig.IG_CODE_I8)):
+        to = [torch.zeros((H, 3, d), dtype=torch.float16, device="cuda") for _ in "KV"]
+        ctx.ig_append_pages(desc(1, H, d, 200, 256, "f16"), p, None, 1, 3, None, k, k, 0, None, None, None, None)
+        ctx.ig_gather_pages(desc(1, H, d, 256, 256, "f16"), p, idx, 3, cnt, *to)
+        torch.cuda.synchronize()
+        got.append(to)
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and got[0][0].any()

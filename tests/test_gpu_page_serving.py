@@ -1,0 +1,332 @@
+"""The calls over pages together, as a decoding program makes them: prompts in chunks, steps, rows read back for the dense calls, in
+one graph; and what they refuse."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paper_2406_19707_amd as ig
+from ig_cache import check_attention as check_dense
+from ig_pages import DT, SENTINEL, Pages, check_attention, desc, i32, rotary, rows, turned
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = ig.Context(0)
+    yield c
+    c.close()
+
+
+class Decoder:
+    """Sequences in pages: every step appends rows of one projection's output, rotated, and attends them."""
+
+    def __init__(self, dtype, code, B, H, G, d, N_cap, page, T, own_context=False, seed=1):
+        self.ctx = ig.Context(0) if own_context else None
+        self.shape = (B, H, G, d, N_cap)
+        self.dtype, self.T = dtype, T
+        self.pages = Pages(B, H, d, N_cap, page, code, seed)
+        self.struct = self.pages.struct()
+        self.rotary, self.freq, self.magnitude = rotary(d // 2, kind=ig.IG_ROPE_WAVELENGTH, factor=4.0, low=1.0, high=4.0, original=64)
+        self.qkv = torch.zeros((B, T, (G + 2) * H, d), dtype=DT[dtype], device="cuda")
+        self.q_out, self.out = (torch.full((B, T, G * H, d), SENTINEL, dtype=DT[dtype], device="cuda") for _ in range(2))
+        self.kv_len, self.after, self.n = (torch.zeros(B, dtype=torch.int32, device="cuda") for _ in range(3))
+        self.desc = desc(B, H, d, N_cap, N_cap, dtype, 1 / math.sqrt(d))
+
+    def step(self, ctx=None):
+        ctx = ctx or self.ctx
+        B, H, G, d, _ = self.shape
+        size = self.qkv.element_size() * d
+        q = self.qkv.data_ptr()
+        ctx.ig_append_pages(self.desc, self.struct, self.rotary, G, self.T, q, q + G * H * size, q + (G + 1) * H * size, (G + 2) * H * d, self.n,
+                            self.kv_len, None, self.q_out)
+        torch.add(self.kv_len, self.n, out=self.after)
+        ctx.ig_page_attention(self.desc, self.struct, G, self.T, self.q_out, self.n, self.after, self.out)
+        self.kv_len.copy_(self.after)
+
+    def state(self):
+        p = self.pages
+        return dict(K=p.K, V=p.V, K_scale=p.K_scale.view(torch.int32), V_scale=p.V_scale.view(torch.int32), q=self.q_out, out=self.out, kv_len=self.kv_len)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+def test_a_prompt_in_chunks_and_steps(ctx, dtype, code):
+    B, H, G, d, N_cap, page = 3, 2, 3, 64, 160, 16
+    plan = [[40, 40, 40], [40, 7, 23], [1, 1, 1], [1, 0, 1], [2, 1, 3], [0, 33, 1]]
+    dec = Decoder(dtype, code, B, H, G, d, N_cap, page, 40)
+    kept = [[[], []] for _ in range(B)]                                   # rotated keys and values as they came
+    lens = [0] * B
+    for i, n in enumerate(plan):
+        dec.qkv.copy_(rows(tuple(dec.qkv.shape), dtype, 10 + i))
+        dec.n.copy_(i32(n))
+        before = dec.out.clone()
+        dec.step(ctx)
+        torch.cuda.synchronize()
+        for b in range(B):
+            x = dec.qkv[b, :n[b]]
+            pos = lens[b] + torch.arange(n[b], device="cuda")
+            for w, y in ((0, turned(x[:, G * H:(G + 1) * H], pos, d // 2, False, dec.freq, 1.0)[0]), (1, x[:, (G + 1) * H:].double())):
+                kept[b][w].append(y)
+        lens = [a + b for a, b in zip(lens, n)]
+        assert dec.kv_len.tolist() == lens
+        check_attention(dec.pages, dec.q_out, lens, n, G, 1 / math.sqrt(d), dtype, dec.out, before)
+    # Against the rows as they came: a code is off by less than a scale (e4m3: 2^-4 of itself and 2^-9 of a scale), so a logit by at most
+    # D = |q|_1 times that times the logits' scale, a weight by a factor of exp(2 D), an output by (exp(2 D) - 1) sum of p |v| and a
+    # value's error.  (And what rounding an output costs, far below that.)
+    for b in range(B):
+        K, V = (torch.cat(kept[b][w]).transpose(0, 1) for w in (0, 1))
+        for x, ref in (("K", K), ("V", V)):
+            at = dec.pages.table[b, torch.arange(lens[b], device="cuda") // page].long()
+            s = getattr(dec.pages, x + "_scale")[at].double().T[:, :, None]
+            err = (dec.pages.values(x, b, lens[b]) - ref).abs()
+            assert (err <= (s if code == "i8" else 2.0 ** -4 * ref.abs() + 2.0 ** -9 * s) + 2.0 ** -10 * ref.abs()).all()
+    # the rows read back, in the dense calls: a pool, and its attention of the last rows
+    stride = N_cap
+    idx = torch.arange(stride, device="cuda", dtype=torch.int32).repeat(B * H, 1)
+    cnt = torch.tensor([n for n in lens for _ in range(H)], dtype=torch.int32, device="cuda")
+    pools = [torch.zeros((B, H, stride, d), dtype=DT[dtype], device="cuda") for _ in "KV"]
+    ctx.ig_gather_pages(dec.desc, dec.struct, idx, stride, cnt, *pools)
+    dense = torch.full_like(dec.out, SENTINEL)
+    before = dense.clone()
+    ctx.ig_cache_attention(dec.desc, G, 40, dec.q_out, dec.n, *pools, dec.kv_len, None, dense)
+    torch.cuda.synchronize()
+    check_dense(dec.q_out, *pools, lens, plan[-1], G, 1 / math.sqrt(d), dtype, dense, before)
+
+
+@pytest.mark.parametrize("dtype,code,T", [("f16", "i8", 1), ("f16", "e4m3", 40), ("f32", "i8", 3), ("f32", "e4m3", 20)])
+def test_steps_in_a_graph(dtype, code, T):
+    """One step captured and replayed, with eager work between the replays, against eager steps."""
+    shape = (dtype, code, 3, 4, 2, 64, 700, 32, T)
+    captured, eager = Decoder(*shape, own_context=True), Decoder(*shape, own_context=True)
+    B, H, G, d, N_cap = captured.shape
+    for dec in (captured, eager):
+        dec.ctx.ig_reserve_pages(dec.desc, G, T)
+        dec.pages.fill([300, 17, 0], 5)
+        dec.kv_len.copy_(i32([300, 17, 0]))
+    held = captured.ctx.ig_workspace_bytes()
+    assert held > 0
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            captured.step()
+    for seed in range(1, 6):
+        n = i32([T, max(0, T - seed), seed % (T + 1)])
+        for dec in (captured, eager):
+            dec.qkv.copy_(rows(tuple(dec.qkv.shape), dtype, seed))
+            dec.n.copy_(n)
+        graph.replay()
+        eager.step()
+        torch.cuda.synchronize()
+        for (name, a), b in zip(captured.state().items(), eager.state().values()):
+            assert torch.equal(a, b), f"{name} after replay {seed}"
+    assert captured.ctx.ig_workspace_bytes() == held
+    captured.ctx.close()
+    eager.ctx.close()
+
+
+def test_without_a_workspace_under_capture():
+    """A call in slices that lacks its workspace is refused while its stream is captured, and says what to call."""
+    c = ig.Context(0)
+    dec = Decoder("f16", "i8", 1, 2, 1, 64, 4096, 64, 1)
+    dec.pages.fill([4096], 1)
+    dec.after.fill_(4096)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            dec.out.zero_()
+            with pytest.raises(ig.IgError) as e:
+                c.ig_page_attention(dec.desc, dec.struct, 1, 1, dec.q_out, None, dec.after, dec.out)
+    assert e.value.code == ig.IG_EINVAL and "reserve" in str(e.value)
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_reserved_for_smaller_calls_too(dtype):
+    """ig_reserve_pages bounds every call of fewer rows and slots."""
+    for B, H, group, n_q, d, N_cap in ((1, 1, 1, 1, 32, 40000), (4, 2, 4, 70, 64, 9000), (16, 8, 1, 40, 128, 2000), (2, 1, 8, 300, 256, 5000)):
+        c = ig.Context(0)
+        c.ig_reserve_pages(desc(B, H, d, 1, N_cap, dtype), group, n_q)
+        held = c.ig_workspace_bytes()
+        pages = Pages(B, H, d, N_cap, 128, "i8", 1)
+        pages.K.zero_(), pages.V.zero_(), pages.K_scale.fill_(1.0), pages.V_scale.fill_(1.0)
+        for b, g, m, n in ((B, group, n_q, N_cap), (1, 1, 1, N_cap), (1, group, 1, N_cap // 3 + 1), (B, 1, n_q, N_cap // 2), (1, group, n_q, N_cap),
+                           (B, group, max(1, n_q // 3), 100)):
+            q = torch.zeros((b, m, H * g, d), dtype=DT[dtype], device="cuda")
+            c.ig_page_attention(desc(b, H, d, n, N_cap, dtype), pages.struct(), g, m, q, None, None, torch.empty_like(q))
+            torch.cuda.synchronize()
+            assert c.ig_workspace_bytes() == held
+        c.close()
+
+
+def test_two_contexts_on_two_streams(ctx):
+    """Calls of two contexts at once, on pages that both read."""
+    B, H, G, d, N = 2, 4, 4, 128, 3000
+    pages = Pages(B, H, d, N, 32, "i8", 1).fill([N, N], 2)
+    other = ig.Context(0)
+    s = [torch.cuda.Stream(), torch.cuda.Stream()]
+    q = [rows((B, 1, H * G, d), "f16", 3), rows((B, 50, H * G, d), "f16", 4)]
+    want = []
+    for x in q:
+        out = torch.zeros_like(x)
+        ctx.ig_page_attention(desc(B, H, d, N, N, "f16", 0.1), pages.struct(), G, x.shape[1], x, None, None, out)
+        torch.cuda.synchronize()
+        want.append(out)
+    got = [torch.zeros_like(x) for x in q]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, st, x, out in zip((ctx, other), s, q, got):
+            c.ig_page_attention(desc(B, H, d, N, N, "f16", 0.1), pages.struct(), G, x.shape[1], x, None, None, out, st)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    other.close()
+
+
+# ---- what is refused -----------------------------------------------------------------------------------------------------
+
+def refused(code, f, *args):
+    with pytest.raises(ig.IgError) as e:
+        f(*args)
+    assert e.value.code == code, e.value
+
+
+def test_pages_that_are_refused(ctx):
+    B, H, d, N = 2, 2, 64, 32
+    p = Pages(B, H, d, N, 16, "i8", 1)
+    q, k = rows((B, 1, H, d), "f16", 1), rows((B, 1, H, d), "f16", 2)
+    out, idx, cnt = torch.full_like(q, SENTINEL), torch.zeros((B * H, 4), dtype=torch.int32, device="cuda"), i32([1] * (B * H))
+    sel = [torch.zeros((B * H, 4, d), dtype=torch.float16, device="cuda") for _ in "KV"]
+
+    def each(code, ds, st):
+        refused(code, ctx.ig_page_attention, ds, st, 1, 1, q, None, None, out)
+        refused(code, ctx.ig_append_pages, ds, st, None, 1, 1, q, k, k, 0, None, None, None, out)
+        refused(code, ctx.ig_gather_pages, ds, st, idx, 4, cnt, *sel)
+
+    ds = desc(B, H, d, N, N, "f16")
+    before = p.state()
+    each(ig.IG_EINVAL, ds, None)
+    for field, value, code in (("code", 2, ig.IG_EDTYPE), ("code", -1, ig.IG_EDTYPE), ("page_size", 8, ig.IG_ESHAPE), ("page_size", 48, ig.IG_ESHAPE),
+                               ("page_size", 256, ig.IG_ESHAPE), ("page_size", 0, ig.IG_ESHAPE), ("page_size", -16, ig.IG_ESHAPE), ("n_pages", 0, ig.IG_ESHAPE),
+                               ("n_pages", -1, ig.IG_ESHAPE), ("table_stride", 0, ig.IG_ESHAPE), ("table_stride", 1, ig.IG_ESHAPE),
+                               ("table", None, ig.IG_EINVAL), ("K", None, ig.IG_EINVAL), ("V", None, ig.IG_EINVAL), ("K_scale", None, ig.IG_EINVAL),
+                               ("V_scale", None, ig.IG_EINVAL), ("K", p.K.data_ptr() + 8, ig.IG_EINVAL), ("V", p.V.data_ptr() + 1, ig.IG_EINVAL),
+                               ("n_pages", 1 << 30, ig.IG_ESHAPE)):
+        each(code, ds, p.struct(**{field: value}))
+    for bad in (dict(d=48), dict(d=512), dict(d=16), dict(B=0), dict(H=0), dict(N=-1), dict(N=33), dict(N_cap=0)):
+        ds = desc(B, H, d, N, N, "f16")
+        for name, value in bad.items():
+            setattr(ds, name, value)
+        each(ig.IG_ESHAPE, ds, p.struct())
+    ds = desc(B, H, d, N, N, "f16")
+    ds.dtype = 2
+    each(ig.IG_EDTYPE, ds, p.struct())
+    torch.cuda.synchronize()
+    assert (out == SENTINEL).all() and all(torch.equal(a, b) for a, b in zip(before, p.state()))
+
+
+def test_arrays_that_are_refused(ctx):
+    B, H, d, N = 2, 2, 64, 32
+    p = Pages(B, H, d, N, 16, "i8", 1)
+    st, ds = p.struct(), desc(B, H, d, N, N, "f16")
+    q, k = rows((B, 1, 2 * H, d), "f16", 1), rows((B, 1, H, d), "f16", 2)
+    out = torch.full_like(q, SENTINEL)
+    idx, cnt = torch.zeros((B * H, 4), dtype=torch.int32, device="cuda"), i32([1] * (B * H))
+    sel = [torch.zeros((B * H, 4, d), dtype=torch.float16, device="cuda") for _ in "KV"]
+    lens = i32([1, 1])
+    r = rotary(64)[0]
+    before = p.state()
+    attend, append, gather = ctx.ig_page_attention, ctx.ig_append_pages, ctx.ig_gather_pages
+    # NULL, unaligned
+    for args in ((None, None, None, out), (q, None, None, None), (q.data_ptr() + 2, None, None, out), (q, None, None, out.data_ptr() + 8)):
+        refused(ig.IG_EINVAL, attend, ds, st, 2, 1, *args)
+    for args in ((q, None, k, 0, None, None, None, out), (q, k, None, 0, None, None, None, out), (q, k, k, 0, None, None, None, None),
+                 (q.data_ptr() + 2, k, k, 0, None, None, None, out), (q, k.data_ptr() + 2, k, 0, None, None, None, out),
+                 (q, k, k.data_ptr() + 4, 0, None, None, None, out), (q, k, k, 0, None, None, None, out.data_ptr() + 2)):
+        refused(ig.IG_EINVAL, append, ds, st, r, 2, 1, *args)
+    for args in ((None, 4, cnt, *sel), (idx, 4, None, *sel), (idx, 4, cnt, None, sel[1]), (idx, 4, cnt, sel[0], None), (idx, 4, cnt, sel[0].data_ptr() + 2, sel[1])):
+        refused(ig.IG_EINVAL, gather, ds, st, *args)
+    refused(ig.IG_ESHAPE, gather, ds, st, idx, 0, cnt, *sel)
+    # counts and strides
+    for group, n in ((0, 1), (2, 0), (-1, 1), (1 << 26, 1)):
+        refused(ig.IG_ESHAPE, attend, ds, st, group, n, q, None, None, out)
+        refused(ig.IG_ESHAPE, append, ds, st, r, group, n, q, k, k, 0, None, None, None, out)
+        refused(ig.IG_ESHAPE, ctx.ig_reserve_pages, ds, group, n)
+    for stride in (-1, 2 * H * d - 8, 2 * H * d + 4, 1 << 41):
+        refused(ig.IG_ESHAPE, append, ds, st, r, 2, 1, q, k, k, stride, None, None, None, out)
+    # overlaps
+    for at in (p.K, p.V, p.K_scale, p.V_scale, p.table, q):
+        refused(ig.IG_EINVAL, attend, ds, st, 2, 1, q, None, None, at)
+        if at is not q:
+            refused(ig.IG_EINVAL, append, ds, st, r, 2, 1, q, k, k, 0, None, None, None, at)
+            refused(ig.IG_EINVAL, gather, ds, st, idx, 4, cnt, at, sel[1])
+            refused(ig.IG_EINVAL, gather, ds, st, idx, 4, cnt, sel[0], at)
+    for at in (p.K, p.V):
+        refused(ig.IG_EINVAL, append, ds, st, r, 2, 1, q, at, k, 0, None, None, None, out)
+        refused(ig.IG_EINVAL, append, ds, st, r, 2, 1, at, k, k, 0, None, None, None, out)
+    refused(ig.IG_EINVAL, attend, ds, st, 2, 1, q, out, None, out)
+    refused(ig.IG_EINVAL, attend, ds, st, 2, 1, q, None, out, out)
+    for args in ((out, None, None), (None, out, None), (None, None, out)):
+        refused(ig.IG_EINVAL, append, ds, st, r, 2, 1, q, k, k, 0, *args, out)
+        refused(ig.IG_EINVAL, append, ds, st, r, 2, 1, q, k, k, 0, *[p.K_scale if x is out else x for x in args], out)
+    refused(ig.IG_EINVAL, append, ds, st, r, 2, 1, q, k, k, 0, None, None, None, k)
+    refused(ig.IG_EINVAL, append, ds, st, r, 2, 1, q, k, k, 2 * H * d, None, None, None, q.view(-1)[8:])
+    refused(ig.IG_EINVAL, append, ds, p.struct(V=p.K.data_ptr()), r, 2, 1, q, k, k, 0, None, None, None, out)
+    refused(ig.IG_EINVAL, append, ds, p.struct(V_scale=p.K_scale.data_ptr()), r, 2, 1, q, k, k, 0, None, None, None, out)
+    refused(ig.IG_EINVAL, gather, ds, st, idx, 4, cnt, sel[0], sel[0])
+    refused(ig.IG_EINVAL, gather, ds, st, sel[0], 4, cnt, *sel)
+    refused(ig.IG_EINVAL, gather, ds, st, idx, 4, sel[1], *sel)
+    torch.cuda.synchronize()
+    assert (out == SENTINEL).all() and all(torch.equal(a, b) for a, b in zip(before, p.state()))
+    # without queries group and q_out are not looked at
+    append(ds, st, r, -5, 1, None, k, k, 0, lens, lens, None, 7)
+    torch.cuda.synchronize()
+
+
+def test_rotations_that_are_refused(ctx):
+    n, heads, d = 3, 2, 64
+    x, out, pos = rows((n, heads, d), "f16", 1), torch.full((n, heads, d), SENTINEL, dtype=torch.float16, device="cuda"), i32([1, 2, 3])
+    r = rotary(64)[0]
+
+    def call(dtype=ig.IG_F16, n=n, heads=heads, d=d, r=r, inverse=0, pos=pos, x=x, xs=0, out=out, os=0):
+        ctx.ig_rotate_rows(dtype, n, heads, d, r, inverse, pos, x, xs, out, os)
+
+    for code, bad in ((ig.IG_EDTYPE, dict(dtype=2)), (ig.IG_ESHAPE, dict(n=0)), (ig.IG_ESHAPE, dict(heads=0)), (ig.IG_ESHAPE, dict(d=0)),
+                      (ig.IG_ESHAPE, dict(d=72)), (ig.IG_ESHAPE, dict(d=1040)), (ig.IG_ESHAPE, dict(d=48)), (ig.IG_EINVAL, dict(r=None)),
+                      (ig.IG_EINVAL, dict(pos=None)), (ig.IG_EINVAL, dict(x=None)), (ig.IG_EINVAL, dict(out=None)), (ig.IG_EINVAL, dict(inverse=2)),
+                      (ig.IG_EINVAL, dict(x=x.data_ptr() + 2)), (ig.IG_EINVAL, dict(out=out.data_ptr() + 8)), (ig.IG_ESHAPE, dict(xs=127)),
+                      (ig.IG_ESHAPE, dict(xs=132)), (ig.IG_ESHAPE, dict(os=-8)), (ig.IG_ESHAPE, dict(os=120)), (ig.IG_EINVAL, dict(out=x, os=136)),
+                      (ig.IG_EINVAL, dict(out=x.view(-1)[64:])), (ig.IG_EINVAL, dict(pos=out)), (ig.IG_ESHAPE, dict(n=2 ** 31 - 1, heads=2 ** 17)),
+                      (ig.IG_ESHAPE, dict(heads=2 ** 20))):
+        with pytest.raises(ig.IgError) as e:
+            call(**bad)
+        assert e.value.code == code, (bad, e.value)
+    for field, value, code in (("dims", 0, ig.IG_ESHAPE), ("dims", 7, ig.IG_ESHAPE), ("dims", 66, ig.IG_ESHAPE), ("dims", -2, ig.IG_ESHAPE),
+                               ("interleaved", 2, ig.IG_EINVAL), ("magnitude", math.nan, ig.IG_EINVAL), ("magnitude", math.inf, ig.IG_EINVAL),
+                               ("freq", None, ig.IG_EINVAL), ("freq", r.tensors[0].data_ptr() + 4, ig.IG_EINVAL), ("freq", out.data_ptr(), ig.IG_EINVAL)):
+        bad = ig.IgRotary(r.tensors[0])
+        setattr(bad, field, value)
+        with pytest.raises(ig.IgError) as e:
+            call(r=bad)
+        assert e.value.code == code, (field, value, e.value)
+        if field != "freq" or value != out.data_ptr():
+            p = Pages(1, 2, 64, 16, 16, "i8", 1)
+            refused(code, ctx.ig_append_pages, desc(1, 2, 64, 0, 16, "f16"), p.struct(), bad, 1, 3, None, x, x, 0, None, None, None, None)
+    torch.cuda.synchronize()
+    assert (out == SENTINEL).all()
+
+
+def test_more_than_a_launch_takes(ctx):
+    """Refused for its size before anything is launched (every call here has an argument that would be refused later, too)."""
+    p = Pages(1, 1, 32, 16, 16, "i8", 1)
+    x = torch.zeros(1 << 12, dtype=torch.float16, device="cuda")
+    bad = x.data_ptr() + 2
+    refused(ig.IG_ESHAPE, ctx.ig_append_pages, desc(1 << 12, 1 << 11, 32, 1, 1, "f16"), p.struct(n_pages=1), None, 1, 9, None, bad, x, 0, None, None, None, None)
+    refused(ig.IG_ESHAPE, ctx.ig_append_pages, desc(1 << 8, 1 << 11, 32, 1, 1, "f16"), p.struct(n_pages=1), None, 64, 4, bad, x, x, 0, None, None, None, x)
+    refused(ig.IG_ESHAPE, ctx.ig_gather_pages, desc(1 << 8, 1 << 8, 256, 1, 1, "f32"), p.struct(n_pages=1), x, 1 << 24, x, bad, x)
+    refused(ig.IG_ESHAPE, ctx.ig_page_attention, desc(1 << 14, 1 << 10, 32, 1, 1, "f16"), p.struct(n_pages=1), 1, 1, bad, None, None, x)
