@@ -336,7 +336,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
 // 64 slots; the 32-slot half blocks are a pipeline of logits, weights and outputs.  A tile's codes come to registers a turn ahead
 // and are written to LDS as halves, once for all waves; so every turn has, beside its products, the codes of one tile of K and
 // one of V to convert (16 codes: 20 vector instructions from int8, 8 from e4m3).
-// A lane's load covers at most 16 consecutive slots, i.e. one page for the whole wave.  Lane l looks after the 16 slots
+// A wave's loads of a tile cover at most 16 consecutive slots, i.e. one page.  Lane l looks after the 16 slots
 // l % 4 of a tile: their entry of the table (asked for three turns ahead), and their scales.
 constexpr float RISE = 6.f, PROMPT_LIFT = 9.f;
 constexpr int PROMPT_KEYS = 64;
@@ -345,7 +345,7 @@ template <int D, int NW, int RB, bool E4M3> __global__ __launch_bounds__(NW * 64
   constexpr int KS = D / 16, OB = D / 32, TK = PROMPT_KEYS, ROWS = RB * NW * 32;
   constexpr int LB = TK * D / (NW * 64) < 16 ? 8 : 16;            // bytes of a lane's load
   constexpr int PIECES = D / LB, LR = 64 / PIECES, LOADS = TK / (LR * NW);      // loads of a row; rows of a wave's load; loads of a wave
-  static_assert(LOADS >= 1 && LR <= 16, "a wave's load stays in a page");
+  static_assert(LOADS >= 1 && 16 % (LR * LOADS) == 0, "a wave's loads of a tile stay in a page");
   constexpr int LW = LB / 4;
   __shared__ __attribute__((aligned(16))) half_t tiles[2][2][TK * D];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -401,13 +401,11 @@ template <int D, int NW, int RB, bool E4M3> __global__ __launch_bounds__(NW * 64
     };
     auto load_codes = [&](const char *pool, int tile, unsigned entries, unsigned (&to)[LOADS][LW]) __attribute__((always_inline)) {
       tile = min(tile, t_end - 1);
+      const unsigned page = (unsigned)__builtin_amdgcn_readlane((int)entries, w * LR * LOADS / 16);
+      const char *base = pool + (unsigned long)page * p.page_bytes + head;
 #pragma unroll
-      for (int x = 0; x < LOADS; ++x) {
-        const int r0 = (w * LOADS + x) * LR;              // (rows r0 .. r0 + LR - 1: one page)
-        const unsigned page = (unsigned)__builtin_amdgcn_readlane((int)entries, r0 / 16);
-        const char *base = pool + (unsigned long)page * p.page_bytes + head;
+      for (int x = 0; x < LOADS; ++x)
         load_words<LW>(base + (unsigned)((min(tile * TK + from_row + x * LR, last) & in_page) * D + from_byte), to[x]);
-      }
     };
     // part `x` of eight of a tile's codes to LDS as halves
     constexpr int RUNS = LOADS * LW / 2;                  // runs of eight codes that a lane holds
@@ -507,6 +505,7 @@ template <int D, int NW, int RB, bool E4M3> __global__ __launch_bounds__(NW * 64
 #pragma unroll
         for (int c = 0; c < RB; ++c) next[c] = floatx16{};
       }
+      __builtin_amdgcn_s_setprio(1);                      // (a wave that multiplies before one that works out references: half a percent)
 #pragma unroll
       for (int x = 0; x < 8; ++x) {
         if (x + LEAD < 8) read(x + LEAD);
@@ -535,6 +534,7 @@ template <int D, int NW, int RB, bool E4M3> __global__ __launch_bounds__(NW * 64
             }
         }
       }
+      __builtin_amdgcn_s_setprio(0);
       if constexpr (NOW) {
 #pragma unroll
         for (int c = 0; c < RB; ++c) {
