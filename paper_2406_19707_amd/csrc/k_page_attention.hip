@@ -651,7 +651,10 @@ int div_up(long n, long d) { return (int)((n + d - 1) / d); }
 
 // Query rows of a workgroup: page_stream's 16 or 32, page_prompt's 128 or 256 (as over a pool of rows, by the same rules).
 int row_block(const ig_desc *d, long R) { return R <= 16 || d->d > 128 || d->dtype == IG_F32 ? 16 : 32; }
-bool many_rows(const ig_desc *d, long R) { return d->dtype == IG_F16 && R > (d->d > 128 ? 16 : 32); }
+// page_stream's row blocks read the codes again for every 32 (d = 256: 16) rows, out of the caches, page_prompt's 128 once, but a turn of
+// its takes longer.  (16 x 8 heads of 4096, 40 rows: 47 us there, 53 here; d = 64, 48 rows 32 and 35; d = 256, 20 rows 75 and
+// 115, 60 rows, 4 x 8 of 4000, 45 and 50; 56 rows, 3 x 11 ragged of 4923, 23 and 26; but 72 rows, 16 x 8 of 4096, 66 and 59.)
+bool many_rows(const ig_desc *d, long R) { return d->dtype == IG_F16 && R > 64; }
 int prompt_rows(const ig_desc *d, const PageCall &c) {
   const long R = (long)c.n_q * c.group;
   if (d->d == 128) return R > 128 && 2 * (long)c.n_q <= d->N ? 256 : 128;
@@ -725,10 +728,14 @@ int ig_launch_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *page
   const dim3 grid(a.per_xcd * 8), block(256);
 #define STREAM(D, NT, E4M3, F32, ONCE)                                                               \
   {                                                                                                  \
-    auto k = page_stream<D, NT, E4M3, F32, ONCE>;                                                         \
+    auto k = page_stream<D, NT, E4M3, F32, ONCE>;                                                    \
     IG_LAUNCH(ctx, IG_K_CACHE, k, grid, block, stream, a, refs);                                     \
   }
-#define PROMPT_WAVES(D, NW, RB, E4M3)                                                                 \
+#define STREAM_ONCE(D, NT, E4M3, F32)                                                                \
+  {                                                                                                  \
+    if (p.nrb == 1) STREAM(D, NT, E4M3, F32, true) else STREAM(D, NT, E4M3, F32, false)              \
+  }
+#define PROMPT_WAVES(D, NW, RB, E4M3)                                                                \
   {                                                                                                  \
     auto k = page_prompt<D, NW, RB, E4M3>;                                                           \
     IG_LAUNCH(ctx, IG_K_CACHE, k, grid, dim3(NW * 64), stream, a, refs);                             \
@@ -741,10 +748,9 @@ int ig_launch_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *page
   }
 #define STREAM_ROWS(D, E4M3)                                                                         \
   {                                                                                                  \
-    if (d->dtype == IG_F32 && p.nrb == 1) STREAM(D, 1, E4M3, true, true)                             \
-    else if (d->dtype == IG_F32) STREAM(D, 1, E4M3, true, false)                                     \
-    else if (p.rb == 16) STREAM(D, 1, E4M3, false, true)                                             \
-    else if constexpr (D <= 128) STREAM(D, 2, E4M3, false, true)                                     \
+    if (d->dtype == IG_F32) STREAM_ONCE(D, 1, E4M3, true)                                            \
+    else if (p.rb == 16) STREAM_ONCE(D, 1, E4M3, false)                                              \
+    else if constexpr (D <= 128) STREAM_ONCE(D, 2, E4M3, false)                                      \
   }
 #define BY_DIM(DO, E4M3)                                                                             \
   switch (d->d) {                                                                                    \
