@@ -650,7 +650,12 @@ template <int D, int NW, int RB, bool E4M3> __global__ __launch_bounds__(NW * 64
 int div_up(long n, long d) { return (int)((n + d - 1) / d); }
 
 // Query rows of a workgroup: page_stream's 16 or 32, page_prompt's 128 or 256 (as over a pool of rows, by the same rules).
-int row_block(const ig_desc *d, long R) { return R <= 16 || d->d > 128 || d->dtype == IG_F32 ? 16 : 32; }
+// In float32 32 only where turns of 128 slots are enough to fill the GPU with (2 x 16 heads of 1024 tokens 48 us with 32, 55 with 16; 20
+// rows, 16 x 8 of 4096, 37 and 43; but 4 heads of 512 9.2 and 6.7).
+int row_block(const ig_desc *d, long R) {
+  if (R <= 16 || d->d > 128) return 16;
+  return d->dtype == IG_F16 || (double)d->B * d->H * div_up(R, 32) * div_up(d->N, 128) >= 1024 ? 32 : 16;
+}
 // page_stream's row blocks read the codes again for every 32 (d = 256: 16) rows, out of the caches, page_prompt's 128 once, but a turn of
 // its takes longer.  (16 x 8 heads of 4096, 40 rows: 47 us there, 53 here; d = 64, 48 rows 32 and 35; d = 256, 20 rows 75 and
 // 115, 60 rows, 4 x 8 of 4000, 45 and 50; 56 rows, 3 x 11 ragged of 4923, 23 and 26; but 72 rows, 16 x 8 of 4096, 66 and 59.)
@@ -704,7 +709,7 @@ PagePlan ig_page_plan(const ig_desc *d, const PageCall &c) {
 // A bound for any number of tokens and slots up to these: states of at most MOST_SLICES slices of every row, and of at most
 // ROUNDS rounds of workgroups.
 size_t ig_page_reserve_bytes(const ig_desc *d, int group, int n_q) {
-  const long all = (long)MOST_SLICES * d->B * d->H * n_q * group, rounds = ROUNDS * (d->dtype == IG_F16 ? 256 * workgroups_of(256) : 16 * workgroups_of(16));
+  const long all = (long)MOST_SLICES * d->B * d->H * n_q * group, rounds = ROUNDS * (d->dtype == IG_F16 ? 256 * workgroups_of(256) : 32 * workgroups_of(32));
   return (size_t)(all < rounds ? all : rounds) * (sizeof(float2) + d->d * sizeof(float)) + 2 * 256;
 }
 
@@ -748,9 +753,11 @@ int ig_launch_page_attention(ig_ctx *ctx, const ig_desc *d, const ig_pages *page
   }
 #define STREAM_ROWS(D, E4M3)                                                                         \
   {                                                                                                  \
-    if (d->dtype == IG_F32) STREAM_ONCE(D, 1, E4M3, true)                                            \
+    if (p.rb == 16 && d->dtype == IG_F32) STREAM_ONCE(D, 1, E4M3, true)                              \
     else if (p.rb == 16) STREAM_ONCE(D, 1, E4M3, false)                                              \
-    else if constexpr (D <= 128) STREAM_ONCE(D, 2, E4M3, false)                                      \
+    else if constexpr (D <= 128) {                                                                   \
+      if (d->dtype == IG_F32) STREAM_ONCE(D, 2, E4M3, true) else STREAM_ONCE(D, 2, E4M3, false)      \
+    }                                                                                                \
   }
 #define BY_DIM(DO, E4M3)                                                                             \
   switch (d->d) {                                                                                    \

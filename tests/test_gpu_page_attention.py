@@ -233,3 +233,17 @@ def test_pages_far_into_the_pool(ctx):
         torch.cuda.synchronize()
         got.append(to)
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and got[0][0].any()
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+def test_float32_rows_in_blocks_of_32(ctx, code, d):
+    """Enough turns to fill the GPU with: two blocks of 16 rows a wave, in slices too."""
+    run_attention(ctx, "f32", code, d, B=4, H=4, group=2, n_q=41, N=3000, N_cap=3000, page=32, kv=[3000, 1500, 41, 7], nq=[41, 33, 41, 9], seed=d)
+    run_attention(ctx, "f32", code, d, B=8, H=16, group=1, n_q=130, N=130, N_cap=140, page=16, seed=d + 1)
+
+
+def test_half_precision_rows_in_several_blocks(ctx):
+    """33 to 64 rows, and 17 to 64 at d = 256: row blocks over the same codes."""
+    for code, d, n_q in (("i8", 128, 17), ("e4m3", 64, 32), ("i8", 256, 9), ("e4m3", 256, 31), ("i8", 32, 20)):
+        run_attention(ctx, "f16", code, d, B=3, H=2, group=2, n_q=n_q, N=1000, N_cap=1000, page=128, kv=[1000, 300, 5], seed=n_q)
