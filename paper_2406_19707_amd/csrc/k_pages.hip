@@ -110,7 +110,7 @@ template <typename T, bool E4M3, int KIND> __global__ __launch_bounds__(1024) vo
     const int first_pos = (a.pos ? a.pos[b] : start) + (r0 - start);
 #pragma unroll
     for (int k = 0; k < APPEND_UNITS; ++k)
-      if (16 * unit[k] < dims) turns_of(unit[k], first_pos + row[k], a.r, turn[k]);
+      if (mine[k] && 16 * unit[k] < dims) turns_of(unit[k], first_pos + row[k], a.r, turn[k]);
   }
   for (int h = h0; h < h1; ++h) {
     float x[APPEND_UNITS][16], top = 0.f;
