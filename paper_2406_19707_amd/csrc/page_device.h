@@ -101,8 +101,8 @@ __device__ __forceinline__ void turns_of(int s, int pos, const RotaryRefs &r, fl
   for (int e = 0; e < 8; ++e) {
     const int c = 8 * s + e;
     turn[e] = turn_of(pos, r.freq[min(c, r.dims / 2 - 1)], r);
-    // (one after the other: all at once they take more registers than there are)
-    asm volatile("" : "+v"(turn[e].x), "+v"(turn[e].y));
+    // (two at a time: all at once they take more registers than there are)
+    if (e % 2) asm volatile("" : "+v"(turn[e - 1].x), "+v"(turn[e - 1].y), "+v"(turn[e].x), "+v"(turn[e].y));
   }
 }
 // eight values of a row
