@@ -514,14 +514,15 @@ typedef struct {
   int32_t code;          /* IG_CODE_* */
   const int32_t *table;  /* device [B, table_stride]: pages of each sequence, in order */
   void *K, *V;           /* device [n_pages, H, page_size, d], a byte each, 16-byte aligned */
-  float *K_scale, *V_scale;  /* device [n_pages, H]: powers of two, 2^-80 .. 2^120 (any other value is read as the power of
-                                two at or below it, within these bounds) */
+  float *K_scale, *V_scale;  /* device [n_pages, H]: powers of two, 2^-80 .. 2^122 (any other value is read as the power of
+                                two at or below it, within these bounds; ig_page_attention with IG_F16: K's up to 2^100) */
 } ig_pages;
 
 /* Common to the calls below: B, H, d, N, N_cap, dtype and (attention) scale of the descriptor are used as in the calls over whole
  * pools, with N_cap the slots a sequence may have; d = 32, 64, 128 or 256.  Entries of the table outside [0, n_pages) are
  * clamped into it where slots are read, and nothing is written through them.  Entries of pages that a sequence does not reach are
- * not looked at.  Several sequences may share pages that are only read; a page that a call appends to belongs to one sequence.
+ * not looked at.  Several sequences may share pages that are only read; a page that a call appends to belongs to one sequence
+ * and stands once in its row of the table.
  *
  * Appends rows to ragged sequences as ig_append_rows does, rotated and rounded to 8 bits on the way.  For j < n_append[b], slot
  * kv_len[b] + j of sequence b receives k_rows[b, j] rotated at pos[b] + j (pos: device int32 [B], or NULL: the slot), and
@@ -532,19 +533,20 @@ typedef struct {
  * parts of one projection's output), or 0: each is dense.  n_append, kv_len as in ig_append_rows.
  * The scale of a page that receives its first row is the least power of two with which its rows' largest value is at most 127 (448)
  * codes, and 2^-80 at least.  That of a page that holds rows is doubled as often as the new rows need it, and the codes of the rows it
- * holds are rounded again.  Values are rounded to the nearest code, ties to the even one: a row is off by at most half a scale
- * (e4m3: by 2^-4 of itself, or 2^-10 of a scale where that is more) after its append, and by less than one scale however often it
- * has doubled since (e4m3: it loses bits only below 2^-6 of a scale).  NaN and infinities are stored as 0.
- * What lies in the other slots of a page is left as it was. */
+ * holds are rounded again: so scales do not depend on how rows are divided among calls.  Values are rounded to the nearest code, ties
+ * to the even one: a row is off by at most half a scale (e4m3: by 2^-4 of itself, or 2^-10 of a scale where that is more) after
+ * its append, and by less than one scale (2^-4 of itself and 2^-9 of a scale) however often it has doubled since.  What is not
+ * finite, after the rotation, is stored as 0.  What lies in the other slots of a page is left as it was.  Rows, lengths, positions, table
+ * and frequencies must not overlap what is written (IG_EINVAL). */
 int ig_append_pages(ig_ctx *ctx, const ig_desc *desc, const ig_pages *pages, const ig_rotary *rotary, int32_t group,
                     int32_t n_rows, const void *q, const void *k_rows, const void *v_rows, int64_t row_stride,
                     const int32_t *n_append, const int32_t *kv_len, const int32_t *pos, void *q_out, void *stream);
 
 /* Attention of n_q tokens per sequence that are in the pages already, as ig_cache_attention without mass: q, out, q_len, kv_len and
- * group as there, and the same expectations of finite rows and logits.  Every product and sum is in float32; with IG_F16 the
+ * group as there, and the same expectations of finite rows and logits.  Products and sums are in float32; with IG_F16 the
  * softmax weights, times their page's scale, are rounded to half precision where they multiply the codes of V, by at most 2^-11
- * of themselves down to 2^-23 of the row's largest (calls of up to 32 query rows a pool: 2^-28), and by at most 2^-34 of that
- * below; with IG_F32 queries and weights are taken as two halves each, which leaves 2^-22 of themselves. */
+ * of themselves down to 2^-23 of the row's largest (calls of up to 64 query rows a pool head: 2^-28), and by at most 2^-34 of that
+ * below; with IG_F32 queries and weights are taken as two halves each: off by at most 2^-22 of themselves, or 2^-38 of a row's largest. */
 int ig_page_attention(ig_ctx *ctx, const ig_desc *desc, const ig_pages *pages, int32_t group, int32_t n_q, const void *q,
                       const int32_t *q_len, const int32_t *kv_len, void *out, void *stream);
 
@@ -552,8 +554,8 @@ int ig_page_attention(ig_ctx *ctx, const ig_desc *desc, const ig_pages *pages, i
  * (allocates; synchronous).  The other calls here need none. */
 int ig_reserve_pages(ig_ctx *ctx, const ig_desc *desc, int32_t group, int32_t n_q);
 
-/* ig_gather_kv out of pages: row j < sel_cnt[b*H+h] of K_sel, V_sel (device [B*H, sel_stride, d] of desc->dtype, 16-byte aligned) is
- * the value of slot sel_idx[b*H+h, j] (clamped into [0, N_cap)), a code times its scale, rounded once; rows from sel_cnt on are not
+/* ig_gather_kv out of pages: row j < sel_cnt[b*H+h] of K_sel, V_sel (device [B*H, sel_stride, d] of desc->dtype, 16-byte aligned, apart
+ * from each other and all inputs) is the value of slot sel_idx[b*H+h, j] (clamped into [0, N_cap)), a code times its scale, rounded once; rows from sel_cnt on are not
  * written.  What ig_slab_build, ig_sparse_attention and the calls over whole pools need of such a cache. */
 int ig_gather_pages(ig_ctx *ctx, const ig_desc *desc, const ig_pages *pages, const int32_t *sel_idx, int32_t sel_stride,
                     const int32_t *sel_cnt, void *K_sel, void *V_sel, void *stream);

@@ -51,6 +51,9 @@ template <int W, bool ONCE> __device__ __forceinline__ void load_codes_of(const 
   }
 }
 
+// K's largest scale: with half-precision queries less, so that its product with the logits' scale stays finite
+template <bool F32> constexpr int k_scale_most() { return F32 ? SCALE_MOST : 100; }
+
 // a float as two halves: x - hi - lo is at most 2^-22 |x|, or 2^-25
 struct Halves {
   half_t hi, lo;
@@ -136,7 +139,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
     page_next = page_at(tile + 4);
   }
   int lim[NT];
-  float q_scale[NT];
+  float q_scale[NT];                                      // of a row's logits, but for K's scale
   half8 qf[NT][PARTS][KS];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
@@ -145,7 +148,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
     const T *src = static_cast<const T *>(a.q) + (((long)b * a.n_q + min(iq, a.n_q - 1)) * a.Hq + h * (int)a.by_group.d + gq) * D;
     // (the eight channels of product c of this lane)
     auto channel = [&](int c) { return KB == 8 ? 8 * g : c / 2 * 64 + g * 16 + c % 2 * 8; };
-    q_scale[n] = 1.f;
+    q_scale[n] = a.c;
     if constexpr (!F32) {
 #pragma unroll
       for (int c = 0; c < KS; ++c) qf[n][0][c] = __builtin_bit_cast(half8, flip_sign<half_t>(*reinterpret_cast<const uint4 *>(src + channel(c)), a.flip));
@@ -160,7 +163,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
       }
       const int e = min(max((int)(__float_as_uint(column_max(top)) >> 23), 20), 254) - 127;
       const float by = exp2_int(13 - e);
-      q_scale[n] = exp2_int(e - 13);
+      q_scale[n] = exp2_int(e - 13) * a.c;
 #pragma unroll
       for (int c = 0; c < KS * 8; ++c) {
         const Halves s = split(x[c] * by);
@@ -200,14 +203,14 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
 #pragma unroll
           for (int x = 0; x < PARTS; ++x) s[n][m] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[n][x][c], s[n][m], 0, 0, 0);
       }
-    const int ke = scale_exponent(ks), ve = scale_exponent(vs[NOW]);
+    const int ke = scale_exponent<k_scale_most<F32>()>(ks), ve = scale_exponent(vs[NOW]);
     if constexpr (more) {
       page = page_next;
       page_next = page_at(tile + 8);
       load_k(tile + 4, page);
       load_v(tile + 4, page, v[1 - NOW], vs[1 - NOW]);
     }
-    const float k_by = exp2_int(ke) * a.c, lift_v = (float)ve, v_back = exp2_int(-ve);
+    const float k_by = exp2_int(ke), lift_v = (float)ve, v_back = exp2_int(-ve);
     const int t0 = tile * TT + 8 * g;
     if ((tile + 1) * TT > lim_min) {
 #pragma unroll
@@ -565,7 +568,7 @@ template <int D, int NW, int RB, bool E4M3> __global__ __launch_bounds__(NW * 64
         return make_float2(p.K_scale[at], p.V_scale[at]);
       };
       auto ready = [&](float2 s) __attribute__((always_inline)) {
-        const int ke = scale_exponent(s.x), ve = scale_exponent(s.y);
+        const int ke = scale_exponent<k_scale_most<false>()>(s.x), ve = scale_exponent(s.y);
         return Scales{exp2_int(ke) * a.c, (float)ve, exp2_int(-ve)};
       };
       Scales now = ready(scales_of(e0)), before = now;

@@ -22,8 +22,8 @@ __device__ __forceinline__ unsigned page_read(const PageRefs &p, int entry) { re
 // Scales are powers of two, so that rounding a value by one is exact, a page's codes can be rounded again to a larger one
 // with errors that halve every time, and a scale is its exponent.
 constexpr int SCALE_LEAST = -80, SCALE_MOST = 122;
-__device__ __forceinline__ int scale_exponent(float s) {
-  return min(max((int)(__float_as_uint(s) >> 23 & 255) - 127, SCALE_LEAST), SCALE_MOST);
+template <int MOST = SCALE_MOST> __device__ __forceinline__ int scale_exponent(float s) {
+  return min(max((int)(__float_as_uint(s) >> 23 & 255) - 127, SCALE_LEAST), MOST);
 }
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }      // -126 <= e <= 127
 // The least exponent e with top <= most * 2^e: most is 127 = 1.984375 * 2^6, or 448 = 1.75 * 2^8.

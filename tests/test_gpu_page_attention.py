@@ -247,3 +247,25 @@ def test_half_precision_rows_in_several_blocks(ctx):
     """33 to 64 rows, and 17 to 64 at d = 256: row blocks over the same codes."""
     for code, d, n_q in (("i8", 128, 17), ("e4m3", 64, 32), ("i8", 256, 9), ("e4m3", 256, 31), ("i8", 32, 20)):
         run_attention(ctx, "f16", code, d, B=3, H=2, group=2, n_q=n_q, N=1000, N_cap=1000, page=128, kv=[1000, 300, 5], seed=n_q)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("n_q", [1, 70])
+def test_scales_at_the_ends_of_their_range(ctx, dtype, n_q):
+    """Pages of zero codes with the largest scales, and of the smallest, beside ordinary ones."""
+    B, H, d, N = 1, 2, 64, 160
+    pages = Pages(B, H, d, N, 32, "i8", 3).fill([N], 4)
+    at = pages.table[0].long()
+    pages.K[at[1]], pages.V[at[1]], pages.K_scale[at[1]], pages.V_scale[at[1]] = 0, 0, 2.0 ** 122, 2.0 ** 122
+    pages.K_scale[at[2]], pages.V_scale[at[2]] = 2.0 ** -80, 2.0 ** -80
+    q = rows((B, n_q, H, d), dtype, 5)
+    out, plain = torch.full_like(q, SENTINEL), torch.full_like(q, SENTINEL)
+    ds = desc(B, H, d, N, N, dtype, 8.0)
+    ctx.ig_page_attention(ds, pages.struct(), 1, n_q, q, None, None, out)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out).all()
+    # keys of zero codes have logits of zero whatever their scale; their values are zero, so they only take weight
+    pages.K_scale[at[1]] = 1.0
+    ctx.ig_page_attention(ds, pages.struct(), 1, n_q, q, None, None, plain)
+    torch.cuda.synchronize()
+    assert torch.equal(out, plain)
