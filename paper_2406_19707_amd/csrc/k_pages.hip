@@ -60,21 +60,8 @@ struct AppendArgs {
 // the value to be stored: 0 for one that is not finite
 __device__ __forceinline__ float finite_or_zero(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? 0.f : x; }
 
-template <typename T, bool E4M3, int KIND> __global__ __launch_bounds__(1024) void append_pages(AppendArgs a) {
-  __shared__ float tops[2][16];
-  const int tid = threadIdx.x, team = blockDim.x;
-  if ((int)blockIdx.x >= a.kv_blocks) {
-    const int u = (blockIdx.x - a.kv_blocks) * team + tid;
-    if (u >= a.q_total) return;
-    const int at = u >> a.unit_shift, s = u & ((1 << a.unit_shift) - 1), i = a.by_q_parts.div(at), h = (at - i * (int)a.by_q_parts.d) * a.q_per;
-    const int b = a.by_rows.div(i), j = i - b * a.n_rows;
-    if (j >= (a.n_append ? min(max(a.n_append[b], 0), a.n_rows) : a.n_rows)) return;
-    const int first = a.pos ? a.pos[b] : (a.kv_len ? min(max(a.kv_len[b], 0), a.N_cap) : a.N);
-    rotate_heads<T, KIND>(static_cast<const T *>(a.q) + i * a.q_stride, static_cast<T *>(a.q_out) + (long)i * a.Hq * a.d, a.d, h, min(h + a.q_per, a.Hq), s,
-                    first + j, a.r);
-    return;
-  }
-  const int kv = blockIdx.x & 1, work = blockIdx.x >> 1;
+template <typename T, bool E4M3, int KIND> __device__ __forceinline__ void append_page(const AppendArgs &a, int kv, float (&tops)[2][16]) {
+  const int tid = threadIdx.x, team = blockDim.x, work = blockIdx.x >> 1;
   const int at = a.by_pages.div(work), p = work - at * (int)a.by_pages.d, b = a.by_parts.div(at), h0 = (at - b * (int)a.by_parts.d) * a.per;
   const int start = a.kv_len ? min(max(a.kv_len[b], 0), a.N_cap) : a.N;
   const int n = min(a.n_append ? min(max(a.n_append[b], 0), a.n_rows) : a.n_rows, a.N_cap - start);
@@ -159,17 +146,28 @@ template <typename T, bool E4M3, int KIND> __global__ __launch_bounds__(1024) vo
       unsigned c[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) c[i] = encode4<E4M3>(x[k][4 * i] * inv, x[k][4 * i + 1] * inv, x[k][4 * i + 2] * inv, x[k][4 * i + 3] * inv);
-      if (Unit<T, KIND>::one_by_one(dims)) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) to[any_channel(8 * unit[k] + e % 8, e / 8, dims)] = (char)(c[e / 4] >> e % 4 * 8);
-      } else {
-        const Runs runs = runs_of<KIND>(unit[k], dims);
-        *reinterpret_cast<uint2 *>(to + runs.first) = make_uint2(c[0], c[1]);
-        *reinterpret_cast<uint2 *>(to + runs.second) = make_uint2(c[2], c[3]);
-      }
+      Unit<T, KIND>::store_codes(to, unit[k], dims, c);
     }
     if (tid == 0 && (!held || e2 > before)) scales[h] = exp2_int(e2);
   }
+}
+
+template <typename T, bool E4M3, int KIND> __global__ __launch_bounds__(1024) void append_pages(AppendArgs a) {
+  __shared__ float tops[2][16];
+  if ((int)blockIdx.x >= a.kv_blocks) {
+    const int u = (blockIdx.x - a.kv_blocks) * blockDim.x + threadIdx.x;
+    if (u >= a.q_total) return;
+    const int at = u >> a.unit_shift, s = u & ((1 << a.unit_shift) - 1), i = a.by_q_parts.div(at), h = (at - i * (int)a.by_q_parts.d) * a.q_per;
+    const int b = a.by_rows.div(i), j = i - b * a.n_rows;
+    if (j >= (a.n_append ? min(max(a.n_append[b], 0), a.n_rows) : a.n_rows)) return;
+    const int first = a.pos ? a.pos[b] : (a.kv_len ? min(max(a.kv_len[b], 0), a.N_cap) : a.N);
+    rotate_heads<T, KIND>(static_cast<const T *>(a.q) + i * a.q_stride, static_cast<T *>(a.q_out) + (long)i * a.Hq * a.d, a.d, h, min(h + a.q_per, a.Hq), s,
+                    first + j, a.r);
+    return;
+  }
+  // (values have no short runs)
+  if (run_of(KIND) < 8 && (blockIdx.x & 1)) append_page<T, E4M3, TURN_NONE>(a, 1, tops);
+  else append_page<T, E4M3, KIND>(a, blockIdx.x & 1, tops);
 }
 
 // ---- rows read back ------------------------------------------------------------------------------------------------
@@ -267,7 +265,9 @@ int ig_launch_rotate(ig_ctx *ctx, int dtype, int n, int heads, int d, const ig_r
   {                                                                                                  \
     if (a.r.kind == TURN_HALVES) ROTATE(T, TURN_HALVES)                                              \
     else if (a.r.kind == TURN_ADJACENT) ROTATE(T, TURN_ADJACENT)                                     \
-    else ROTATE(T, TURN_ANY)                                                                         \
+    else if (a.r.kind == TURN_HALVES_4) ROTATE(T, TURN_HALVES_4)                                     \
+    else if (a.r.kind == TURN_HALVES_2) ROTATE(T, TURN_HALVES_2)                                     \
+    else ROTATE(T, TURN_HALVES_1)                                                                    \
   }
   if (dtype == IG_F16) ROTATE_KIND(half_t) else ROTATE_KIND(float)
   return IG_OK;
@@ -315,7 +315,9 @@ int ig_launch_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, con
     if (a.r.kind == TURN_NONE) APPEND(T, E4M3, TURN_NONE)                                            \
     else if (a.r.kind == TURN_HALVES) APPEND(T, E4M3, TURN_HALVES)                                   \
     else if (a.r.kind == TURN_ADJACENT) APPEND(T, E4M3, TURN_ADJACENT)                               \
-    else APPEND(T, E4M3, TURN_ANY)                                                                   \
+    else if (a.r.kind == TURN_HALVES_4) APPEND(T, E4M3, TURN_HALVES_4)                               \
+    else if (a.r.kind == TURN_HALVES_2) APPEND(T, E4M3, TURN_HALVES_2)                               \
+    else APPEND(T, E4M3, TURN_HALVES_1)                                                              \
   }
 #define APPEND_CODE(T)                                                                               \
   {                                                                                                  \

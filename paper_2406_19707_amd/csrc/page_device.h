@@ -55,10 +55,11 @@ template <bool E4M3> __device__ __forceinline__ floatx4 decode4(unsigned v) {
 
 // ---- rotary embedding ----------------------------------------------------------------------------------------------
 // A thread takes units of 16 channels of a row, eight pairs a_e, b_e.  The first dims/2 pairs of a row's are rotated, pair c
-// by freq[c]; channels past dims are pairs that stay.  Where pairs are (c, c + dims/2) with dims a multiple of 16, and where
-// they are next to each other, a unit is two runs of eight channels; else its channels are taken one by one.  No two units share
-// a channel, so rows may be rotated in place.
-enum Turn { TURN_NONE, TURN_HALVES, TURN_ADJACENT, TURN_ANY };
+// by freq[c]; channels past dims are pairs that stay.  Pairs next to each other make a unit of two runs of eight channels.  Pairs
+// (c, c + dims/2) are taken in runs of as many as divide dims/2, eight where they can be: a run of a's and a run of b's.  No two
+// units share a channel, so rows may be rotated in place.
+enum Turn { TURN_NONE, TURN_ADJACENT, TURN_HALVES, TURN_HALVES_4, TURN_HALVES_2, TURN_HALVES_1 };
+constexpr int run_of(int kind) { return kind == TURN_HALVES_4 ? 4 : kind == TURN_HALVES_2 ? 2 : kind == TURN_HALVES_1 ? 1 : 8; }
 struct RotaryRefs {
   const double *freq;
   float magnitude, sign;              // -1: the transpose
@@ -66,18 +67,16 @@ struct RotaryRefs {
 };
 static inline RotaryRefs ig_rotary_refs(const ig_rotary *r, int inverse) {
   if (!r) return RotaryRefs{nullptr, 1.f, 1.f, 0, TURN_NONE};
-  return RotaryRefs{r->freq, r->magnitude, inverse ? -1.f : 1.f, r->dims, r->interleaved ? TURN_ADJACENT : (r->dims % 16 ? TURN_ANY : TURN_HALVES)};
+  const int half = r->dims / 2, halves = half % 8 == 0 ? TURN_HALVES : half % 4 == 0 ? TURN_HALVES_4 : half % 2 == 0 ? TURN_HALVES_2 : TURN_HALVES_1;
+  return RotaryRefs{r->freq, r->magnitude, inverse ? -1.f : 1.f, r->dims, r->interleaved ? TURN_ADJACENT : halves};
 }
+// where the a's and the b's of the run of pairs from pair c on begin
 struct Runs {
   int first, second;
 };
-template <int KIND> __device__ __forceinline__ Runs runs_of(int s, int dims) {
-  const bool halves = KIND == TURN_HALVES && 16 * s < dims;
-  return Runs{halves ? 8 * s : 16 * s, halves ? 8 * s + dims / 2 : 16 * s + 8};
-}
-// TURN_ANY: channel x (0: a, 1: b) of pair c
-__device__ __forceinline__ int any_channel(int c, int x, int dims) {
-  return 2 * c < dims ? c + (x ? dims / 2 : 0) : 2 * c + x;
+template <int KIND> __device__ __forceinline__ Runs runs_of(int c, int dims) {
+  const bool halves = KIND >= TURN_HALVES && 2 * c < dims;
+  return Runs{halves ? c : 2 * c, halves ? c + dims / 2 : 2 * c + run_of(KIND)};
 }
 // Cosine and sine of pos * freq: the product and the reduction to a quarter turn in double (a float32 angle of a far position
 // has no phase left), the Taylor polynomials to x^13 and x^12 in float32 on [-pi/4, pi/4] (truncation below 2^-40).
@@ -105,71 +104,70 @@ __device__ __forceinline__ void turns_of(int s, int pos, const RotaryRefs &r, fl
     if (e % 2) asm volatile("" : "+v"(turn[e - 1].x), "+v"(turn[e - 1].y), "+v"(turn[e].x), "+v"(turn[e].y));
   }
 }
-// eight values of a row
-template <typename T> struct Run8;
-template <> struct Run8<half_t> {
-  uint4 v;
-  __device__ __forceinline__ void load(const half_t *p) { v = *reinterpret_cast<const uint4 *>(p); }
-  __device__ __forceinline__ void set(int e, half_t x) {
-    half8 h = __builtin_bit_cast(half8, v);
-    h[e] = x;
-    v = __builtin_bit_cast(uint4, h);
+// N values of a row, up to 16 bytes a load
+template <typename T, int N> struct RunOf {
+  static constexpr int PER = N * (int)sizeof(T) <= 16 ? N : 16 / (int)sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(PER)));
+  vec v[N / PER];
+  __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+    for (int i = 0; i < N / PER; ++i) v[i] = reinterpret_cast<const vec *>(p)[i];
   }
   __device__ __forceinline__ void get(float *x) const {
-    const half8 h = __builtin_bit_cast(half8, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)h[e];
+    for (int e = 0; e < N; ++e) x[e] = (float)v[e / PER][e % PER];
   }
-  static __device__ __forceinline__ void store(half_t *p, const float *x) {
-    half8 h;
+  static __device__ __forceinline__ void store(T *p, const float *x) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = (half_t)x[e];
-    *reinterpret_cast<uint4 *>(p) = __builtin_bit_cast(uint4, h);
-  }
-};
-template <> struct Run8<float> {
-  floatx4 v[2];
-  __device__ __forceinline__ void load(const float *p) {
-    v[0] = reinterpret_cast<const floatx4 *>(p)[0], v[1] = reinterpret_cast<const floatx4 *>(p)[1];
-  }
-  __device__ __forceinline__ void set(int e, float x) { v[e / 4][e % 4] = x; }
-  __device__ __forceinline__ void get(float *x) const {
+    for (int i = 0; i < N / PER; ++i) {
+      vec y;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = v[e / 4][e % 4];
-  }
-  static __device__ __forceinline__ void store(float *p, const float *x) {
-    reinterpret_cast<floatx4 *>(p)[0] = floatx4{x[0], x[1], x[2], x[3]};
-    reinterpret_cast<floatx4 *>(p)[1] = floatx4{x[4], x[5], x[6], x[7]};
-  }
-};
-
-// a unit's values: x[0 .. 7] the first run, x[8 .. 15] the second (channels one by one: the pairs' a, the pairs' b)
-template <typename T, int KIND> struct Unit {
-  Run8<T> lo, hi;
-  static __device__ __forceinline__ bool one_by_one(int dims) { return KIND == TURN_ANY && dims > 0; }
-  __device__ __forceinline__ void load(const T *row, int s, int dims) {
-    if (one_by_one(dims)) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) lo.set(e, row[any_channel(8 * s + e, 0, dims)]), hi.set(e, row[any_channel(8 * s + e, 1, dims)]);
-      return;
+      for (int e = 0; e < PER; ++e) y[e] = (T)x[i * PER + e];
+      reinterpret_cast<vec *>(p)[i] = y;
     }
-    const Runs c = runs_of<KIND>(s, dims);
-    lo.load(row + c.first);
-    hi.load(row + c.second);
+  }
+};
+// a unit's values: x[0 .. 7] the a's (of pairs next to each other: the first run), x[8 .. 15] the b's (the second)
+template <typename T, int KIND> struct Unit {
+  static constexpr int G = run_of(KIND);
+  RunOf<T, G> lo[8 / G], hi[8 / G];
+  __device__ __forceinline__ void load(const T *row, int s, int dims) {
+#pragma unroll
+    for (int j = 0; j < 8 / G; ++j) {
+      const Runs c = runs_of<KIND>(8 * s + G * j, dims);
+      lo[j].load(row + c.first);
+      hi[j].load(row + c.second);
+    }
   }
   __device__ __forceinline__ void get(float (&x)[16]) const {
-    lo.get(x);
-    hi.get(x + 8);
+#pragma unroll
+    for (int j = 0; j < 8 / G; ++j) {
+      lo[j].get(x + G * j);
+      hi[j].get(x + 8 + G * j);
+    }
   }
   static __device__ __forceinline__ void store(T *row, int s, int dims, const float (&x)[16]) {
-    if (one_by_one(dims)) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) row[any_channel(8 * s + e, 0, dims)] = (T)x[e], row[any_channel(8 * s + e, 1, dims)] = (T)x[8 + e];
-      return;
+    for (int j = 0; j < 8 / G; ++j) {
+      const Runs c = runs_of<KIND>(8 * s + G * j, dims);
+      RunOf<T, G>::store(row + c.first, x + G * j);
+      RunOf<T, G>::store(row + c.second, x + 8 + G * j);
     }
-    const Runs c = runs_of<KIND>(s, dims);
-    Run8<T>::store(row + c.first, x);
-    Run8<T>::store(row + c.second, x + 8);
+  }
+  // the same of codes, four a word: c[0], c[1] those of x[0 .. 7], c[2], c[3] of x[8 .. 15]
+  static __device__ __forceinline__ void store_codes(char *row, int s, int dims, const unsigned (&c)[4]) {
+#pragma unroll
+    for (int j = 0; j < 8 / G; ++j) {
+      const Runs at = runs_of<KIND>(8 * s + G * j, dims);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        char *to = row + (b ? at.second : at.first);
+        if constexpr (G == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(c[2 * b], c[2 * b + 1]);
+        else if constexpr (G == 4) *reinterpret_cast<unsigned *>(to) = c[2 * b + j];
+        else if constexpr (G == 2) *reinterpret_cast<unsigned short *>(to) = (unsigned short)(c[2 * b + j / 2] >> j % 2 * 16);
+        else *to = (char)(c[2 * b + j / 4] >> j % 4 * 8);
+      }
+    }
   }
 };
 // (channels that stay are not multiplied: an infinity there would make a NaN of its neighbour)

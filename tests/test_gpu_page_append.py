@@ -111,7 +111,7 @@ def test_few_rows(ctx, dtype, code, T, dims, interleaved):
 
 
 @pytest.mark.parametrize("fused", [False, True])
-@pytest.mark.parametrize("dims,interleaved", [(128, False), (128, True), (40, False), (None, False)])
+@pytest.mark.parametrize("dims,interleaved", [(128, False), (128, True), (40, False), (20, False), (6, False), (20, True), (None, False)])
 def test_ragged(ctx, fused, dims, interleaved):
     """Counts of zero and out of range, sequences that end at their capacity or behind it, positions of the caller's."""
     run_append(ctx, "f16", "i8", 128, B=6, H=2, group=4, T=40, page=32, start=[0, 90, 70, 100, 99, 33], n_append=[40, 40, 0, 5, -3, 1000], N_cap=100,
