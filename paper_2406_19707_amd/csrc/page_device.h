@@ -12,7 +12,7 @@ struct PageRefs {
 static inline PageRefs ig_page_refs(const ig_desc *d, const ig_pages *p) {
   PageRefs r;
   r.table = p->table, r.K = static_cast<char *>(p->K), r.V = static_cast<char *>(p->V), r.K_scale = p->K_scale, r.V_scale = p->V_scale;
-  r.n_pages = (unsigned)p->n_pages, r.page_bytes = (unsigned)(d->H * p->page_size * d->d);
+  r.n_pages = (unsigned)p->n_pages, r.page_bytes = (unsigned)d->H * (unsigned)p->page_size * (unsigned)d->d;      // (at most 2^31)
   r.stride = p->table_stride, r.shift = __builtin_ctz(p->page_size), r.H = d->H;
   return r;
 }
