@@ -669,6 +669,11 @@ int row_block(const ig_desc *d, long R) {
 // its takes longer.  (16 x 8 heads of 4096, 40 rows: 47 us there, 53 here; d = 64, 48 rows 32 and 35; d = 256, 20 rows 75 and
 // 115, 60 rows, 4 x 8 of 4000, 45 and 50; 56 rows, 3 x 11 ragged of 4923, 23 and 26; but 72 rows, 16 x 8 of 4096, 66 and 59.)
 bool many_rows(const ig_desc *d, long R) { return d->dtype == IG_F16 && R > 64; }
+// page_prompt's: at d = 128 eight waves or four.  Eight where most of what the rows see is seen by all of them (317 x 4 query rows
+// over up to 9001, 4 x 8 heads: 197 us, 206 with four), four for prompts, where a block of 256 rows works out more that its first
+// rows do not see (2048 over 2048, 8 x 32 heads: 380 us, 394 with eight; no difference with 4 x 8 heads of 4 query heads each).  At
+// d = 64 two row blocks a wave or one: two where workgroups enough are left (2048 over 2048, 4 x 32 heads 113 us, 123 with one;
+// 4 x 16 of 2 query heads each 106 and 117), one where not (317 x 4 over up to 9001, 4 x 8 heads: 116 us, 125 with two).
 int prompt_rows(const ig_desc *d, const PageCall &c) {
   const long R = (long)c.n_q * c.group;
   if (d->d == 128) return R > 128 && 2 * (long)c.n_q <= d->N ? 256 : 128;

@@ -226,7 +226,9 @@ template <typename T, int D, bool E4M3> __global__ __launch_bounds__(256) void g
 }
 
 // Heads that are taken one after the other, so that turns are worked out once for them: one where that is what fills the GPU
-// with waves, up to eight where there are enough.
+// with waves, up to eight where there are enough.  (One and eight.  The kernel alone: a row each for 16 ragged sequences of 8 heads
+// with their 4 query heads each, 5.0 and 12.7 us; 317 rows each for 3 ragged sequences of 12 heads of 64 in float32, 7.3 and 14.1;
+// one row of 4 heads rotated 2.7 and 3.4.  The whole call: 2048 rows each for 16 x 32 heads 611 and 408 us, rotated alone 126 and 102.)
 int heads_each(int heads, double threads) {
   int per = 1;
   while (per < 8 && per < heads && threads / (2 * per) >= 65536.0) per *= 2;
