@@ -519,8 +519,8 @@ typedef struct {
 } ig_pages;
 
 /* Common to the calls below: B, H, d, N, N_cap, dtype and (attention) scale of the descriptor are used as in the calls over whole
- * pools, with N_cap the slots a sequence may have; d = 32, 64, 128 or 256.  Entries of the table outside [0, n_pages) are
- * clamped into it where slots are read, and nothing is written through them.  Entries of pages that a sequence does not reach are
+ * pools, with N_cap the slots a sequence may have, at most 2^30 (IG_ESHAPE); d = 32, 64, 128 or 256.  Entries of the table outside
+ * [0, n_pages) are clamped into it where slots are read, and nothing is written through them.  Entries of pages that a sequence does not reach are
  * not looked at.  Several sequences may share pages that are only read; a page that a call appends to belongs to one sequence
  * and stands once in its row of the table.
  *

@@ -1119,6 +1119,8 @@ static int check_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, const c
     return ig_fail(ctx, IG_ESHAPE, "%s: pages of %d slots", what, p->page_size);
   if (p->n_pages < 1 || (double)p->n_pages * d->H > 2147483647.0)
     return ig_fail(ctx, IG_ESHAPE, "%s: %d pages", what, p->n_pages);
+  // (slots are 32-bit: the end of a page or a turn behind the last one, too)
+  if (d->N_cap > 1 << 30) return ig_fail(ctx, IG_ESHAPE, "%s: N_cap = %d, at most 2^30", what, d->N_cap);
   if (p->table_stride < 1 || (int64_t)p->table_stride * p->page_size < d->N_cap)
     return ig_fail(ctx, IG_ESHAPE, "%s: %d entries of %d slots do not hold N_cap = %d", what, p->table_stride, p->page_size, d->N_cap);
   if (!p->table || !p->K || !p->V || !p->K_scale || !p->V_scale) return ig_fail(ctx, IG_EINVAL, "%s: NULL argument among the pages", what);

@@ -330,3 +330,15 @@ def test_more_than_a_launch_takes(ctx):
     refused(ig.IG_ESHAPE, ctx.ig_append_pages, desc(1 << 8, 1 << 11, 32, 1, 1, "f16"), p.struct(n_pages=1), None, 64, 4, bad, x, x, 0, None, None, None, x)
     refused(ig.IG_ESHAPE, ctx.ig_gather_pages, desc(1 << 8, 1 << 8, 256, 1, 1, "f32"), p.struct(n_pages=1), x, 1 << 24, x, bad, x)
     refused(ig.IG_ESHAPE, ctx.ig_page_attention, desc(1 << 14, 1 << 10, 32, 1, 1, "f16"), p.struct(n_pages=1), 1, 1, bad, None, None, x)
+
+
+@pytest.mark.parametrize("N_cap, code", [(1 << 30, ig.IG_EINVAL), ((1 << 30) + 1, ig.IG_ESHAPE), (2 ** 31 - 1, ig.IG_ESHAPE)])
+def test_slots_past_32_bits_are_refused(ctx, N_cap, code):
+    """A page that ends at slot 2^31 has no end in 32 bits.  (Nothing is launched: every call has an unaligned array, refused later.)"""
+    p = Pages(1, 1, 64, 16, 16, "i8", 1)
+    x = torch.zeros(4096, dtype=torch.float16, device="cuda")
+    bad, idx = x.data_ptr() + 2, i32([0])
+    st, ds = p.struct(table_stride=1 << 27), desc(1, 1, 64, 1, N_cap, "f16")
+    refused(code, ctx.ig_append_pages, ds, st, None, 1, 1, None, bad, x, 0, None, None, None, None)
+    refused(code, ctx.ig_page_attention, ds, st, 1, 1, bad, None, None, x)
+    refused(code, ctx.ig_gather_pages, ds, st, idx, 1, idx, bad, x)
