@@ -525,7 +525,7 @@ typedef struct {
  * and stands once in its row of the table.
  *
  * Appends rows to ragged sequences as ig_append_rows does, rotated and rounded to 8 bits on the way.  For j < n_append[b], slot
- * kv_len[b] + j of sequence b receives k_rows[b, j] rotated at pos[b] + j (pos: device int32 [B], or NULL: the slot), and
+ * kv_len[b] + j of sequence b receives k_rows[b, j] rotated at pos[b] + j < 2^31 (pos: device int32 [B], or NULL: the slot), and
  * v_rows[b, j]; slots >= N_cap are skipped.  rotary NULL: keys are taken as they are.
  * q (or NULL): device [B, n_rows, H*group, d], rotated at the same positions into q_out (dense; may be q where that is dense too),
  * rows j < n_append[b] of it; the others are left as they were.  Without q, group and q_out are not used.
