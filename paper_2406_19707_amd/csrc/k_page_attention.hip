@@ -53,6 +53,9 @@ template <int W, bool ONCE> __device__ __forceinline__ void load_codes_of(const 
 
 // K's largest scale: with half-precision queries less, so that its product with the logits' scale stays finite
 template <bool F32> constexpr int k_scale_most() { return F32 ? SCALE_MOST : 100; }
+// The factor of the logits, from K's scale and the queries' or the logits' own: above zero, so that a masked slot's -infinity stays one,
+// and finite, so that a product of zero stays zero.  (Products of codes and queries are below 2^34: at 2^-126 a logit is zero either way.)
+__device__ __forceinline__ float factor_of(float k, float own) { return __builtin_amdgcn_fmed3f(k * own, 0x1p-126f, 0x1.fffffep127f); }
 
 // a float as two halves: x - hi - lo is at most 2^-22 |x|, or 2^-25
 struct Halves {
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
     half8 wf[NT][PARTS];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float by = k_by * q_scale[n];
+      const float by = factor_of(k_by, q_scale[n]);
       float top = s[n][0][0];
 #pragma unroll
       for (int m = 0; m < 2; ++m)
@@ -575,7 +578,7 @@ template <int D, int NW, int RB, bool E4M3> __global__ __launch_bounds__(NW * 64
       };
       auto ready = [&](float2 s) __attribute__((always_inline)) {
         const int ke = scale_exponent<k_scale_most<false>()>(s.x), ve = scale_exponent(s.y);
-        return Scales{exp2_int(ke) * a.c, (float)ve, exp2_int(-ve)};
+        return Scales{factor_of(exp2_int(ke), a.c), (float)ve, exp2_int(-ve)};
       };
       Scales now = ready(scales_of(e0)), before = now;
       float2 ahead;
