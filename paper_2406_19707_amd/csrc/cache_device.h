@@ -128,6 +128,12 @@ __device__ __forceinline__ int node_read(unsigned long long seen, int j) { retur
 // 2^x to the last bit but one; denormal results are zero (a weight of 2^-126 of the largest)
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// y + x 2^d for d <= 0.  A sum of weights may be far from one (over pages of codes, by a page's scale), so that x 2^d counts where
+// 2^d alone is below the smallest float: two factors, of which the second one is 1 down to d = -100.
+__device__ __forceinline__ float add_scaled(float y, float x, float d) {
+  return fmaf(x * exp2_fast(fminf(d + 100.f, 0.f)), exp2_fast(fmaxf(d, -100.f)), y);
+}
+
 // 1 / sum, zero for a row without weights
 __device__ __forceinline__ float inverse_of(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
 

@@ -607,15 +607,15 @@ template <int E> __device__ __forceinline__ Joined<E> join_row(const StreamArgs 
     float ref = j.ref;
 #pragma unroll
     for (int u = 0; u < U; ++u) ref = fmaxf(ref, ml[u].x);          // (the last slice again and again is the same)
-    const float shrink = exp2_fast(j.ref - ref);
-    j.sum *= shrink, j.ref = ref;
+    const float shrink = exp2_fast(j.ref - ref);          // (of outputs)
+    j.sum = add_scaled(0.f, j.sum, j.ref - ref), j.ref = ref;
 #pragma unroll
     for (int k = 0; k < E; ++k) j.out[k] *= shrink;
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (s0 + u < span.slices) {
         const float by = exp2_fast(ml[u].x - ref);
-        j.sum = fmaf(ml[u].y, by, j.sum);
+        j.sum = add_scaled(j.sum, ml[u].y, ml[u].x - ref);
 #pragma unroll
         for (int k = 0; k < E; ++k) j.out[k] = fmaf(__uint_as_float(o[u][k]), by, j.out[k]);
       }

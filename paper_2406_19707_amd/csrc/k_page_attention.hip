@@ -57,6 +57,14 @@ template <bool F32> constexpr int k_scale_most() { return F32 ? SCALE_MOST : 100
 // and finite, so that a product of zero stays zero.  (Products of codes and queries are below 2^34: at 2^-126 a logit is zero either way.)
 __device__ __forceinline__ float factor_of(float k, float own) { return __builtin_amdgcn_fmed3f(k * own, 0x1p-126f, 0x1.fffffep127f); }
 
+// Float32: a lane's sum is worked out without its page's scale of V where its largest weight times scale is below 2^FAR.  With ev >=
+// SCALE_LEAST such a lane's logits are 10 or more below the reference, which is at most SCALE_MOST above the largest logit: what
+// counts of 2^(logit - reference) lies between about 2^-(SCALE_MOST + 30) and 2^-10, and 2^FAR_LIFT times that is in range.  (In half precision a weight that is lost
+// so belongs to a row with a weight times scale of 2^46 of its largest weight and more: infinite where that one's code is not zero, and
+// where it is, the others are below what weights as halves keep.)
+constexpr float FAR = -90.f;
+constexpr int FAR_LIFT = 64;
+
 // a float as two halves: x - hi - lo is at most 2^-22 |x|, or 2^-25
 struct Halves {
   half_t hi, lo;
@@ -76,7 +84,8 @@ __device__ __forceinline__ Halves split(float x) {
 //    by four.  Those eight slots lie in one page: its scales are the lane's.
 // K's scale goes into the factor of the logits.  V's scale 2^ev goes into the exponent of the weights, which are
 // exp2(l + ev - ref) with ref the largest l + ev (or LIFT less): so no page's scale takes them out of half precision's range, and
-// sums take them times 2^-ev.  Float32 queries and weights are two halves each, and their products two.
+// sums take them times 2^-ev, or without ev where a page of small values beside one of large ones would take all of a lane's
+// weights below the smallest float (FAR): outputs do without them, but not the sum.  Float32 queries and weights are two halves each, and their products two.
 // Bound by memory: one token of 16 x 32 heads over 4096 slots, d = 128, 84 us = 6.4 TB/s (a plain read reaches 6.3; the same over halves
 // 177), of 16 x 8 x 4 ragged heads over 32768 115 us = 6.0; float32 16 x 32 over 4096 90 us.  V is asked for with K, a turn ahead:
 // asked for after its own turn's products, 8 x 32 heads of 2048 took 32 us instead of 31.
@@ -236,11 +245,12 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, s[n][m][r]);
-      top = column_max(fmaf(top, by, lift_v));
+      const float mine = fmaf(top, by, lift_v);
+      top = column_max(mine);
       const float ref = fmaxf(m_run[n], lifted(top, LIFT));
       if (__any(ref > m_run[n])) {
         const float shrink = exp2_fast(m_run[n] - ref);
-        l_run[n] *= shrink;
+        l_run[n] = add_scaled(0.f, l_run[n], m_run[n] - ref);
 #pragma unroll
         for (int j = 0; j < CJ; ++j) acc[n][j] *= shrink;
         m_run[n] = ref;
@@ -259,7 +269,19 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
             wf[n][0][4 * m + r] = (half_t)x;
           }
         }
-      l_run[n] = fmaf(sum, v_back, l_run[n]);
+      float back = v_back;
+      if constexpr (F32) {
+        const bool far = mine - ref < FAR && mine > NOTHING_SEEN;
+        if (__any(far)) {                                 // (before the weights it takes more registers: 2 x 16 heads of 1024 tokens 55 us, not 51)
+          float y = 0.f;
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y += exp2_fast(fmaf(s[n][m][r], by, FAR_LIFT - ref));
+          sum = far ? y : sum, back = far ? exp2_int(-FAR_LIFT) : back;
+        }
+      }
+      l_run[n] = fmaf(sum, back, l_run[n]);
     }
 #pragma unroll
     for (int x = 0; x < VW; ++x) {
@@ -322,9 +344,8 @@ __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs 
     floatx4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      const float by = exp2_fast(box_m[x][at] - m);
-      l = fmaf(box_l[x][at], by, l);
-      o += *reinterpret_cast<const floatx4 *>(boxes[x] + at * LDB + e) * by;
+      l = add_scaled(l, box_l[x][at], box_m[x][at] - m);
+      o += *reinterpret_cast<const floatx4 *>(boxes[x] + at * LDB + e) * exp2_fast(box_m[x][at] - m);
     }
     if (a.slices == 1) {
       const float inv = inverse_of(l);
@@ -662,8 +683,8 @@ template <int D, int NW, int RB, bool E4M3> __global__ __launch_bounds__(NW * 64
 int div_up(long n, long d) { return (int)((n + d - 1) / d); }
 
 // Query rows of a workgroup: page_stream's 16 or 32, page_prompt's 128 or 256 (as over a pool of rows, by the same rules).
-// In float32 32 only where turns of 128 slots are enough to fill the GPU with (2 x 16 heads of 1024 tokens 48 us with 32, 55 with 16; 20
-// rows, 16 x 8 of 4096, 37 and 43; but 4 heads of 512 9.2 and 6.7).
+// In float32 32 only where turns of 128 slots are enough to fill the GPU with (whole calls, d = 128: 2 x 16 heads of 1024 tokens 51
+// us with 32, 55 with 16; 20 rows, 16 x 8 of 4096, 39 and 48; but 4 heads of 512 13.7 and 10.0).
 int row_block(const ig_desc *d, long R) {
   if (R <= 16 || d->d > 128) return 16;
   return d->dtype == IG_F16 || (double)d->B * d->H * div_up(R, 32) * div_up(d->N, 128) >= 1024 ? 32 : 16;
