@@ -1147,7 +1147,7 @@ int ig_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *pages, const 
   int rc = check_pages(ctx, d, pages, what, group, n_rows, stream);
   if (rc) return rc;
   const int Hq = q ? d->H * group : 0, size = ig_elem_bytes(d->dtype);
-  // (2^26 rows, of queries too, are a launch of at most 2^29 threads)
+  if (ig_append_pages_threads(d, pages, Hq, n_rows) > IG_MOST_THREADS) return ig_fail(ctx, IG_ESHAPE, "%s: too many rows for a launch", what);
   if (!k_rows || !v_rows || (q && !q_out)) return ig_fail(ctx, IG_EINVAL, "%s: NULL argument", what);
   if (rotary && (rc = check_rotary(ctx, what, rotary, d->d))) return rc;
   if ((rc = check_aligned(ctx, what, {q, k_rows, v_rows, q_out}))) return rc;

@@ -320,6 +320,7 @@ int ig_launch_append_rows(ig_ctx *ctx, const ig_desc *d, int n_rows, const void 
 long ig_rotate_threads(int n, int heads, int d);
 int ig_launch_rotate(ig_ctx *ctx, int dtype, int n, int heads, int d, const ig_rotary *rotary, int inverse, const int32_t *pos, const void *x,
                      long x_stride, void *out, long out_stride, hipStream_t s);
+long ig_append_pages_threads(const ig_desc *d, const ig_pages *p, int Hq, int n_rows);
 int ig_launch_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, const ig_rotary *rotary, int Hq, int n_rows, const void *q,      // Hq = 0: no queries
                            const void *k, const void *v, long row_stride, const int32_t *n_append, const int32_t *kv_len, const int32_t *pos,
                            void *q_out, hipStream_t s);

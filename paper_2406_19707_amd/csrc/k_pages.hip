@@ -248,7 +248,27 @@ int append_each(const ig_desc *d, const ig_pages *p, int n_rows) {
   return heads_each(d->H, 2.0 * d->B * append_page_count(p, n_rows) * d->H * append_team(d, p, n_rows));
 }
 
+// An append's launch: workgroups of `team` threads for the new rows of a page, of K or of V, and behind them those that rotate queries.
+struct AppendGrid {
+  int pages, per, parts, q_per, q_parts, team;
+  long kv_blocks, q_total;            // (at most 2^27 and 2^30: there are at most 2^26 rows, of queries too)
+};
+AppendGrid append_grid(const ig_desc *d, const ig_pages *p, int Hq, int n_rows) {
+  AppendGrid g;
+  const long n = (long)d->B * n_rows;
+  g.pages = append_page_count(p, n_rows), g.team = append_team(d, p, n_rows);
+  g.per = append_each(d, p, n_rows), g.q_per = Hq ? rotate_each(n, Hq, d->d) : 1;
+  g.parts = div_up(d->H, g.per), g.q_parts = Hq ? div_up(Hq, g.q_per) : 1;
+  g.kv_blocks = 2l * d->B * g.pages * g.parts, g.q_total = Hq ? n * g.q_parts * (d->d / 16) : 0;
+  return g;
+}
+
 }  // namespace
+
+long ig_append_pages_threads(const ig_desc *d, const ig_pages *p, int Hq, int n_rows) {
+  const AppendGrid g = append_grid(d, p, Hq, n_rows);
+  return (g.kv_blocks + div_up(g.q_total, g.team)) * g.team;
+}
 
 long ig_rotate_threads(int n, int heads, int d) { return (long)n * div_up(heads, rotate_each(n, heads, d)) * (d / 16) + 255; }
 
@@ -302,15 +322,11 @@ int ig_launch_append_pages(ig_ctx *ctx, const ig_desc *d, const ig_pages *p, con
   a.q = q, a.k = k, a.v = v, a.q_out = q_out, a.n_append = n_append, a.kv_len = kv_len, a.pos = pos;
   a.q_stride = row_stride ? row_stride : (long)Hq * d->d, a.kv_stride = row_stride ? row_stride : (long)d->H * d->d;
   a.H = d->H, a.Hq = Hq, a.d = d->d, a.unit_shift = __builtin_ctz(d->d / 16), a.N = d->N, a.N_cap = d->N_cap, a.n_rows = n_rows;
-  const int n = d->B * n_rows, pages = append_page_count(p, n_rows);
-  a.per = append_each(d, p, n_rows), a.q_per = Hq ? rotate_each(n, Hq, d->d) : 1;
-  const int parts = div_up(d->H, a.per), q_parts = Hq ? div_up(Hq, a.q_per) : 1;
-  a.kv_blocks = 2 * d->B * pages * parts;
-  a.q_total = q ? n * q_parts * (d->d / 16) : 0;
-  a.by_pages = ig_fast_div(pages), a.by_parts = ig_fast_div(parts), a.by_rows = ig_fast_div(n_rows), a.by_q_parts = ig_fast_div(q_parts);
+  const AppendGrid g = append_grid(d, p, Hq, n_rows);
+  a.per = g.per, a.q_per = g.q_per, a.kv_blocks = (int)g.kv_blocks, a.q_total = (int)g.q_total;
+  a.by_pages = ig_fast_div(g.pages), a.by_parts = ig_fast_div(g.parts), a.by_rows = ig_fast_div(n_rows), a.by_q_parts = ig_fast_div(g.q_parts);
   a.r = ig_rotary_refs(rotary, 0);
-  const int team = append_team(d, p, n_rows);
-  const dim3 grid((unsigned)(a.kv_blocks + div_up(a.q_total, team))), block(team);
+  const dim3 grid((unsigned)(a.kv_blocks + div_up(a.q_total, g.team))), block(g.team);
 #define APPEND(T, E4M3, KIND)                                                                        \
   {                                                                                                  \
     auto kernel = append_pages<T, E4M3, KIND>;                                                       \
