@@ -546,7 +546,9 @@ int ig_append_pages(ig_ctx *ctx, const ig_desc *desc, const ig_pages *pages, con
  * group as there, and the same expectations of finite rows and logits.  Products and sums are in float32; with IG_F16 the
  * softmax weights, times their page's scale, are rounded to half precision where they multiply the codes of V, by at most 2^-11
  * of themselves down to 2^-23 of the row's largest (calls of up to 64 query rows a pool head: 2^-28), and by at most 2^-34 of that
- * below; with IG_F32 queries and weights are taken as two halves each: off by at most 2^-22 of themselves, or 2^-38 of a row's largest. */
+ * below; with IG_F32 queries and weights are taken as two halves each: off by at most 2^-22 of themselves, or 2^-38 of a row's largest.
+ * A slot's share of the softmax's sum does not depend on its page's scale of V; with IG_F16 as long as these lie within 2^100 of
+ * each other, as those of pages filled with half-precision rows do. */
 int ig_page_attention(ig_ctx *ctx, const ig_desc *desc, const ig_pages *pages, int32_t group, int32_t n_q, const void *q,
                       const int32_t *q_len, const int32_t *kv_len, void *out, void *stream);
 

@@ -338,7 +338,7 @@ struct PagePlan {
   int rb, nrb, slices;                          // query rows of a workgroup, row blocks and slices of a pool head
   bool prompt;
   long threads;                                 // of the largest launch
-  size_t part_ml_at, part_at, bytes;            // parts of the workspace
+  size_t part_at, bytes;                        // parts of the workspace
 };
 PagePlan ig_page_plan(const ig_desc *d, const PageCall &c);
 size_t ig_page_reserve_bytes(const ig_desc *d, int group, int n_q);

@@ -87,7 +87,7 @@ __device__ __forceinline__ Halves split(float x) {
 // sums take them times 2^-ev, or without ev where a page of small values beside one of large ones would take all of a lane's
 // weights below the smallest float (FAR): outputs do without them, but not the sum.  Float32 queries and weights are two halves each, and their products two.
 // Bound by memory: one token of 16 x 32 heads over 4096 slots, d = 128, 84 us = 6.4 TB/s (a plain read reaches 6.3; the same over halves
-// 177), of 16 x 8 x 4 ragged heads over 32768 115 us = 6.0; float32 16 x 32 over 4096 90 us.  V is asked for with K, a turn ahead:
+// 177), of 16 x 8 x 4 ragged heads over 32768 116 us = 6.0 among other calls (121 on a GPU that was idle before); float32 16 x 32 over 4096 90 us.  V is asked for with K, a turn ahead:
 // asked for after its own turn's products, 8 x 32 heads of 2048 took 32 us instead of 31.
 template <int D, int NT, bool E4M3, bool F32, bool ONCE>
 __global__ __launch_bounds__(256, D <= 128 ? 2 : 1) void page_stream(StreamArgs a, PageRefs p) {
@@ -691,7 +691,9 @@ int row_block(const ig_desc *d, long R) {
 }
 // page_stream's row blocks read the codes again for every 32 (d = 256: 16) rows, out of the caches, page_prompt's 128 once, but a turn of
 // its takes longer.  (16 x 8 heads of 4096, 40 rows: 47 us there, 53 here; d = 64, 48 rows 32 and 35; d = 256, 20 rows 75 and
-// 115, 60 rows, 4 x 8 of 4000, 45 and 50; 56 rows, 3 x 11 ragged of 4923, 23 and 26; but 72 rows, 16 x 8 of 4096, 66 and 59.)
+// 115, 60 rows, 4 x 8 of 4000, 45 and 50; 56 rows, 3 x 11 ragged of 4923, 23 and 26; but 72 rows, 16 x 8 of 4096, 66 and 59.
+// Where a few heads leave the GPU mostly empty page_stream is the faster one beyond 64 rows, too: a sequence of 1000 slots, d = 128, 256 rows of 1, 4
+// and 8 heads 12, 13 and 19 us, page_prompt 17, 18 and 20; 512 rows of 8 heads over 4096 33 and 33.)
 bool many_rows(const ig_desc *d, long R) { return d->dtype == IG_F16 && R > 64; }
 // page_prompt's: at d = 128 eight waves or four.  Eight where most of what the rows see is seen by all of them (317 x 4 query rows
 // over up to 9001, 4 x 8 heads: 197 us, 206 with four), four for prompts, where a block of 256 rows works out more that its first
